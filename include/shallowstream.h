@@ -126,7 +126,8 @@ size_t ss_index_required_bytes(const ss_index_desc* desc);
  * shallow cache of Sec. 4.1 ("Full-History Shallow Cache", Eq.
  * shallow_streaming_cache) for L_s = P shallow layers, with room for each
  * unit's descriptor (Eq. memory_key).  Only keys are kept: the values of the
- * cache are not read by retrieval.  The arena must stay allocated until
+ * cache are not read by retrieval (ss_index_attach_values keeps them too).  The
+ * arena must stay allocated until
  * ss_index_destroy; the library writes it only through ss_index_append.
  * *out receives the handle (host memory owned by the library).  Errors:
  * SS_ERR_INVALID_ARGUMENT / SS_ERR_UNSUPPORTED for a bad shape, SS_ERR_CAPACITY
@@ -150,8 +151,8 @@ ss_status ss_index_window(const ss_index* idx, int64_t* first_stored, int64_t* f
 
 /* The memory side of long-history compression (Eq.
  * optional_context_compression): the frames that left the detailed window
- * leave the arena too.  Their rows, member counts, descriptors, pooled keys and
- * row offsets are dropped; the stored rows of the detailed frames move to the
+ * leave the arena too.  Their rows (values and weights too, where kept), member
+ * counts, descriptors, pooled keys and row offsets are dropped; the stored rows of the detailed frames move to the
  * start of every (layer, KV head) run of the arena (one kernel on `stream`,
  * in place), so that later appends reuse the space: max_frames and max_rows
  * then bound the frames and rows kept in detail, not the stream's length.  Frame ids stay as they were.  Retrieval,
@@ -167,7 +168,8 @@ ss_status ss_index_compact(ss_index* idx, void* stream);
  * long-term clusters while the recent units and the near history stay in
  * detail).  Mem counts the arena bytes of the frames in the detailed window:
  * a frame of r stored rows takes r*L_s*H_kv*(2d + 4) + (1 + L_s)*H_kv*d*4 + 4
- * bytes (keys, member counts, descriptor, pooled keys, row offset).
+ * bytes (keys, member counts, descriptor, pooled keys, row offset), and another
+ * r*L_s*H_kv*(2d + 4) where the index keeps values (values, weights).
  * *frame_hi (host) receives the smallest frame_hi in [first_detail,
  * max(first_detail, n_frames - n_recent)] whose frames [frame_hi, n_frames) fit
  * in budget_bytes, or the end of that range when none does (the recent window
@@ -178,7 +180,8 @@ ss_status ss_index_budget_split(const ss_index* idx, uint64_t budget_bytes, int6
 /* Append n_frames frames of n_tokens visual tokens each: each unit's keys at
  * every shallow layer join the cache in temporal order (Sec. 4.1, Eq.
  * shallow_streaming_cache; frame t of the paper's stream is frame id t - 1
- * here), and its descriptor (Eq. memory_key) is computed on the device.
+ * here), and its descriptor (Eq. memory_key) is computed on the device.  An
+ * index that keeps values is appended to through ss_index_append_kv instead.
  *   layer_keys  host array of L_s device pointers; pointer l addresses bf16
  *               [H_kv][n_frames*n_tokens][d] keys of shallow layer l (16-byte
  *               aligned).  Frame f owns tokens [f*n_tokens, (f+1)*n_tokens).
@@ -431,6 +434,123 @@ ss_status ss_assemble_evidence(ss_index* const* idx, int32_t n_streams, const in
                                int32_t n_select, const ss_evidence_clusters* clusters,
                                const ss_evidence_params* params, void* stream, int64_t* units, int32_t* kinds,
                                int32_t* n_units, int32_t max_units);
+
+/* A value cache beside the keys (the V of Eq. shallow_streaming_cache) and one
+ * attention weight for each stored row.  Layout of its caller-owned arena
+ * (256-byte aligned parts): values bf16 [L_s][H_kv][max_rows][d], row for row
+ * as the keys; weights fp32 [L_s][H_kv][max_rows].  Its bytes: 0 if `desc` is
+ * invalid.  ss_index_attach_values gives an empty index that arena, which must
+ * stay allocated until ss_index_destroy; frames then come through
+ * ss_index_append_kv.  The library writes values there at append, compaction
+ * and eviction, weights also in ss_attend_accumulate; a caller may write
+ * weights between calls. */
+size_t ss_values_required_bytes(const ss_index_desc* desc);
+ss_status ss_index_attach_values(ss_index* idx, void* dev_arena, size_t arena_bytes);
+
+/* ss_index_append for an index that keeps values: layer_values is a host array
+ * of L_s device pointers laid out as layer_keys.  Rows are stored raw (no
+ * compression) and start with weight 0. */
+ss_status ss_index_append_kv(ss_index* idx, const void* const* layer_keys, const void* const* layer_values,
+                             int32_t n_frames, int32_t n_tokens, void* stream, int64_t* first_frame_id);
+
+/* How attention scores are formed and which rows they reach.  Query head h reads
+ * KV head h / G.  With x = q.k / sqrt(d) the score of a row is
+ *   s = cap(x) - slopes[h] * age,
+ * cap(x) = softcap * tanh(x / softcap), or x when softcap is 0; age = frames
+ * stored so far - the row's frame id (the newest frame has age 1; the question's
+ * own tokens have age 0).  The rows are those of the detailed window (every
+ * frame of the arena from first_detail on, the recent ones among them).
+ *   layer     the shallow layer, 0 .. L_s - 1;
+ *   softcap   0, or 1e-3 .. 1e6;
+ *   slopes    device fp32 [H_q], finite, or NULL for no bias;
+ *   frames    NULL for every row; else device int64 [n_streams][n_listed] frame
+ *             ids: rows of other frames are not seen.  Any order; a frame listed
+ *             twice counts once; negative ids and frames outside the detailed
+ *             window are skipped.  With kinds (device int32 of the same shape,
+ *             may be NULL) entries of a kind other than 0 are skipped too, so
+ *             that the units and kinds of ss_assemble_evidence can be given;
+ *   n_listed  1..4096 with frames, else 0. */
+typedef struct {
+  int32_t layer;
+  float softcap;
+  const float* slopes;
+  const int64_t* frames;
+  const int32_t* kinds;
+  int32_t n_listed;
+} ss_attend_params;
+
+/* Each stream's own tokens at this layer: the text so far, whose last n_q tokens
+ * are the queries.
+ *   keys, values  host arrays of n_streams device pointers to bf16
+ *                 [H_kv][capacity][d] (16-byte aligned); tokens n_own .. capacity
+ *                 are not read.  An entry is not read when its n_own is 0;
+ *   n_own         host array: 0 (the history alone) or n_q .. 2^20;
+ *   capacity      host array: tokens from one KV head to the next, >= n_own;
+ *   parents       NULL, or a host array of device pointers to int32 [n_q], each of
+ *                 which may be NULL.  NULL: query i sees the own tokens up to
+ *                 itself.  Else the queries are a tree of drafted tokens (at most
+ *                 512): parents[i] is the index of draft i's parent among the
+ *                 drafts, below i, and anything outside 0 .. i - 1 makes i a root;
+ *                 draft i sees the tokens before the drafts, its ancestors and
+ *                 itself. */
+typedef struct {
+  const void* const* keys;
+  const void* const* values;
+  const int32_t* n_own;
+  const int32_t* capacity;
+  const int32_t* const* parents;
+} ss_own_tokens;
+
+/* Attention of n_streams questions over the stored history (Eq.
+ * query_full_history_attention), one layer a call: for every query head and token
+ *   out = sum_j p_j v_j,   p = softmax over the visible rows and own tokens of s_j.
+ *   idx      host array of handles of identical shapes, each keeping values (one
+ *            index may stand for several streams);
+ *   queries  host array of n_streams device pointers to bf16 [H_q][n_q][d]
+ *            (16-byte aligned), n_q host array of 1..4096;
+ *   own      NULL: the history alone;
+ *   ws       device workspace of ss_attend_workspace_bytes() bytes, which a call
+ *            leaves dirty: calls that may overlap need one each;
+ *   out      host array of device pointers to bf16 [H_q][n_q][d] (16-byte aligned);
+ *   lse      NULL, or a host array of device pointers to fp32 [H_q][n_q]: the
+ *            natural log of the softmax's denominator, ln sum_j exp(s_j).
+ * A query that sees nothing gives out = 0 and lse = -inf.  Scores, maxima and sums
+ * are fp32; p is rounded to bf16 before it meets the values.  A result depends on
+ * its stream's arguments and on the batch's sizes (how the rows are shared out),
+ * and is the same bit for bit each time. */
+size_t ss_attend_workspace_bytes(ss_index* const* idx, int32_t n_streams, const int32_t* n_q,
+                                 const ss_own_tokens* own, const ss_attend_params* params);
+ss_status ss_attend(ss_index* const* idx, int32_t n_streams, const void* const* queries, const int32_t* n_q,
+                    const ss_own_tokens* own, const ss_attend_params* params, void* ws, size_t ws_bytes,
+                    void* stream, void* const* out, float* const* lse);
+
+/* The attention weight that the queries gave each stored row, added to the
+ * index's weights of that layer: for every row j of the detailed window and KV head
+ *   weight_j = decay * weight_j + sum over its G query heads and n_q tokens of
+ *              exp(s_j - lse),
+ * the sum only for rows that the call sees (params->frames).  decay is in 0..1: 1
+ * adds up, 0 overwrites.  queries, n_q and params as in ss_attend; lse its output
+ * (a host array; a token with lse = -inf adds nothing).  No index may occur twice
+ * in a call. */
+size_t ss_attend_accumulate_workspace_bytes(ss_index* const* idx, int32_t n_streams, const int32_t* n_q,
+                                            const ss_attend_params* params);
+ss_status ss_attend_accumulate(ss_index* const* idx, int32_t n_streams, const void* const* queries,
+                               const int32_t* n_q, const float* const* lse, const ss_attend_params* params,
+                               float decay, void* ws, size_t ws_bytes, void* stream);
+
+/* Eviction by accumulated attention weight: dst receives the detailed window of
+ * src, thinned.  Each frame in [first_detail, frame_hi) keeps, for each (layer, KV
+ * head), the keep_rows rows of the largest weight (all when it has no more; ties to
+ * the earlier row), in their order, with keys, values, weights and member counts;
+ * frames from frame_hi on come whole.  Frame ids, descriptors and pooled keys stay.
+ * src is not changed; what dst held is replaced (both keep values, have the same
+ * shape and separate arenas; capacities and n_recent may differ).  frame_hi is in
+ * [first_detail, max(first_detail, n_frames - n_recent)] of src; keep_rows >= 1.
+ * Every (layer, KV head) of a frame keeps the same number of rows, so all entry
+ * points work on dst as on an index appended to.  Weights must not be NaN.
+ * Fails with SS_ERR_CAPACITY, dst unchanged, when dst is too small; on
+ * SS_ERR_DEVICE dst must be discarded. */
+ss_status ss_index_evict(const ss_index* src, ss_index* dst, int64_t frame_hi, int32_t keep_rows, void* stream);
 
 /* Every score of one list over rows [row0, row0+n_rows) of one index, with the
  * same arithmetic as ss_retrieve (parity only).  queries: host array of L_s

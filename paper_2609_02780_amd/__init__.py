@@ -5,8 +5,8 @@ The work runs in ``libshallowstream.so`` (HIP kernels behind the C ABI of
 ``include/shallowstream.h``); this package only marshals arguments.
 """
 from ._lib import SSError, lib  # noqa: F401
-from .index import (LongClusters, PooledRanker, Retriever, ShallowIndex, assemble_evidence,  # noqa: F401
-                    sample_plan, set_profile_events)
+from .index import (HistoryAttention, LongClusters, PooledRanker, Retriever, ShallowIndex,  # noqa: F401
+                    assemble_evidence, sample_plan, set_profile_events)
 
-__all__ = ["ShallowIndex", "Retriever", "PooledRanker", "LongClusters", "assemble_evidence", "SSError", "sample_plan",
-           "set_profile_events", "lib"]
+__all__ = ["ShallowIndex", "Retriever", "PooledRanker", "LongClusters", "HistoryAttention", "assemble_evidence",
+           "SSError", "sample_plan", "set_profile_events", "lib"]

@@ -61,6 +61,16 @@ class DebugOut(C.Structure):
                 ("list_stats", C.c_void_p)]
 
 
+class AttendParams(C.Structure):
+    _fields_ = [("layer", C.c_int32), ("softcap", C.c_float), ("slopes", C.c_void_p), ("frames", C.c_void_p),
+                ("kinds", C.c_void_p), ("n_listed", C.c_int32)]
+
+
+class OwnTokens(C.Structure):
+    _fields_ = [("keys", C.c_void_p), ("values", C.c_void_p), ("n_own", C.c_void_p), ("capacity", C.c_void_p),
+                ("parents", C.c_void_p)]
+
+
 _P = C.c_void_p
 _SIGS = {
     "ss_index_required_bytes": (C.c_size_t, [C.POINTER(IndexDesc)]),
@@ -100,6 +110,19 @@ _SIGS = {
     "ss_evidence_max_units": (C.c_int32, [C.POINTER(EvidenceParams), C.c_int32, C.c_int32]),
     "ss_assemble_evidence": (C.c_int32, [C.POINTER(_P), C.c_int32, _P, C.c_int32, C.POINTER(EvidenceClusters),
                                          C.POINTER(EvidenceParams), _P, _P, _P, _P, C.c_int32]),
+    "ss_values_required_bytes": (C.c_size_t, [C.POINTER(IndexDesc)]),
+    "ss_index_attach_values": (C.c_int32, [_P, _P, C.c_size_t]),
+    "ss_index_append_kv": (C.c_int32, [_P, C.POINTER(_P), C.POINTER(_P), C.c_int32, C.c_int32, _P,
+                                       C.POINTER(C.c_int64)]),
+    "ss_attend_workspace_bytes": (C.c_size_t, [C.POINTER(_P), C.c_int32, C.POINTER(C.c_int32), C.POINTER(OwnTokens),
+                                               C.POINTER(AttendParams)]),
+    "ss_attend": (C.c_int32, [C.POINTER(_P), C.c_int32, C.POINTER(_P), C.POINTER(C.c_int32), C.POINTER(OwnTokens),
+                              C.POINTER(AttendParams), _P, C.c_size_t, _P, C.POINTER(_P), C.POINTER(_P)]),
+    "ss_attend_accumulate_workspace_bytes": (C.c_size_t, [C.POINTER(_P), C.c_int32, C.POINTER(C.c_int32),
+                                                          C.POINTER(AttendParams)]),
+    "ss_attend_accumulate": (C.c_int32, [C.POINTER(_P), C.c_int32, C.POINTER(_P), C.POINTER(C.c_int32),
+                                         C.POINTER(_P), C.POINTER(AttendParams), C.c_float, _P, C.c_size_t, _P]),
+    "ss_index_evict": (C.c_int32, [_P, _P, C.c_int64, C.c_int32, _P]),
     "ss_debug_sample_plan": (C.c_int32, [C.c_int64, C.c_int32, C.POINTER(C.c_int32)]),
     "ss_set_profile_events": (C.c_int32, [_P, _P]),
     "ss_status_string": (C.c_char_p, [C.c_int32]),

@@ -14,7 +14,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB_NAME = "libshallowstream.so"
 LIB_PATH = os.path.join(HERE, LIB_NAME)
-SOURCES = [os.path.join(CSRC, "ss_kernels.hip"), os.path.join(CSRC, "ss_api.cpp")]
+SOURCES = [os.path.join(CSRC, f) for f in ("ss_kernels.hip", "ss_attend.hip", "ss_api.cpp")]
 ARCH = "gfx950"
 
 # Packed fp32 VALU ops are kept out of every kernel (hipcc would otherwise form

@@ -27,6 +27,9 @@ struct ss_index {
   std::vector<int64_t> off;  // arena row offsets of frames frame_base .. n_frames
   int64_t first_detail = 0;  // frames before it were folded into long-term clusters
   int32_t rpf;               // common rows per frame, 0 if mixed, -1 before the first append
+  uint16_t* values = nullptr;  // [L][H_kv][max_rows][d] bf16, null without a value cache
+  float* weights = nullptr;    // [L][H_kv][max_rows], with the value cache
+  size_t values_bytes = 0;     // of their arena
 };
 
 namespace {
@@ -115,6 +118,18 @@ Layout layout(const ss_index_desc& d) {
   off = align256(off + 16);
   L.total = off;
   return L;
+}
+
+// The value cache's arena: values, then weights.
+struct ValuesLayout {
+  size_t weights, total;
+};
+ValuesLayout values_layout(const ss_index_desc& d) {
+  const size_t rows = (size_t)d.n_layers * d.n_kv_heads * (size_t)d.max_rows;
+  ValuesLayout v{};
+  v.weights = align256(rows * d.head_dim * 2);
+  v.total = align256(v.weights + rows * 4);
+  return v;
 }
 
 bool same_shape(const ss_index_desc& a, const ss_index_desc& b) {
@@ -551,6 +566,285 @@ int64_t evidence_units_max(const ss_evidence_params* p, int32_t n_select, int32_
   return n;
 }
 
+ss_status append_common(ss_index* idx, const void* const* layer_keys, const void* const* layer_values,
+                        int32_t n_frames, int32_t n_tokens, const ss_compress* compress, void* stream,
+                        int64_t* first_frame_id) {
+  const ss_index_desc& d = idx->desc;
+  if (!layer_keys) return fail(SS_ERR_INVALID_ARGUMENT, "layer_keys is NULL");
+  if (n_frames < 1 || n_tokens < 1)
+    return fail(SS_ERR_INVALID_ARGUMENT, "n_frames and n_tokens must be >= 1");
+  if ((int64_t)n_frames * n_tokens > 0x7FFFFFFF)
+    return fail(SS_ERR_UNSUPPORTED, "n_frames * n_tokens exceeds 2^31-1");
+  for (int l = 0; l < d.n_layers; ++l) {
+    if (!layer_keys[l]) return fail(SS_ERR_INVALID_ARGUMENT, "layer_keys[%d] is NULL", l);
+    if (!aligned(layer_keys[l], 16))
+      return fail(SS_ERR_INVALID_ARGUMENT, "layer_keys[%d] not 16-byte aligned", l);
+  }
+  for (int l = 0; layer_values && l < d.n_layers; ++l) {
+    if (!layer_values[l]) return fail(SS_ERR_INVALID_ARGUMENT, "layer_values[%d] is NULL", l);
+    if (!aligned(layer_values[l], 16))
+      return fail(SS_ERR_INVALID_ARGUMENT, "layer_values[%d] not 16-byte aligned", l);
+  }
+  int rpf = n_tokens;
+  if (compress) {
+    if (compress->n_centroids < 1 || compress->n_centroids > ss::kMaxCentroids)
+      return fail(SS_ERR_UNSUPPORTED, "n_centroids %d outside 1..%d", compress->n_centroids,
+                  ss::kMaxCentroids);
+    if (compress->n_iters < 0 || compress->n_iters > 100)
+      return fail(SS_ERR_INVALID_ARGUMENT, "n_iters %d outside 0..100", compress->n_iters);
+    if (n_tokens > ss::kMaxTokensCompress)
+      return fail(SS_ERR_UNSUPPORTED, "compression supports at most %d tokens per frame",
+                  ss::kMaxTokensCompress);
+    rpf = std::min(compress->n_centroids, n_tokens);
+  }
+  const int64_t stored = idx->n_frames - idx->frame_base;
+  if (stored + n_frames > d.max_frames)
+    return fail(SS_ERR_CAPACITY, "%lld stored frames + %d exceeds max_frames %lld", (long long)stored,
+                n_frames, (long long)d.max_frames);
+  const int64_t new_rows = (int64_t)n_frames * rpf;
+  if (idx->n_rows + new_rows > d.max_rows)
+    return fail(SS_ERR_CAPACITY, "%lld rows + %lld exceeds max_rows %lld", (long long)idx->n_rows,
+                (long long)new_rows, (long long)d.max_rows);
+  // the host offsets are reserved before anything is enqueued, so that the
+  // bookkeeping after the launch cannot fail and leave the index behind the
+  // device state
+  // (grown by doubling: reserving each call's few frames alone would copy them all each time)
+  const size_t want = idx->off.size() + (size_t)n_frames;
+  if (want > idx->off.capacity()) idx->off.reserve(std::max(want, 2 * idx->off.capacity()));
+  ss::AppendArgs a{};
+  a.L = d.n_layers;
+  a.Hk = d.n_kv_heads;
+  a.D = d.head_dim;
+  a.n_frames = n_frames;
+  a.n_tokens = n_tokens;
+  a.max_rows = d.max_rows;
+  a.row0 = idx->n_rows;
+  a.frame0 = stored;        // per-frame arena entries sit at id - frame_base
+  a.rows_per_frame = rpf;
+  a.n_centroids = compress ? compress->n_centroids : 0;
+  a.n_iters = compress ? compress->n_iters : 0;
+  for (int l = 0; l < d.n_layers; ++l) a.src[l] = static_cast<const uint16_t*>(layer_keys[l]);
+  a.dst = idx->dev;
+  hipError_t e = hipSuccess;
+  if (idx->n_frames == 0)   // the key-magnitude statistic starts with the first append
+    e = ss::launch_zero32(reinterpret_cast<int32_t*>(idx->dev.stats), 1, static_cast<hipStream_t>(stream));
+  if (e == hipSuccess) e = ss::launch_append(a, compress != nullptr, static_cast<hipStream_t>(stream));
+  if (e == hipSuccess && layer_values) {
+    ss::StoreValuesArgs v{};
+    v.L = d.n_layers;
+    v.Hk = d.n_kv_heads;
+    v.D = d.head_dim;
+    v.max_rows = d.max_rows;
+    v.row0 = idx->n_rows;
+    v.rows = new_rows;
+    for (int l = 0; l < d.n_layers; ++l) v.src[l] = static_cast<const uint16_t*>(layer_values[l]);
+    v.values = idx->values;
+    v.weights = idx->weights;
+    e = ss::launch_store_values(v, static_cast<hipStream_t>(stream));
+  }
+  if (e != hipSuccess) return fail(SS_ERR_DEVICE, "append launch failed: %s", hipGetErrorString(e));
+  if (first_frame_id) *first_frame_id = idx->n_frames;
+  for (int f = 1; f <= n_frames; ++f) idx->off.push_back(idx->n_rows + (int64_t)f * rpf);   // reserved
+  idx->n_frames += n_frames;
+  idx->n_rows += new_rows;
+  idx->rpf = (idx->rpf == -1 || idx->rpf == rpf) ? rpf : 0;
+  return SS_OK;
+}
+
+// Own tokens of a stream in a call (0: history alone).
+int own_count(const ss_own_tokens* own, int s) { return own ? own->n_own[s] : 0; }
+
+ss_status check_attend(ss_index* const* idx, int32_t n_streams, const int32_t* n_q, const ss_own_tokens* own,
+                       const ss_attend_params* prm) {
+  if (!idx) return fail(SS_ERR_INVALID_ARGUMENT, "idx is NULL");
+  if (n_streams < 1) return fail(SS_ERR_INVALID_ARGUMENT, "n_streams must be >= 1");
+  if (!n_q) return fail(SS_ERR_INVALID_ARGUMENT, "n_q is NULL");
+  if (!prm) return fail(SS_ERR_INVALID_ARGUMENT, "params is NULL");
+  if (own && (!own->n_own || !own->capacity)) return fail(SS_ERR_INVALID_ARGUMENT, "own->n_own or own->capacity is NULL");
+  for (int s = 0; s < n_streams; ++s) {
+    if (!idx[s]) return fail(SS_ERR_INVALID_ARGUMENT, "idx[%d] is NULL", s);
+    if (!same_shape(idx[s]->desc, idx[0]->desc))
+      return fail(SS_ERR_INVALID_ARGUMENT, "idx[%d] shape differs from idx[0]", s);
+    if (!idx[s]->values) return fail(SS_ERR_INVALID_ARGUMENT, "idx[%d] keeps no values (ss_index_attach_values)", s);
+    if (n_q[s] < 1 || n_q[s] > 4096)
+      return fail(SS_ERR_INVALID_ARGUMENT, "n_q[%d] = %d outside 1..4096", s, n_q[s]);
+    if (!own) continue;
+    const int n = own->n_own[s];
+    if (n != 0 && (n < n_q[s] || n > ss::kMaxOwn))
+      return fail(SS_ERR_INVALID_ARGUMENT, "n_own[%d] = %d is neither 0 nor in n_q .. %d", s, n, ss::kMaxOwn);
+    if (n != 0 && (own->capacity[s] < n || own->capacity[s] > ss::kMaxOwn))
+      return fail(SS_ERR_INVALID_ARGUMENT, "capacity[%d] = %d outside n_own .. %d", s, own->capacity[s], ss::kMaxOwn);
+    if (own->parents && own->parents[s]) {
+      if (n == 0) return fail(SS_ERR_INVALID_ARGUMENT, "stream %d has a tree but no own tokens", s);
+      if (n_q[s] > ss::kMaxTree)
+        return fail(SS_ERR_UNSUPPORTED, "stream %d drafts %d tokens > %d", s, n_q[s], ss::kMaxTree);
+    }
+  }
+  if (prm->layer < 0 || prm->layer >= idx[0]->desc.n_layers)
+    return fail(SS_ERR_INVALID_ARGUMENT, "layer %d outside 0..%d", prm->layer, idx[0]->desc.n_layers - 1);
+  if (!std::isfinite(prm->softcap) || prm->softcap < 0.0f)
+    return fail(SS_ERR_INVALID_ARGUMENT, "softcap must be 0 (none) or positive and finite");
+  if (prm->softcap > 0.0f && (prm->softcap < 1e-3f || prm->softcap > 1e6f))
+    return fail(SS_ERR_UNSUPPORTED, "softcap outside 1e-3 .. 1e6");
+  if (prm->frames && (prm->n_listed < 1 || prm->n_listed > ss::kMaxListed))
+    return fail(SS_ERR_UNSUPPORTED, "n_listed %d outside 1..%d", prm->n_listed, ss::kMaxListed);
+  if (!prm->frames && (prm->n_listed != 0 || prm->kinds))
+    return fail(SS_ERR_INVALID_ARGUMENT, "n_listed or kinds without frames");
+  if (!aligned(prm->frames, 8) || !aligned(prm->kinds, 4) || !aligned(prm->slopes, 4))
+    return fail(SS_ERR_INVALID_ARGUMENT, "misaligned device pointer");
+  return SS_OK;
+}
+
+// Launch shapes of k_attend (query columns of a block, keys of a tile) by the
+// columns M = G n_q of a KV head: the fewest that hold them, since every column
+// block reads the keys again.
+struct AttendTile {
+  int columns, keys;
+};
+constexpr AttendTile kAttendTiles[4] = {{32, 128}, {64, 128}, {128, 64}, {256, 64}};
+constexpr int kCus = 256;
+
+// Fills the arguments of one group of streams [s0, s0 + S); pointers into the
+// workspace when `ws` is given.  Returns the group's workspace bytes.
+size_t plan_attend(ss::AttendArgs& a, ss::AttendPlan& p, ss::RowsArgs& rows, ss_index* const* idx, int s0, int S,
+                   const int32_t* n_q, const ss_own_tokens* own, const ss_attend_params* prm, bool accumulate,
+                   void* ws) {
+  const ss_index_desc& d = idx[0]->desc;
+  std::memset(&a, 0, sizeof a);
+  std::memset(&p, 0, sizeof p);
+  std::memset(&rows, 0, sizeof rows);
+  a.S = rows.S = S;
+  a.Hk = d.n_kv_heads;
+  a.G = d.n_q_heads / d.n_kv_heads;
+  p.D = d.head_dim;
+  const double scale = 1.0 / std::sqrt((double)d.head_dim), log2e = 1.4426950408889634;
+  a.c1 = (float)(scale * log2e);
+  if (prm->softcap > 0.0f) {
+    a.cap_x = (float)(scale / (double)prm->softcap);
+    a.cap_log2 = (float)((double)prm->softcap * log2e);
+  }
+  a.slopes = prm->slopes;
+  p.listed = prm->frames != nullptr;
+  p.map = p.listed || prm->slopes;
+  rows.n_listed = prm->n_listed;
+  int m_max = 0;
+  for (int i = 0; i < S; ++i) m_max = std::max(m_max, a.G * n_q[s0 + i]);
+  p.join_rows = m_max * a.Hk;
+
+  size_t off = 0;
+  auto take = [&](size_t bytes) -> char* {
+    off = align256(off);
+    char* r = ws ? static_cast<char*>(ws) + off : nullptr;
+    off += bytes;
+    return r;
+  };
+  int64_t visible[ss::kAttendStreams];   // most rows each stream can see
+  for (int i = 0; i < S; ++i) {
+    const ss_index* x = idx[s0 + i];
+    ss::AttendStream& st = a.st[i];
+    const int64_t f_lo = std::min(x->first_detail, x->n_frames), r_lo = row_of(x, f_lo), n = x->n_rows - r_lo;
+    const int64_t base = (int64_t)prm->layer * a.Hk * x->desc.max_rows;
+    const int64_t first = p.map ? 0 : r_lo;
+    st.keys = x->dev.keys + (base + first) * p.D;
+    st.values = x->values + (base + first) * p.D;
+    st.weights = x->weights + base + first;
+    st.head_stride = x->desc.max_rows * p.D;
+    st.w_stride = x->desc.max_rows;
+    st.row0 = (int32_t)(p.map ? r_lo : 0);
+    st.n_rows = (int32_t)n;
+    st.n_q = n_q[s0 + i];
+    st.n_own = own_count(own, s0 + i);
+    visible[i] = n;
+    if (!p.map) continue;
+    if (p.listed) {
+      int64_t longest = x->rpf;
+      if (x->rpf <= 0) {
+        longest = 0;
+        for (int64_t f = f_lo; f < x->n_frames; ++f) longest = std::max(longest, row_of(x, f + 1) - row_of(x, f));
+      }
+      visible[i] = std::min<int64_t>(n, longest * prm->n_listed);
+    }
+    const size_t one = align256((size_t)(visible[i] + 1) * 4);
+    char* map = take(2 * one + 256);
+    ss::RowsStream& r = rows.st[i];
+    r.list = p.listed ? prm->frames + (size_t)(s0 + i) * prm->n_listed : nullptr;
+    r.kinds = prm->kinds ? prm->kinds + (size_t)(s0 + i) * prm->n_listed : nullptr;
+    r.frame_off = x->dev.frame_off;
+    r.frame_base = x->frame_base;
+    r.f_lo = f_lo;
+    r.f_hi = r.n_frames = x->n_frames;
+    r.row0 = (int32_t)r_lo;
+    r.n_rows = (int32_t)n;
+    if (map) {
+      r.rowmap = reinterpret_cast<int32_t*>(map);
+      r.age = reinterpret_cast<float*>(map + one);
+      r.n_vis = reinterpret_cast<int32_t*>(map + 2 * one);
+      st.rowmap = r.rowmap;
+      st.n_vis = r.n_vis;
+      st.age_off = (uint32_t)one;
+    }
+  }
+
+  if (accumulate) {
+    // 32 keys a wave at a time; as many shares as keep the card's waves busy
+    p.shape = m_max <= 32 ? 0 : 1;
+    const int64_t waves = p.shape == 0 ? 4 : 8, want = (p.shape == 0 ? 8 : 4) * kCus;
+    for (int i = 0; i < S; ++i) {
+      ss::AttendStream& st = a.st[i];
+      const int64_t groups = (visible[i] + 31) / 32;
+      st.n_split = (int32_t)std::max<int64_t>(1, std::min((groups + waves - 1) / waves, want / std::max(1, S * a.Hk)));
+      st.item0 = p.items;
+      p.items += st.n_split * a.Hk;
+    }
+    return align256(off);
+  }
+
+  p.shape = 0;
+  while (p.shape < 3 && kAttendTiles[p.shape].columns < m_max) ++p.shape;
+  const AttendTile tile = kAttendTiles[p.shape];
+  // Shares of the key axis: about four items a CU over the batch, in proportion to
+  // each stream's tiles, none below two tiles of 128 keys.
+  auto tiles_of = [&](int i) {
+    return (visible[i] + tile.keys - 1) / tile.keys + (a.st[i].n_own + tile.keys - 1) / tile.keys;
+  };
+  int64_t total = 0;
+  for (int i = 0; i < S; ++i) {
+    const int64_t blocks = (a.G * a.st[i].n_q + tile.columns - 1) / tile.columns;
+    total += tiles_of(i) * blocks * a.Hk;
+  }
+  const int64_t least = 256 / tile.keys;
+  const int64_t per = std::max(least, (total + 4 * kCus - 1) / (4 * kCus));
+  int64_t parts = 0;
+  for (int i = 0; i < S; ++i) {
+    ss::AttendStream& st = a.st[i];
+    const int64_t M = (int64_t)a.G * st.n_q, blocks = (M + tile.columns - 1) / tile.columns;
+    st.n_split = (int32_t)std::max<int64_t>(1, (tiles_of(i) + per - 1) / per);
+    st.item0 = p.items;
+    p.items += (int)(st.n_split * blocks * a.Hk);
+    st.part0 = parts;
+    if (st.n_split > 1) {
+      parts += st.n_split * M * a.Hk;
+      p.join = true;
+    }
+  }
+  a.part_o = reinterpret_cast<float*>(take((size_t)parts * p.D * 4));
+  a.part_ml = reinterpret_cast<float*>(take((size_t)parts * 8));
+  return align256(off);
+}
+
+size_t attend_ws(ss_index* const* idx, int32_t n_streams, const int32_t* n_q, const ss_own_tokens* own,
+                 const ss_attend_params* prm, bool accumulate) {
+  size_t need = 256;
+  for (int s0 = 0; s0 < n_streams; s0 += ss::kAttendStreams) {
+    ss::AttendArgs a;
+    ss::AttendPlan p;
+    ss::RowsArgs r;
+    need = std::max(need, plan_attend(a, p, r, idx, s0, std::min(ss::kAttendStreams, n_streams - s0), n_q, own, prm,
+                                      accumulate, nullptr));
+  }
+  return need;
+}
+
 }  // namespace
 
 struct ss_clusters {
@@ -891,6 +1185,8 @@ ss_status ss_index_compact(ss_index* idx, void* stream) {
     ss::CompactArgs a{};
     const ss_index_desc& d = idx->desc;
     a.dev = idx->dev;
+    a.values = idx->values;
+    a.weights = idx->weights;
     a.L = d.n_layers; a.Hk = d.n_kv_heads; a.D = d.head_dim; a.max_rows = d.max_rows;
     a.row_shift = rs;
     a.keep_rows = idx->n_rows - rs;
@@ -910,9 +1206,10 @@ ss_status ss_index_budget_split(const ss_index* idx, uint64_t budget_bytes, int6
     if (!idx || !frame_hi) return fail(SS_ERR_INVALID_ARGUMENT, "idx or frame_hi is NULL");
     const ss_index_desc& d = idx->desc;
     const uint64_t L = (uint64_t)d.n_layers, Hk = (uint64_t)d.n_kv_heads, D = (uint64_t)d.head_dim;
+    const uint64_t row_bytes = (idx->values ? 2 : 1) * (2 * D + 4);
     auto bytes = [&](int64_t f) {
       const uint64_t rows = (uint64_t)(row_of(idx, f + 1) - row_of(idx, f));
-      return rows * L * Hk * (2 * D + 4) + (Hk * D + L * Hk * D) * 4 + 4;
+      return rows * L * Hk * row_bytes + (Hk * D + L * Hk * D) * 4 + 4;
     };
     const int64_t T = idx->n_frames, lo = idx->first_detail;
     const int64_t hi = std::max(lo, T - (int64_t)d.n_recent);   // the recent window stays detailed
@@ -930,67 +1227,206 @@ ss_status ss_index_append(ss_index* idx, const void* const* layer_keys, int32_t 
                           int64_t* first_frame_id) {
   return guarded([&]() -> ss_status {
     if (!idx) return fail(SS_ERR_INVALID_ARGUMENT, "idx is NULL");
-    const ss_index_desc& d = idx->desc;
-    if (!layer_keys) return fail(SS_ERR_INVALID_ARGUMENT, "layer_keys is NULL");
-    if (n_frames < 1 || n_tokens < 1)
-      return fail(SS_ERR_INVALID_ARGUMENT, "n_frames and n_tokens must be >= 1");
-    if ((int64_t)n_frames * n_tokens > 0x7FFFFFFF)
-      return fail(SS_ERR_UNSUPPORTED, "n_frames * n_tokens exceeds 2^31-1");
-    for (int l = 0; l < d.n_layers; ++l) {
-      if (!layer_keys[l]) return fail(SS_ERR_INVALID_ARGUMENT, "layer_keys[%d] is NULL", l);
-      if (!aligned(layer_keys[l], 16))
-        return fail(SS_ERR_INVALID_ARGUMENT, "layer_keys[%d] not 16-byte aligned", l);
+    if (idx->values)
+      return fail(SS_ERR_INVALID_ARGUMENT, "the index keeps values: append through ss_index_append_kv");
+    return append_common(idx, layer_keys, nullptr, n_frames, n_tokens, compress, stream, first_frame_id);
+  });
+}
+
+size_t ss_values_required_bytes(const ss_index_desc* desc) {
+  if (check_desc(desc) != SS_OK) return 0;
+  return values_layout(*desc).total;
+}
+
+ss_status ss_index_attach_values(ss_index* idx, void* dev_arena, size_t arena_bytes) {
+  return guarded([&]() -> ss_status {
+    if (!idx) return fail(SS_ERR_INVALID_ARGUMENT, "idx is NULL");
+    if (idx->values) return fail(SS_ERR_INVALID_ARGUMENT, "the index keeps values already");
+    if (idx->n_frames != 0) return fail(SS_ERR_INVALID_ARGUMENT, "values can only be attached to an empty index");
+    if (!dev_arena || !aligned(dev_arena, 256))
+      return fail(SS_ERR_INVALID_ARGUMENT, "arena NULL or not 256-byte aligned");
+    const ValuesLayout v = values_layout(idx->desc);
+    if (arena_bytes < v.total) return fail(SS_ERR_CAPACITY, "arena %zu bytes, %zu needed", arena_bytes, v.total);
+    idx->values = static_cast<uint16_t*>(dev_arena);
+    idx->weights = reinterpret_cast<float*>(static_cast<char*>(dev_arena) + v.weights);
+    idx->values_bytes = v.total;
+    return SS_OK;
+  });
+}
+
+ss_status ss_index_append_kv(ss_index* idx, const void* const* layer_keys, const void* const* layer_values,
+                             int32_t n_frames, int32_t n_tokens, void* stream, int64_t* first_frame_id) {
+  return guarded([&]() -> ss_status {
+    if (!idx) return fail(SS_ERR_INVALID_ARGUMENT, "idx is NULL");
+    if (!idx->values) return fail(SS_ERR_INVALID_ARGUMENT, "the index keeps no values (ss_index_attach_values)");
+    if (!layer_values) return fail(SS_ERR_INVALID_ARGUMENT, "layer_values is NULL");
+    return append_common(idx, layer_keys, layer_values, n_frames, n_tokens, nullptr, stream, first_frame_id);
+  });
+}
+
+size_t ss_attend_workspace_bytes(ss_index* const* idx, int32_t n_streams, const int32_t* n_q,
+                                 const ss_own_tokens* own, const ss_attend_params* params) {
+  if (check_attend(idx, n_streams, n_q, own, params) != SS_OK) return 0;
+  return attend_ws(idx, n_streams, n_q, own, params, false);
+}
+
+ss_status ss_attend(ss_index* const* idx, int32_t n_streams, const void* const* queries, const int32_t* n_q,
+                    const ss_own_tokens* own, const ss_attend_params* params, void* ws, size_t ws_bytes,
+                    void* stream, void* const* out, float* const* lse) {
+  return guarded([&]() -> ss_status {
+    const ss_status st = check_attend(idx, n_streams, n_q, own, params);
+    if (st) return st;
+    if (!queries || !out) return fail(SS_ERR_INVALID_ARGUMENT, "queries or out is NULL");
+    for (int s = 0; s < n_streams; ++s) {
+      if (!queries[s] || !aligned(queries[s], 16))
+        return fail(SS_ERR_INVALID_ARGUMENT, "queries[%d] NULL or not 16-byte aligned", s);
+      if (!out[s] || !aligned(out[s], 16))
+        return fail(SS_ERR_INVALID_ARGUMENT, "out[%d] NULL or not 16-byte aligned", s);
+      if (lse && (!lse[s] || !aligned(lse[s], 4)))
+        return fail(SS_ERR_INVALID_ARGUMENT, "lse[%d] NULL or misaligned", s);
+      if (own_count(own, s) == 0) continue;
+      if (!own->keys || !own->values || !own->keys[s] || !own->values[s] || !aligned(own->keys[s], 16) ||
+          !aligned(own->values[s], 16))
+        return fail(SS_ERR_INVALID_ARGUMENT, "own keys or values of stream %d NULL or not 16-byte aligned", s);
+      if (own->parents && !aligned(own->parents[s], 4))
+        return fail(SS_ERR_INVALID_ARGUMENT, "parents[%d] misaligned", s);
     }
-    int rpf = n_tokens;
-    if (compress) {
-      if (compress->n_centroids < 1 || compress->n_centroids > ss::kMaxCentroids)
-        return fail(SS_ERR_UNSUPPORTED, "n_centroids %d outside 1..%d", compress->n_centroids,
-                    ss::kMaxCentroids);
-      if (compress->n_iters < 0 || compress->n_iters > 100)
-        return fail(SS_ERR_INVALID_ARGUMENT, "n_iters %d outside 0..100", compress->n_iters);
-      if (n_tokens > ss::kMaxTokensCompress)
-        return fail(SS_ERR_UNSUPPORTED, "compression supports at most %d tokens per frame",
-                    ss::kMaxTokensCompress);
-      rpf = std::min(compress->n_centroids, n_tokens);
+    if (!ws || !aligned(ws, 256)) return fail(SS_ERR_WORKSPACE, "workspace NULL or not 256-byte aligned");
+    const size_t need = attend_ws(idx, n_streams, n_q, own, params, false);
+    if (ws_bytes < need) return fail(SS_ERR_WORKSPACE, "workspace %zu bytes, %zu needed", ws_bytes, need);
+    const hipStream_t hs = static_cast<hipStream_t>(stream);
+    for (int s0 = 0; s0 < n_streams; s0 += ss::kAttendStreams) {
+      ss::AttendArgs a;
+      ss::AttendPlan p;
+      ss::RowsArgs r;
+      plan_attend(a, p, r, idx, s0, std::min(ss::kAttendStreams, n_streams - s0), n_q, own, params, false, ws);
+      for (int i = 0; i < a.S; ++i) {
+        ss::AttendStream& t = a.st[i];
+        const int s = s0 + i;
+        t.q = static_cast<const uint16_t*>(queries[s]);
+        t.out = static_cast<uint16_t*>(out[s]);
+        t.lse = lse ? lse[s] : nullptr;
+        if (t.n_own == 0) continue;
+        t.own_k = static_cast<const uint16_t*>(own->keys[s]);
+        t.own_v = static_cast<const uint16_t*>(own->values[s]);
+        t.own_cap = own->capacity[s];
+        t.parents = own->parents ? own->parents[s] : nullptr;
+      }
+      hipError_t e = p.map ? ss::launch_rows(r, hs) : hipSuccess;
+      if (e == hipSuccess) e = ss::launch_attend(a, p, hs);
+      if (e != hipSuccess) return fail(SS_ERR_DEVICE, "attention launch failed: %s", hipGetErrorString(e));
     }
-    const int64_t stored = idx->n_frames - idx->frame_base;
-    if (stored + n_frames > d.max_frames)
-      return fail(SS_ERR_CAPACITY, "%lld stored frames + %d exceeds max_frames %lld", (long long)stored,
-                  n_frames, (long long)d.max_frames);
-    const int64_t new_rows = (int64_t)n_frames * rpf;
-    if (idx->n_rows + new_rows > d.max_rows)
-      return fail(SS_ERR_CAPACITY, "%lld rows + %lld exceeds max_rows %lld", (long long)idx->n_rows,
-                  (long long)new_rows, (long long)d.max_rows);
-    // the host offsets are reserved before anything is enqueued, so that the
-    // bookkeeping after the launch cannot fail and leave the index behind the
-    // device state
-    // (grown by doubling: reserving each call's few frames alone would copy them all each time)
-    const size_t want = idx->off.size() + (size_t)n_frames;
-    if (want > idx->off.capacity()) idx->off.reserve(std::max(want, 2 * idx->off.capacity()));
-    ss::AppendArgs a{};
+    return SS_OK;
+  });
+}
+
+size_t ss_attend_accumulate_workspace_bytes(ss_index* const* idx, int32_t n_streams, const int32_t* n_q,
+                                            const ss_attend_params* params) {
+  if (check_attend(idx, n_streams, n_q, nullptr, params) != SS_OK) return 0;
+  return attend_ws(idx, n_streams, n_q, nullptr, params, true);
+}
+
+ss_status ss_attend_accumulate(ss_index* const* idx, int32_t n_streams, const void* const* queries,
+                               const int32_t* n_q, const float* const* lse, const ss_attend_params* params,
+                               float decay, void* ws, size_t ws_bytes, void* stream) {
+  return guarded([&]() -> ss_status {
+    const ss_status st = check_attend(idx, n_streams, n_q, nullptr, params);
+    if (st) return st;
+    if (!(decay >= 0.0f && decay <= 1.0f)) return fail(SS_ERR_INVALID_ARGUMENT, "decay outside 0..1");
+    if (!queries || !lse) return fail(SS_ERR_INVALID_ARGUMENT, "queries or lse is NULL");
+    for (int s = 0; s < n_streams; ++s) {
+      if (!queries[s] || !aligned(queries[s], 16))
+        return fail(SS_ERR_INVALID_ARGUMENT, "queries[%d] NULL or not 16-byte aligned", s);
+      if (!lse[s] || !aligned(lse[s], 4)) return fail(SS_ERR_INVALID_ARGUMENT, "lse[%d] NULL or misaligned", s);
+      for (int t = 0; t < s; ++t)
+        if (idx[t] == idx[s])
+          return fail(SS_ERR_INVALID_ARGUMENT, "idx[%d] and idx[%d] are one index: their weights would be added at once",
+                      t, s);
+    }
+    if (!ws || !aligned(ws, 256)) return fail(SS_ERR_WORKSPACE, "workspace NULL or not 256-byte aligned");
+    const size_t need = attend_ws(idx, n_streams, n_q, nullptr, params, true);
+    if (ws_bytes < need) return fail(SS_ERR_WORKSPACE, "workspace %zu bytes, %zu needed", ws_bytes, need);
+    const hipStream_t hs = static_cast<hipStream_t>(stream);
+    for (int s0 = 0; s0 < n_streams; s0 += ss::kAttendStreams) {
+      ss::AttendArgs a;
+      ss::AttendPlan p;
+      ss::RowsArgs r;
+      plan_attend(a, p, r, idx, s0, std::min(ss::kAttendStreams, n_streams - s0), n_q, nullptr, params, true, ws);
+      for (int i = 0; i < a.S; ++i) {
+        a.st[i].q = static_cast<const uint16_t*>(queries[s0 + i]);
+        a.st[i].lse = const_cast<float*>(lse[s0 + i]);   // read only
+      }
+      hipError_t e = p.map ? ss::launch_rows(r, hs) : hipSuccess;
+      if (e == hipSuccess) e = ss::launch_accumulate(a, p, decay, hs);
+      if (e != hipSuccess) return fail(SS_ERR_DEVICE, "weight accumulation launch failed: %s", hipGetErrorString(e));
+    }
+    return SS_OK;
+  });
+}
+
+ss_status ss_index_evict(const ss_index* src, ss_index* dst, int64_t frame_hi, int32_t keep_rows, void* stream) {
+  return guarded([&]() -> ss_status {
+    if (!src || !dst) return fail(SS_ERR_INVALID_ARGUMENT, "src or dst is NULL");
+    if (src == dst) return fail(SS_ERR_INVALID_ARGUMENT, "src and dst are one index");
+    const ss_index_desc &d = src->desc, &e = dst->desc;
+    if (!same_shape(d, e)) return fail(SS_ERR_INVALID_ARGUMENT, "src and dst shapes differ");
+    if (!src->values || !dst->values)
+      return fail(SS_ERR_INVALID_ARGUMENT, "src or dst keeps no values (ss_index_attach_values)");
+    auto overlap = [](const void* a, size_t an, const void* b, size_t bn) {
+      const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+      return x < y + bn && y < x + an;
+    };
+    if (overlap(src->arena, layout(d).total, dst->arena, layout(e).total) ||
+        overlap(src->arena, layout(d).total, dst->values, dst->values_bytes) ||
+        overlap(src->values, src->values_bytes, dst->arena, layout(e).total) ||
+        overlap(src->values, src->values_bytes, dst->values, dst->values_bytes))
+      return fail(SS_ERR_INVALID_ARGUMENT, "the arenas of src and dst overlap");
+    if (keep_rows < 1) return fail(SS_ERR_INVALID_ARGUMENT, "keep_rows must be >= 1");
+    const int64_t f_lo = src->first_detail, f_end = std::max(f_lo, src->n_frames - (int64_t)d.n_recent);
+    if (frame_hi < f_lo || frame_hi > f_end)
+      return fail(SS_ERR_INVALID_ARGUMENT, "frame_hi %lld outside %lld..%lld (the recent window stays whole)",
+                  (long long)frame_hi, (long long)f_lo, (long long)f_end);
+    const int64_t frames = src->n_frames - f_lo;
+    if (frames > e.max_frames)
+      return fail(SS_ERR_CAPACITY, "%lld frames exceed dst's max_frames %lld", (long long)frames, (long long)e.max_frames);
+    std::vector<int64_t> off((size_t)frames + 1, 0);
+    int32_t rpf = -1;
+    for (int64_t i = 0; i < frames; ++i) {
+      int64_t n = row_of(src, f_lo + i + 1) - row_of(src, f_lo + i);
+      if (f_lo + i < frame_hi) n = std::min<int64_t>(n, keep_rows);
+      off[(size_t)i + 1] = off[(size_t)i] + n;
+      rpf = (rpf == -1 || rpf == (int32_t)n) ? (int32_t)n : 0;
+    }
+    if (off.back() > e.max_rows)
+      return fail(SS_ERR_CAPACITY, "%lld rows exceed dst's max_rows %lld", (long long)off.back(), (long long)e.max_rows);
+    if (frames * d.n_layers * d.n_kv_heads > (int64_t)1 << 32)
+      return fail(SS_ERR_UNSUPPORTED, "too many frames in one call");
+    ss::EvictArgs a{};
     a.L = d.n_layers;
     a.Hk = d.n_kv_heads;
     a.D = d.head_dim;
-    a.n_frames = n_frames;
-    a.n_tokens = n_tokens;
-    a.max_rows = d.max_rows;
-    a.row0 = idx->n_rows;
-    a.frame0 = stored;        // per-frame arena entries sit at id - frame_base
-    a.rows_per_frame = rpf;
-    a.n_centroids = compress ? compress->n_centroids : 0;
-    a.n_iters = compress ? compress->n_iters : 0;
-    for (int l = 0; l < d.n_layers; ++l) a.src[l] = static_cast<const uint16_t*>(layer_keys[l]);
-    a.dst = idx->dev;
-    hipError_t e = hipSuccess;
-    if (idx->n_frames == 0)   // the key-magnitude statistic starts with the first append
-      e = ss::launch_zero32(reinterpret_cast<int32_t*>(idx->dev.stats), 1, static_cast<hipStream_t>(stream));
-    if (e == hipSuccess) e = ss::launch_append(a, compress != nullptr, static_cast<hipStream_t>(stream));
-    if (e != hipSuccess) return fail(SS_ERR_DEVICE, "append launch failed: %s", hipGetErrorString(e));
-    if (first_frame_id) *first_frame_id = idx->n_frames;
-    for (int f = 1; f <= n_frames; ++f) idx->off.push_back(idx->n_rows + (int64_t)f * rpf);   // reserved
-    idx->n_frames += n_frames;
-    idx->n_rows += new_rows;
-    idx->rpf = (idx->rpf == -1 || idx->rpf == rpf) ? rpf : 0;
+    a.n_frames = frames;
+    a.n_thin = frame_hi - f_lo;
+    a.keep = keep_rows;
+    a.src_max_rows = d.max_rows;
+    a.dst_max_rows = e.max_rows;
+    a.src = src->dev;
+    const int64_t f0 = f_lo - src->frame_base;
+    a.src.frame_off += f0;
+    a.src.desc += f0 * d.n_kv_heads * d.head_dim;
+    a.src.pooled += f0 * d.n_layers * d.n_kv_heads * d.head_dim;
+    a.dst = dst->dev;
+    a.src_values = src->values;
+    a.dst_values = dst->values;
+    a.src_weights = src->weights;
+    a.dst_weights = dst->weights;
+    const hipError_t he = ss::launch_evict(a, static_cast<hipStream_t>(stream));
+    if (he != hipSuccess) return fail(SS_ERR_DEVICE, "eviction launch failed: %s", hipGetErrorString(he));
+    dst->n_frames = src->n_frames;
+    dst->frame_base = dst->first_detail = f_lo;
+    dst->n_rows = off.back();
+    dst->off.swap(off);
+    dst->rpf = rpf;
     return SS_OK;
   });
 }

@@ -239,12 +239,101 @@ hipError_t launch_evidence(const EvidenceArgs& a, hipStream_t st);
 // row_shift.
 struct CompactArgs {
   IndexDev dev;
+  uint16_t* values;      // null without a value cache
+  float* weights;
   int L, Hk, D;
   int64_t max_rows;
   int64_t row_shift, keep_rows;
   int64_t frame_shift, keep_frames;
 };
 hipError_t launch_compact(const CompactArgs& a, hipStream_t st);
+
+// ---------------------------------------------------------------------------
+// Values beside the keys, attention over the stored history, eviction
+// ---------------------------------------------------------------------------
+constexpr int kAttendStreams = 16;   // streams of one attention launch (its arguments stay below 4 KB)
+constexpr int kMaxTree = 512;        // drafted tokens of one stream
+constexpr int kMaxListed = 4096;     // listed frames of one stream (sorted in LDS)
+constexpr int kMaxOwn = 1 << 20;     // own tokens of one stream
+
+struct StoreValuesArgs {
+  int L, Hk, D;
+  int64_t max_rows, row0, rows;
+  const uint16_t* src[kMaxLayers];   // per layer [H_kv][rows][d]
+  uint16_t* values;                  // [L][H_kv][max_rows][d]
+  float* weights;                    // [L][H_kv][max_rows], zeroed for the new rows
+};
+hipError_t launch_store_values(const StoreValuesArgs& a, hipStream_t st);
+
+// The rows that a call sees, laid out in the workspace: see k_rows.
+struct RowsStream {
+  const int64_t* list;         // [n_listed] frame ids (n_listed == 0: every detailed frame)
+  const int32_t* kinds;        // entries of another kind than 0 are skipped; may be null
+  const int32_t* frame_off;    // of the stored frames
+  int64_t frame_base, f_lo, f_hi, n_frames;
+  int32_t row0, n_rows;        // the detailed rows
+  int32_t* rowmap;
+  float* age;
+  int32_t* n_vis;
+};
+struct RowsArgs {
+  int S, n_listed;
+  RowsStream st[kAttendStreams];
+};
+hipError_t launch_rows(const RowsArgs& a, hipStream_t st);
+
+struct AttendStream {
+  const uint16_t* keys;        // KV head 0 of the layer: from the first detailed row, with a row map from row 0
+  const uint16_t* values;
+  int64_t head_stride;         // elements from one KV head to the next
+  const uint16_t* q;           // [H_q][n_q][d]
+  const uint16_t* own_k;       // [H_kv][own_cap][d]
+  const uint16_t* own_v;
+  const int32_t* parents;      // [n_q], null: causal
+  uint16_t* out;               // [H_q][n_q][d]
+  float* lse;                  // [H_q][n_q]: attention writes it (may be null), accumulation reads it
+  const int32_t* rowmap;       // with a row map: places of the visible rows ...
+  const int32_t* n_vis;        // ... and how many there are
+  float* weights;              // accumulation: the layer's, based like keys
+  int64_t w_stride;
+  int64_t part0;               // first partial row in the workspace
+  uint32_t age_off;            // bytes from rowmap to the rows' ages
+  int32_t row0, n_rows;        // the detailed rows in the arena run
+  int32_t n_q, n_own, own_cap;
+  int32_t n_split, item0;
+};
+struct AttendArgs {
+  int S, Hk, G;
+  float c1;                    // log2(e) / sqrt(d)
+  float cap_x, cap_log2;       // 1 / (cap sqrt(d)), cap log2(e); 0: scores are not capped
+  const float* slopes;         // [H_q] or null
+  float* part_o;               // partial sums [rows][d] and their (maximum, sum)
+  float* part_ml;
+  AttendStream st[kAttendStreams];
+};
+struct AttendPlan {
+  int D, shape, items;         // shape: which tiling of k_attend / k_accumulate
+  bool map, listed, join;
+  int join_rows;               // largest H_q n_q of the batch
+};
+hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t st);
+hipError_t launch_accumulate(const AttendArgs& a, const AttendPlan& p, float decay, hipStream_t st);
+
+// Frames [0, n_frames) of src (views from its first detailed frame) into an empty dst; the first
+// n_thin keep at most `keep` rows for each (layer, KV head).
+struct EvictArgs {
+  int L, Hk, D;
+  int64_t n_frames, n_thin;
+  int keep;
+  int64_t src_max_rows, dst_max_rows;
+  IndexDev src, dst;
+  const uint16_t* src_values;
+  uint16_t* dst_values;
+  const float* src_weights;
+  float* dst_weights;
+  int64_t item_blocks;         // set by the launcher
+};
+hipError_t launch_evict(EvictArgs a, hipStream_t st);
 
 // Scores of one list over a row range, same arithmetic as the retrieval.
 hipError_t launch_debug_scores(RetrievePlan& p, int layer, int q_head, int64_t row0,

@@ -155,6 +155,64 @@ class ShallowIndex:
                                         _stream_handle(stream), C.byref(first)))
         return first.value
 
+    def attach_values(self) -> None:
+        """Keep values (and an attention weight for each row) beside the keys, in a
+        second arena owned by this object.  Only while the index is empty; frames then
+        come through :meth:`append_kv`."""
+        nbytes = L.lib().ss_values_required_bytes(C.byref(self.desc))
+        arena = torch.empty(nbytes, dtype=torch.uint8, device=self.arena.device)
+        L.check(L.lib().ss_index_attach_values(self.handle, arena.data_ptr(), nbytes))
+        self.value_arena = arena
+
+    def append_kv(self, layer_keys, layer_values, n_frames: int, n_tokens: int, stream=None) -> int:
+        """:meth:`append` for an index that keeps values; ``layer_values[l]`` is laid
+        out as ``layer_keys[l]``.  Rows are stored raw and start with weight 0."""
+        shape = (self.n_kv_heads, n_frames * n_tokens, self.head_dim)
+        if len(layer_keys) != self.n_layers or len(layer_values) != self.n_layers:
+            raise ValueError(f"expected {self.n_layers} key and {self.n_layers} value tensors")
+        kp = [_check_bf16(t, shape, "layer_keys[%d]", l) for l, t in enumerate(layer_keys)]
+        vp = [_check_bf16(t, shape, "layer_values[%d]", l) for l, t in enumerate(layer_values)]
+        first = C.c_int64()
+        L.check(L.lib().ss_index_append_kv(self.handle, L.ptr_array(kp), L.ptr_array(vp), n_frames, n_tokens,
+                                           _stream_handle(stream), C.byref(first)))
+        _used_on(stream, *layer_keys, *layer_values)
+        return first.value
+
+    def _rows_view(self, arena, at: int, dtype, width: int):
+        d = self.desc
+        n = d.n_layers * d.n_kv_heads * d.max_rows * width * dtype.itemsize
+        t = arena[at:at + n].view(dtype).view(d.n_layers, d.n_kv_heads, d.max_rows, width)
+        return t[:, :, :self.n_rows]
+
+    def _values_arena(self):
+        if getattr(self, "value_arena", None) is None:
+            raise ValueError("the index keeps no values (attach_values)")
+        return self.value_arena
+
+    @property
+    def keys(self) -> torch.Tensor:
+        """View of the stored keys, bfloat16 ``[L][H_kv][n_rows][d]`` (read only)."""
+        return self._rows_view(self.arena, 0, torch.bfloat16, self.head_dim)
+
+    @property
+    def values(self) -> torch.Tensor:
+        """View of the stored values, laid out as :attr:`keys` (read only)."""
+        return self._rows_view(self._values_arena(), 0, torch.bfloat16, self.head_dim)
+
+    @property
+    def weights(self) -> torch.Tensor:
+        """View of the rows' attention weights, fp32 ``[L][H_kv][n_rows]`` (may be written)."""
+        d = self.desc
+        at = (d.n_layers * d.n_kv_heads * d.max_rows * d.head_dim * 2 + 255) // 256 * 256
+        return self._rows_view(self._values_arena(), at, torch.float32, 1)[..., 0]
+
+    def evict_into(self, dst: "ShallowIndex", frame_hi: int, keep_rows: int, stream=None) -> None:
+        """Replace what ``dst`` holds by this index's detailed window, thinned: each
+        frame before ``frame_hi`` keeps the ``keep_rows`` rows of the largest weight for
+        each (layer, KV head), in their order (ties to the earlier row); later frames
+        come whole."""
+        L.check(L.lib().ss_index_evict(self.handle, dst.handle, frame_hi, keep_rows, _stream_handle(stream)))
+
     def export(self, stream=None) -> dict:
         """Stored rows, member counts, descriptors and frame offsets of the frames
         the arena stores (synchronises)."""
@@ -449,6 +507,154 @@ def assemble_evidence(indices, frame_ids, n_recent: int, n_before: int = 1, n_af
                                          n_units.data_ptr(), max_units))
     _used_on(stream, units, kinds, n_units)
     return units, kinds, n_units
+
+
+class HistoryAttention:
+    """Attention over the stored history of a batch of indices that keep values and
+    have identical shapes: for questions, single tokens and trees of drafted tokens,
+    and the weight that it gives each stored row.
+
+    ``softcap`` caps the scores at ``softcap * tanh(score / softcap)`` (0: not at
+    all); ``slopes`` (device fp32 ``[H_q]``) subtracts ``slopes[h] * age`` from the
+    scores of query head ``h``, a row's age being the frames from its own to the end
+    of the stream.  Keeps no buffers: each call allocates its workspace and outputs,
+    so calls on different streams or in different captured graphs share nothing.
+    """
+
+    def __init__(self, indices, softcap: float = 0.0, slopes: torch.Tensor | None = None):
+        self.indices = list(indices)
+        if not self.indices:
+            raise ValueError("expected at least one index")
+        x = self.indices[0]
+        self._device = x.arena.device
+        for i, y in enumerate(self.indices):
+            if y.arena.device != self._device:
+                raise ValueError(f"indices[{i}] lives on {y.arena.device}, indices[0] on {self._device}")
+        if slopes is not None and (not isinstance(slopes, torch.Tensor) or slopes.dtype != torch.float32
+                                   or tuple(slopes.shape) != (x.n_q_heads,) or not slopes.is_contiguous()
+                                   or slopes.device != self._device):
+            raise ValueError(f"slopes must be a contiguous fp32 tensor [{x.n_q_heads}] on {self._device}")
+        self.softcap, self.slopes = float(softcap), slopes
+        self._handles = L.ptr_array([y.handle.value for y in self.indices])
+
+    def _on_device(self, t, what: str, *at):
+        if t.device != self._device:
+            raise ValueError(f"{what % at} lives on {t.device}, the indices on {self._device}")
+
+    def _params(self, layer: int, frames, kinds):
+        p = L.AttendParams(layer, self.softcap, self.slopes.data_ptr() if self.slopes is not None else None,
+                           None, None, 0)
+        if torch.cuda.current_device() != self._device.index:
+            raise ValueError(f"the indices live on {self._device}, which is not the current device")
+        S = len(self.indices)
+        if frames is None:
+            if kinds is not None:
+                raise ValueError("kinds without frames")
+            return p
+        for t, dt, what in ((frames, torch.int64, "frames"), (kinds, torch.int32, "kinds")):
+            if t is None:
+                continue
+            if t.dtype != dt or t.dim() != 2 or t.shape[0] != S or t.shape != frames.shape or not t.is_contiguous():
+                raise ValueError(f"{what} must be a contiguous {dt} tensor [{S}][n_listed]")
+            self._on_device(t, what)
+        if frames.shape[1] == 0:     # an empty tensor has no address, which would mean every frame
+            raise ValueError("frames must list at least one entry (a negative one to see none)")
+        p.frames, p.n_listed = frames.data_ptr(), frames.shape[1]
+        if kinds is not None:
+            p.kinds = kinds.data_ptr()
+        return p
+
+    def _queries(self, queries):
+        S = len(self.indices)
+        if len(queries) != S:
+            raise ValueError(f"expected queries for {S} streams, got {len(queries)}")
+        x = self.indices[0]
+        ptrs, n_q = [], []
+        for s, q in enumerate(queries):
+            if q.dim() != 3:
+                raise ValueError(f"queries[{s}] must be [{x.n_q_heads}][n_q][{x.head_dim}]")
+            ptrs.append(_check_bf16(q, (x.n_q_heads, q.shape[1], x.head_dim), "queries[%d]", s))
+            self._on_device(q, "queries[%d]", s)
+            n_q.append(q.shape[1])
+        return L.ptr_array(ptrs), (C.c_int32 * S)(*n_q), n_q
+
+    def __call__(self, layer: int, queries, own=None, tree=None, frames=None, kinds=None, stream=None):
+        """``queries[s]``: ``[H_q][n_q][d]`` bfloat16.  ``own``: per stream ``None`` or
+        ``(keys, values, n_own)``, the question's own tokens at this layer as bfloat16
+        ``[H_kv][capacity][d]`` with ``n_own`` of them in use, the last ``n_q`` being the
+        queries.  ``tree``: per stream ``None`` (each query sees the own tokens up to
+        itself) or the parents of a drafted tree, device int32 ``[n_q]``.  ``frames`` and
+        ``kinds``: device int64 / int32 ``[n_streams][n_listed]``, the only frames to see
+        (as :class:`Retriever` and :func:`assemble_evidence` return them).  Returns
+        ``(out, lse)``: per stream bfloat16 ``[H_q][n_q][d]`` and fp32 ``[H_q][n_q]``."""
+        S, x = len(self.indices), self.indices[0]
+        qp, nqa, n_q = self._queries(queries)
+        prm = self._params(layer, frames, kinds)
+        ot, used = None, []
+        if own is not None:
+            if len(own) != S:
+                raise ValueError(f"expected own tokens (or None) for {S} streams")
+            kp, vp = (L._P * S)(), (L._P * S)()
+            no, cap = (C.c_int32 * S)(), (C.c_int32 * S)()
+            for s, o in enumerate(own):
+                if o is None:
+                    continue
+                k, v, n = o
+                shape = (x.n_kv_heads, k.shape[1] if k.dim() == 3 else 0, x.head_dim)
+                kp[s] = _check_bf16(k, shape, "own[%d] keys", s)
+                vp[s] = _check_bf16(v, shape, "own[%d] values", s)
+                self._on_device(k, "own[%d] keys", s)
+                self._on_device(v, "own[%d] values", s)
+                no[s], cap[s] = n, shape[1]
+                used += [k, v]
+            ot = L.OwnTokens(C.cast(kp, L._P), C.cast(vp, L._P), C.cast(no, L._P), C.cast(cap, L._P), None)
+        if tree is not None:
+            if ot is None or len(tree) != S:
+                raise ValueError(f"tree needs own tokens and an entry for each of {S} streams")
+            pp = (L._P * S)()
+            for s, t in enumerate(tree):
+                if t is None:
+                    continue
+                if t.dtype != torch.int32 or tuple(t.shape) != (n_q[s],) or not t.is_contiguous():
+                    raise ValueError(f"tree[{s}] must be a contiguous int32 tensor [{n_q[s]}]")
+                self._on_device(t, "tree[%d]", s)
+                pp[s] = t.data_ptr()
+                used.append(t)
+            ot.parents = C.cast(pp, L._P)
+        own_ref = C.byref(ot) if ot is not None else None
+        need = L.lib().ss_attend_workspace_bytes(self._handles, S, nqa, own_ref, C.byref(prm))
+        if need == 0:
+            raise L.SSError(L.SS_ERR_INVALID_ARGUMENT, L.lib().ss_last_error().decode())
+        ws = torch.empty(need, dtype=torch.uint8, device=self._device)
+        out = [torch.empty(q.shape, dtype=torch.bfloat16, device=self._device) for q in queries]
+        lse = [torch.empty(q.shape[:2], dtype=torch.float32, device=self._device) for q in queries]
+        L.check(L.lib().ss_attend(self._handles, S, qp, nqa, own_ref, C.byref(prm), ws.data_ptr(), need,
+                                  _stream_handle(stream), L.ptr_array([t.data_ptr() for t in out]),
+                                  L.ptr_array([t.data_ptr() for t in lse])))
+        _used_on(stream, ws, *out, *lse, *queries, *used, self.slopes, frames, kinds)
+        return out, lse
+
+    def accumulate(self, layer: int, queries, lse, frames=None, kinds=None, decay: float = 1.0, stream=None) -> None:
+        """Add the weight that these queries gave each stored row of ``layer`` to the
+        indices' :attr:`ShallowIndex.weights`, which are scaled by ``decay`` first (0
+        overwrites).  ``lse``: per stream what the attention of the same queries,
+        ``frames`` and ``kinds`` returned."""
+        S = len(self.indices)
+        qp, nqa, _ = self._queries(queries)
+        prm = self._params(layer, frames, kinds)
+        if len(lse) != S:
+            raise ValueError(f"expected lse for {S} streams, got {len(lse)}")
+        for s, (t, q) in enumerate(zip(lse, queries)):
+            if t.dtype != torch.float32 or t.shape != q.shape[:2] or not t.is_contiguous():
+                raise ValueError(f"lse[{s}] must be a contiguous fp32 tensor {list(q.shape[:2])}")
+            self._on_device(t, "lse[%d]", s)
+        need = L.lib().ss_attend_accumulate_workspace_bytes(self._handles, S, nqa, C.byref(prm))
+        if need == 0:
+            raise L.SSError(L.SS_ERR_INVALID_ARGUMENT, L.lib().ss_last_error().decode())
+        ws = torch.empty(need, dtype=torch.uint8, device=self._device)
+        L.check(L.lib().ss_attend_accumulate(self._handles, S, qp, nqa, L.ptr_array([t.data_ptr() for t in lse]),
+                                             C.byref(prm), decay, ws.data_ptr(), need, _stream_handle(stream)))
+        _used_on(stream, ws, *queries, *lse, self.slopes, frames, kinds)
 
 
 def set_profile_events(start, stop) -> None:
