@@ -802,25 +802,49 @@ size_t plan_attend(ss::AttendArgs& a, ss::AttendPlan& p, ss::RowsArgs& rows, ss_
   p.shape = 0;
   while (p.shape < 3 && kAttendTiles[p.shape].columns < m_max) ++p.shape;
   const AttendTile tile = kAttendTiles[p.shape];
-  // Shares of the key axis: about four items a CU over the batch, in proportion to
-  // each stream's tiles, none below two tiles of 128 keys.
-  auto tiles_of = [&](int i) {
-    return (visible[i] + tile.keys - 1) / tile.keys + (a.st[i].n_own + tile.keys - 1) / tile.keys;
-  };
-  int64_t total = 0;
+  // Shares of the key axis.  A CU holds one block, so items run in rounds of kCus, and
+  // a round costs its longest item: `per` tiles and what starting and ending an item
+  // costs (kItemTiles).  For each number of rounds the smallest `per` that fits it is
+  // found, and the cheapest number taken, or no sharing at all where that saves the
+  // second launch (kJoinTiles).  Measured, us, one / two / four / eight rounds: one
+  // token over 1 hour 276 / 281 / 289 / 316, 64 tokens 691 / 706 / 736 / 793; 1,024
+  // tokens over 10 minutes (112 column blocks): 224 items 1,593, 336 items 1,996, 1,008
+  // items 1,690.
+  const int64_t kItemTiles = tile.keys == 128 ? 2 : 8, kJoinTiles = 8;
+  int64_t tiles[ss::kAttendStreams], blocks_of[ss::kAttendStreams], longest_tiles = 1, whole = 0;
   for (int i = 0; i < S; ++i) {
-    const int64_t blocks = (a.G * a.st[i].n_q + tile.columns - 1) / tile.columns;
-    total += tiles_of(i) * blocks * a.Hk;
+    tiles[i] = (visible[i] + tile.keys - 1) / tile.keys + (a.st[i].n_own + tile.keys - 1) / tile.keys;
+    blocks_of[i] = (a.G * a.st[i].n_q + tile.columns - 1) / tile.columns * a.Hk;
+    longest_tiles = std::max(longest_tiles, tiles[i]);
+    whole += blocks_of[i];
   }
-  const int64_t least = 256 / tile.keys;
-  const int64_t per = std::max(least, (total + 4 * kCus - 1) / (4 * kCus));
+  auto items_at = [&](int64_t per) {
+    int64_t n = 0;
+    for (int i = 0; i < S; ++i) n += std::max<int64_t>(1, (tiles[i] + per - 1) / per) * blocks_of[i];
+    return n;
+  };
+  const int64_t rounds_whole = (whole + kCus - 1) / kCus;
+  int64_t per = longest_tiles, cost = rounds_whole * (longest_tiles + kItemTiles);
+  for (int64_t r = rounds_whole; r <= rounds_whole + 7; ++r) {
+    int64_t lo = 1, hi = longest_tiles;             // items_at(hi) = whole <= r kCus
+    while (lo < hi) {
+      const int64_t mid = (lo + hi) / 2;
+      if (items_at(mid) <= r * kCus) hi = mid;
+      else lo = mid + 1;
+    }
+    const int64_t c = r * (lo + kItemTiles) + kJoinTiles;
+    if (c < cost) {
+      cost = c;
+      per = lo;
+    }
+  }
   int64_t parts = 0;
   for (int i = 0; i < S; ++i) {
     ss::AttendStream& st = a.st[i];
-    const int64_t M = (int64_t)a.G * st.n_q, blocks = (M + tile.columns - 1) / tile.columns;
-    st.n_split = (int32_t)std::max<int64_t>(1, (tiles_of(i) + per - 1) / per);
+    const int64_t M = (int64_t)a.G * st.n_q;
+    st.n_split = (int32_t)std::max<int64_t>(1, (tiles[i] + per - 1) / per);
     st.item0 = p.items;
-    p.items += (int)(st.n_split * blocks * a.Hk);
+    p.items += (int)(st.n_split * blocks_of[i]);
     st.part0 = parts;
     if (st.n_split > 1) {
       parts += st.n_split * M * a.Hk;

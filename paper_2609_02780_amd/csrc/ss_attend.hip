@@ -203,6 +203,18 @@ __global__ __launch_bounds__(kRowsThreads) void k_rows(RowsArgs a) {
 }
 
 // ---------------------------------------------------------------------------
+// Where the 16-byte pieces of a staged row lie: piece p of row r at p ^ swizzle(r), so
+// that the lanes that read LDS in one clock (256 bytes) meet different banks: 16
+// rows at one piece for the keys, four rows at four pieces for the values.
+template <int D>
+__device__ __forceinline__ int key_swizzle(int r) {
+  return D == 128 ? (r & 15) : ((r >> 1) & 7);
+}
+template <int D>
+__device__ __forceinline__ int value_swizzle(int r) {
+  return D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2;
+}
+
 // k_attend<D, WQ, WK, BN, NS, MAP>: one item = (stream, KV head, block of 32 WQ
 // query columns, share of the key tiles).  WQ waves along the columns x WK along
 // the keys; a tile of BN keys and values is staged in LDS, NS tiles in flight.
@@ -233,6 +245,7 @@ __global__ __launch_bounds__(64 * WQ * WK) void k_attend(AttendArgs a) {
   using T = AttendShape<D, WQ, WK, BN, NS, MAP>;
   constexpr int NW = T::NW, BM = T::BM, RB = T::RB, CH = T::CH, RPI = T::RPI, NI = T::NI, SUB = T::SUB, NL = T::NL;
   constexpr int KST = D / 16, DT = D / 32;
+  constexpr bool PP = NS == 4 && NW == 8;               // two groups of waves take turns
   constexpr int MERGE_AT = (T::RING > T::MERGE ? T::RING : T::MERGE);
   __shared__ __align__(1024) unsigned char smem[T::LDS];
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(SS_LDS unsigned char*)smem);
@@ -268,6 +281,12 @@ __global__ __launch_bounds__(64 * WQ * WK) void k_attend(AttendArgs a) {
   const unsigned char* vh = reinterpret_cast<const unsigned char*>(st.values + hk * st.head_stride);
   const unsigned char* ko = reinterpret_cast<const unsigned char*>(st.own_k + (int64_t)hk * st.own_cap * D);
   const unsigned char* vo = reinterpret_cast<const unsigned char*>(st.own_v + (int64_t)hk * st.own_cap * D);
+
+  // arguments that the loop needs, kept in registers (they would be read again behind every barrier)
+  int n_own = st.n_own, draft0 = st.n_own - st.n_q;    // own tokens before draft0 are seen by every query
+  const int32_t* rowmap = st.rowmap;
+  uint32_t age_off = st.age_off;
+  asm volatile("" : "+s"(n_own), "+s"(draft0), "+s"(rowmap), "+s"(age_off));
 
   // this lane's query column
   const int c = c_lo + wq * 32 + c32, cc = min(c, M - 1);
@@ -310,14 +329,14 @@ __global__ __launch_bounds__(64 * WQ * WK) void k_attend(AttendArgs a) {
     const int g = wave % T::NG;
     const int j = max(0, min(t * BN + g * 32 + c32, n_vis - 1));
     // lanes 0..31 the rows' places, 32..63 their ages
-    const uint32_t off = (uint32_t)j * 4u + (half ? st.age_off : 0u);
-    load_lds4(st.rowmap, off, lds0 + meta_at(t, g));
+    const uint32_t off = (uint32_t)j * 4u + (half ? age_off : 0u);
+    load_lds4(rowmap, off, lds0 + meta_at(t, g));
   };
   auto issue = [&](int t) {
     const bool hist = t < Th;
     const unsigned char* kb = hist ? kh : ko;
     const unsigned char* vb = hist ? vh : vo;
-    const int n = hist ? n_vis : st.n_own, j0 = (hist ? t : t - Th) * BN;
+    const int n = hist ? n_vis : n_own, j0 = (hist ? t : t - Th) * BN;
     const uint32_t buf = lds0 + (uint32_t)((t - t0) % NS) * 2u * T::KB;
 #pragma unroll
     for (int k = 0; k < NI; ++k) {
@@ -325,30 +344,108 @@ __global__ __launch_bounds__(64 * WQ * WK) void k_attend(AttendArgs a) {
       int j = min(j0 + r, n - 1);
       if (MAP && hist) j = *reinterpret_cast<const int*>(smem + meta_at(t, r >> 5) + (r & 31) * 4);
       const uint32_t row = (uint32_t)j * RB;
-      load_lds16(kb, row + ((pos ^ (r & (CH - 1))) << 4), buf + idx * 1024);
-      load_lds16(vb, row + ((pos ^ ((r & (CH / 2 - 1)) << 1)) << 4), buf + T::KB + idx * 1024);
+      load_lds16(kb, row + ((pos ^ key_swizzle<D>(r)) << 4), buf + idx * 1024);
+      load_lds16(vb, row + ((pos ^ value_swizzle<D>(r)) << 4), buf + T::KB + idx * 1024);
     }
     if (MAP) load_meta(t + 2);
   };
 
-  auto compute = [&](int t) {
+  // LDS places of this lane's operands in the first buffer; rows 32 apart, and 8 apart
+  // for the values, have the same swizzle and differ by constants
+  const int kr = wk * 32 + c32;
+  uint32_t k_at[KST];
+#pragma unroll
+  for (int i = 0; i < KST; ++i) k_at[i] = lds0 + kr * RB + (((2 * i + half) ^ key_swizzle<D>(kr)) << 4);
+  // dimensions 32 dt + c32, keys 16 w + 8 x + 4 half + 0..3 of a group
+  const int vr = wk * 32 + 4 * half + ((lane & 15) >> 2), vd = 16 * (c32 >> 4) + (lane & 3) * 4;
+  uint32_t v_at[DT];
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+    v_at[i] = lds0 + T::KB + vr * RB + ((((32 * i + vd) >> 3) ^ value_swizzle<D>(vr)) << 4) + (vd & 7) * 2;
+
+  u32x4 pb[SUB * 2];      // p as the second product's B operand
+  f32x16 S[SUB];
+  // Both products run in steps of up to four fragments (16 bytes a lane each), the next
+  // step's read from LDS while this one's are multiplied: 128 clocks of the matrix unit
+  // cover the reads' latency.  Without that order the compiler waits for each read.
+  constexpr int VS = SUB * 2, VF = DT;                       // steps and fragments of the second product
+  constexpr int KF = KST * SUB < 4 ? KST * SUB : 4, KS = KST * SUB / KF;   // and of the first
+  constexpr int FR = VF > KF ? VF : KF;
+  u32x4 fr[2][FR];
+  uint32_t kb_at[KST], vb_at[DT];
+  auto key_buffer = [&](int t) {
+    const uint32_t buf = (uint32_t)((t - t0) % NS) * 2u * T::KB;
+#pragma unroll
+    for (int i = 0; i < KST; ++i) {
+      kb_at[i] = k_at[i] + buf;
+      asm("" : "+v"(kb_at[i]));            // one address, the groups by constant offsets
+    }
+  };
+  auto value_buffer = [&](int t) {
+    const uint32_t buf = (uint32_t)((t - t0) % NS) * 2u * T::KB;
+#pragma unroll
+    for (int i = 0; i < DT; ++i) {
+      vb_at[i] = v_at[i] + buf;
+      asm("" : "+v"(vb_at[i]));
+    }
+  };
+  auto read_keys = [&](int step, u32x4 (&f)[FR]) {
+#pragma unroll
+    for (int x = 0; x < KF; ++x) {
+      const int n = step * KF + x, i = n / SUB, u = n % SUB;
+      f[x] = *((const SS_LDS u32x4*)(uintptr_t)kb_at[i] + u * WK * 32 * RB / 16);
+    }
+  };
+  auto multiply_keys = [&](int step, const u32x4 (&f)[FR]) {
+#pragma unroll
+    for (int x = 0; x < KF; ++x) {
+      const int n = step * KF + x, i = n / SUB, u = n % SUB;
+      S[u] = mfma32(f[x], qf[i], i == 0 ? f32x16{} : S[u]);
+    }
+  };
+  auto read_values = [&](int step, u32x4 (&f)[FR]) {
+    const int u = step >> 1, w = step & 1;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (SS_LDS s16x4*)(uintptr_t)vb_at[dt] + (u * WK * 32 + 16 * w + 8 * x) * RB / 8));
+        f[dt][2 * x] = y[0];
+        f[dt][2 * x + 1] = y[1];
+      }
+  };
+  auto multiply_values = [&](int step, const u32x4 (&f)[FR]) {
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) O[dt] = mfma32(f[dt], pb[step], O[dt]);
+  };
+  // S^T of a tile whose first step is in fr[first]
+  auto scores_from = [&](int first) {
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      if (k + 1 < KS) read_keys(k + 1, fr[(first + k + 1) & 1]);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply_keys(k, fr[(first + k) & 1]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // O^T += V^T P^T with the first step in fr[0]; more(k) goes with step k
+  auto values_from = [&](auto&& more) {
+#pragma unroll
+    for (int k = 0; k < VS; ++k) {
+      if (k + 1 < VS) read_values(k + 1, fr[(k + 1) & 1]);
+      more(k);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply_values(k, fr[k & 1]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  auto softmax = [&](int t) {
     const bool hist = t < Th;
     const int n = hist ? n_vis : own_end, j0 = (hist ? t : t - Th) * BN;
-    const unsigned char* kt = smem + ((t - t0) % NS) * 2 * T::KB;
-    const unsigned char* vt = kt + T::KB;
     float sv[SUB * 16];
 #pragma unroll
-    for (int u = 0; u < SUB; ++u) {
-      const int r = (wk + u * WK) * 32 + c32;
-      f32x16 S = f32x16{};
-#pragma unroll
-      for (int i = 0; i < KST; ++i) {
-        const u32x4 k = *reinterpret_cast<const u32x4*>(kt + r * RB + (((2 * i + half) ^ (r & (CH - 1))) << 4));
-        S = mfma32(k, qf[i], S);
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sv[u * 16 + i] = S[i];
-    }
+    for (int i = 0; i < SUB * 16; ++i) sv[i] = S[i >> 4][i & 15];
     // scores in units of log 2: value * cs
     float cs = a.c1;
     if (a.cap_log2 > 0.0f) {
@@ -369,7 +466,6 @@ __global__ __launch_bounds__(64 * WQ * WK) void k_attend(AttendArgs a) {
       cs = 1.0f;
     }
     if (!hist || j0 + BN > n) {
-      const int draft0 = st.n_own - st.n_q;            // own tokens before it are seen by every query
 #pragma unroll
       for (int u = 0; u < SUB; ++u)
 #pragma unroll
@@ -379,7 +475,7 @@ __global__ __launch_bounds__(64 * WQ * WK) void k_attend(AttendArgs a) {
           if (!hist) {
             const int e = j - draft0;
             if (tree) {
-              if (e >= 0) see = see && ((anc[(min(e, st.n_q - 1) >> 5) * BM + wq * 32 + c32] >> (e & 31)) & 1u);
+              if (e >= 0) see = see && ((anc[(min(e, n_own - draft0 - 1) >> 5) * BM + wq * 32 + c32] >> (e & 31)) & 1u);
             } else {
               see = see && e <= qi;
             }
@@ -387,78 +483,123 @@ __global__ __launch_bounds__(64 * WQ * WK) void k_attend(AttendArgs a) {
           if (!see) sv[u * 16 + i] = neg_inf();
         }
     }
-    float top = sv[0];
+    // p of all scores against the subtracted maximum, packed as pb; returns their sum
+    auto form = [&](float mu) -> float {
+      float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int i = 1; i < SUB * 16; ++i) top = fmaxf(top, sv[i]);
-    top = fmaxf(top, other_half(top)) * cs;
-    if (__any(top > m)) {
+      for (int w = 0; w < SUB * 2; ++w) {
+        bf16x8 p;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float x = exp2_fast(fmaf(sv[w * 8 + e], cs, -mu));
+          sum[e & 3] += x;
+          p[e] = (__bf16)x;
+        }
+        pb[w] = __builtin_bit_cast(u32x4, p);
+      }
+      return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    };
+    // The subtracted maximum m moves only when it has to: as long as a lane's p add up
+    // to at most 2^13, fp32 sums and bf16 p are as good against an older, smaller m, and
+    // a tile needs neither its maximum nor a rescaling.  The first tile that a column
+    // sees, and one that outgrows m, forms its p anew.
+    float sum = form(m == neg_inf() ? 0.0f : m);
+    if (__any(!(sum <= 8192.0f) || m == neg_inf())) {
+      float top = sv[0];
+#pragma unroll
+      for (int i = 1; i < SUB * 16; ++i) top = fmaxf(top, sv[i]);
+      top = fmaxf(top, other_half(top)) * cs;
       const float mn = fmaxf(m, top);
       const float al = m == neg_inf() ? 0.0f : exp2_fast(m - mn);
       m = mn;
       l *= al;
 #pragma unroll
       for (int i = 0; i < DT; ++i) O[i] *= al;
-    }
-    const float mu = m == neg_inf() ? 0.0f : m;
-    float sum = 0.0f;
-#pragma unroll
-    for (int i = 0; i < SUB * 16; ++i) {
-      sv[i] = exp2_fast(fmaf(sv[i], cs, -mu));
-      sum += sv[i];
+      sum = form(m == neg_inf() ? 0.0f : m);
     }
     l += sum;
+    if constexpr (PP) {       // formed here, not behind the barrier
 #pragma unroll
-    for (int u = 0; u < SUB; ++u)
-#pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        bf16x8 p;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] = (__bf16)sv[u * 16 + w * 8 + e];
-        const u32x4 pb = __builtin_bit_cast(u32x4, p);
-        // lane: dimensions 32 dt + c32, keys 16 w + 8 x + 4 half + 0..3 of the group
-        const int g4 = (lane & 15) >> 2, d4 = 16 * (c32 >> 4) + (lane & 3) * 4;
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-          u32x4 v;
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            const int r = (wk + u * WK) * 32 + 16 * w + 8 * x + 4 * half + g4, d = 32 * dt + d4;
-            const int at = r * RB + ((((d >> 3) ^ ((r & (CH / 2 - 1)) << 1)) << 4) | ((d & 7) * 2));
-            const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SS_LDS s16x4*)(SS_LDS unsigned char*)(vt + at));
-            const u32x2 yy = __builtin_bit_cast(u32x2, y);
-            v[2 * x] = yy[0];
-            v[2 * x + 1] = yy[1];
-          }
-          O[dt] = mfma32(v, pb, O[dt]);
-        }
-      }
+      for (int w = 0; w < SUB * 2; ++w) asm volatile("" : "+v"(pb[w]));
+      asm volatile("" : "+v"(l));
+    }
   };
 
   if (t0 < t1) {
     if (MAP) {
       load_meta(t0);
       load_meta(t0 + 1);
+      if (PP) load_meta(t0 + 2);
       wait_loads<0, T::BAR>();
     }
     issue(t0);
-    if (NS > 2 && t0 + 1 < t1) issue(t0 + 1);
-    for (int t = t0; t < t1; ++t) {
-      if constexpr (NS == 2) {
-        if (t + 1 < t1) {
-          wait_loads<63, T::BAR>();       // every reader is done with the buffer that is filled next
-          issue(t + 1);
-          wait_loads<NL, T::BAR>();
-        } else {
-          wait_loads<0, T::BAR>();
-        }
-      } else {
-        if (t + 1 < t1)
-          wait_loads<NL, T::BAR>();
-        else
-          wait_loads<0, T::BAR>();
-        if (t + 2 < t1) issue(t + 2);
+    if constexpr (PP) {
+      // The two waves of a SIMD (w and w + 4) take turns: while one forms its softmax on
+      // the vector unit, the other keeps the matrix unit busy, half an iteration behind.
+      // A barrier ends each half.  Half 2t + 1 (first group: products of tile t, second:
+      // softmax of tile t) begins with tile t + 1 in LDS and all readers of tile t - 1
+      // done, whose buffer tile t + 3 then takes: each group orders its part of it at
+      // the start of its next softmax (between the products it cost 4% more).
+      const bool second = wave >= 4;
+      const int fill = second ? 3 : 2;
+      auto end_even = [&](int t) {      // of half 2t: tile t + 1 has come, t + 2 may be under way
+        if (t + 2 < t1) wait_loads<NL, true>();
+        else wait_loads<0, true>();
+      };
+      if (t0 + 1 < t1) issue(t0 + 1);
+      if (t0 + 2 < t1) issue(t0 + 2);
+      if (t0 + 2 < t1) wait_loads<2 * NL, true>();
+      else wait_loads<0, true>();
+      key_buffer(t0);
+      read_keys(0, fr[0]);
+      scores_from(0);
+      if (second) end_even(t0);
+      for (int t = t0; t < t1; ++t) {
+        // first: half 2t begins here, second: half 2t + 1
+        if (t + fill < t1 && t + fill > t0 + 2) issue(t + fill);
+        softmax(t);
+        value_buffer(t);
+        read_values(0, fr[0]);
+        if (second) wait_loads<63, true>();
+        else end_even(t);
+        // (behind the last tile the scores are those of an old buffer, and not used)
+        key_buffer(t + 1);
+        __builtin_amdgcn_s_setprio(1);
+        values_from([&](int k) {
+          if (k == VS - 1) read_keys(0, fr[VS & 1]);
+        });
+        scores_from(VS & 1);
+        __builtin_amdgcn_s_setprio(0);
+        if (second) end_even(t + 1);
+        else wait_loads<63, true>();
       }
-      compute(t);
+      if (!second) wait_loads<63, true>();
+    } else {
+      if (NS > 2 && t0 + 1 < t1) issue(t0 + 1);
+      for (int t = t0; t < t1; ++t) {
+        if constexpr (NS == 2) {
+          if (t + 1 < t1) {
+            wait_loads<63, T::BAR>();       // every reader is done with the buffer that is filled next
+            issue(t + 1);
+            wait_loads<NL, T::BAR>();
+          } else {
+            wait_loads<0, T::BAR>();
+          }
+        } else {
+          if (t + 1 < t1)
+            wait_loads<NL, T::BAR>();
+          else
+            wait_loads<0, T::BAR>();
+          if (t + 2 < t1) issue(t + 2);
+        }
+        key_buffer(t);
+        read_keys(0, fr[0]);
+        scores_from(0);
+        value_buffer(t);
+        read_values(0, fr[0]);
+        softmax(t);
+        values_from([](int) {});
+      }
     }
   }
   l += other_half(l);
@@ -566,6 +707,7 @@ __global__ __launch_bounds__(256) void k_join(AttendArgs a) {
   const float mu = mt == neg_inf() ? 0.0f : mt;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   float l = 0.0f;
+#pragma unroll 4
   for (int i = g; i < n; i += NGR) {
     const int64_t p = p0 + (int64_t)i * M;
     const float w = exp2_fast(a.part_ml[p * 2] - mu);
@@ -871,8 +1013,8 @@ hipError_t attend_impl(const AttendArgs& a, const AttendPlan& p, hipStream_t st)
   switch (p.shape) {
     case 0: e = attend_go<D, 1, 4, 128, 2>(a, p.map, p.items, st); break;
     case 1: e = attend_go<D, 2, 4, 128, 2>(a, p.map, p.items, st); break;
-    case 2: e = attend_go<D, 4, 2, 64, 3>(a, p.map, p.items, st); break;
-    default: e = attend_go<D, 8, 1, 64, 3>(a, p.map, p.items, st); break;
+    case 2: e = attend_go<D, 4, 2, 64, 4>(a, p.map, p.items, st); break;
+    default: e = attend_go<D, 8, 1, 64, 4>(a, p.map, p.items, st); break;
   }
   if (e != hipSuccess) return e;
   if (p.join) hipLaunchKernelGGL((k_join<D>), dim3(p.join_rows, a.S), dim3(256), 0, st, a);
