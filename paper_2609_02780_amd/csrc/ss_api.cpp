@@ -721,7 +721,8 @@ size_t plan_attend(ss::AttendArgs& a, ss::AttendPlan& p, ss::RowsArgs& rows, ss_
   a.c1 = (float)(scale * log2e);
   if (prm->softcap > 0.0f) {
     a.cap_x = (float)(scale / (double)prm->softcap);
-    a.cap_log2 = (float)((double)prm->softcap * log2e);
+    constexpr double fit[6] = {0.999999998, -0.333332833, 0.13331689, -0.0537687049, 0.0207536292, -0.00585216861};
+    for (int k = 0; k < 6; ++k) a.cap_c[k] = (float)((double)prm->softcap * log2e * fit[k]);
   }
   a.slopes = prm->slopes;
   p.listed = prm->frames != nullptr;
@@ -1316,14 +1317,17 @@ ss_status ss_attend(ss_index* const* idx, int32_t n_streams, const void* const* 
         return fail(SS_ERR_INVALID_ARGUMENT, "parents[%d] misaligned", s);
     }
     if (!ws || !aligned(ws, 256)) return fail(SS_ERR_WORKSPACE, "workspace NULL or not 256-byte aligned");
-    const size_t need = attend_ws(idx, n_streams, n_q, own, params, false);
+    // a batch of one group is sized by the plan it runs; of more, every group before the first is enqueued
+    size_t need = n_streams > ss::kAttendStreams ? attend_ws(idx, n_streams, n_q, own, params, false) : 0;
     if (ws_bytes < need) return fail(SS_ERR_WORKSPACE, "workspace %zu bytes, %zu needed", ws_bytes, need);
     const hipStream_t hs = static_cast<hipStream_t>(stream);
     for (int s0 = 0; s0 < n_streams; s0 += ss::kAttendStreams) {
       ss::AttendArgs a;
       ss::AttendPlan p;
       ss::RowsArgs r;
-      plan_attend(a, p, r, idx, s0, std::min(ss::kAttendStreams, n_streams - s0), n_q, own, params, false, ws);
+      need = std::max<size_t>(256, plan_attend(a, p, r, idx, s0, std::min(ss::kAttendStreams, n_streams - s0), n_q, own,
+                                               params, false, ws));
+      if (ws_bytes < need) return fail(SS_ERR_WORKSPACE, "workspace %zu bytes, %zu needed", ws_bytes, need);
       for (int i = 0; i < a.S; ++i) {
         ss::AttendStream& t = a.st[i];
         const int s = s0 + i;
@@ -1368,14 +1372,16 @@ ss_status ss_attend_accumulate(ss_index* const* idx, int32_t n_streams, const vo
                       t, s);
     }
     if (!ws || !aligned(ws, 256)) return fail(SS_ERR_WORKSPACE, "workspace NULL or not 256-byte aligned");
-    const size_t need = attend_ws(idx, n_streams, n_q, nullptr, params, true);
+    size_t need = n_streams > ss::kAttendStreams ? attend_ws(idx, n_streams, n_q, nullptr, params, true) : 0;
     if (ws_bytes < need) return fail(SS_ERR_WORKSPACE, "workspace %zu bytes, %zu needed", ws_bytes, need);
     const hipStream_t hs = static_cast<hipStream_t>(stream);
     for (int s0 = 0; s0 < n_streams; s0 += ss::kAttendStreams) {
       ss::AttendArgs a;
       ss::AttendPlan p;
       ss::RowsArgs r;
-      plan_attend(a, p, r, idx, s0, std::min(ss::kAttendStreams, n_streams - s0), n_q, nullptr, params, true, ws);
+      need = std::max<size_t>(256, plan_attend(a, p, r, idx, s0, std::min(ss::kAttendStreams, n_streams - s0), n_q,
+                                               nullptr, params, true, ws));
+      if (ws_bytes < need) return fail(SS_ERR_WORKSPACE, "workspace %zu bytes, %zu needed", ws_bytes, need);
       for (int i = 0; i < a.S; ++i) {
         a.st[i].q = static_cast<const uint16_t*>(queries[s0 + i]);
         a.st[i].lse = const_cast<float*>(lse[s0 + i]);   // read only
@@ -1432,6 +1438,8 @@ ss_status ss_index_evict(const ss_index* src, ss_index* dst, int64_t frame_hi, i
     a.n_frames = frames;
     a.n_thin = frame_hi - f_lo;
     a.keep = keep_rows;
+    a.rpf = src->rpf > 0 ? src->rpf : 0;
+    a.src_row0 = row_of(src, f_lo);
     a.src_max_rows = d.max_rows;
     a.dst_max_rows = e.max_rows;
     a.src = src->dev;

@@ -78,36 +78,37 @@ __device__ __forceinline__ void wait_loads() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
 }
 
-// tanh for |x| < 1 by the continued fraction x / (1 + x^2 / (3 + x^2 / (5 + ...)))
-// cut after 13 (off by less than 2^-30 there), so that small scores keep their
-// relative precision; elsewhere through exp.
-__device__ __forceinline__ float tanh_small(float x) {
+// tanh through exp; below 1 by the continued fraction x / (1 + x^2 / (3 + x^2 / (5 +
+// ...))) cut after 13 (off by less than 2^-30 there), which keeps small scores' relative
+// precision.
+__device__ __forceinline__ float tanh_any(float x) {
   const float y = x * x;
   const float p = fmaf(y, fmaf(y, 21.0f, 1260.0f), 10395.0f);
   const float q = fmaf(y, fmaf(y, y + 210.0f, 4725.0f), 10395.0f);
-  return x * p * __builtin_amdgcn_rcpf(q);
-}
-__device__ __forceinline__ float tanh_any(float x) {
-  const float a = fabsf(x);
-  const float e = exp2_fast(a * (-2.0f * kLog2e));
+  const float e = exp2_fast(fabsf(x) * (-2.0f * kLog2e));
   const float t = (1.0f - e) * __builtin_amdgcn_rcpf(1.0f + e);
-  return a < 1.0f ? tanh_small(x) : copysignf(t, x);
+  return fabsf(x) < 1.0f ? x * p * __builtin_amdgcn_rcpf(q) : copysignf(t, x);
 }
-// v[i] <- cap * tanh(v[i] * x) in units of log 2, x = scale / cap.
+// v[i] <- cap tanh(v[i] x) in units of log 2, x = scale / cap.  Where all of a wave's
+// |v x| are below 0.6, the usual case of a cap, tanh(z) / z is the polynomial in z^2 that
+// is off by 2^-28.6 at most there (a least-maximum fit); c holds it times the cap.
 template <int N>
-__device__ __forceinline__ void cap_scores(float (&v)[N], float x, float cap_log2) {
+__device__ __forceinline__ void cap_scores(float (&v)[N], float x, const float (&c)[6]) {
   float top = 0.0f;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     v[i] *= x;
     top = fmaxf(top, fabsf(v[i]));
   }
-  if (__any(!(top < 1.0f))) {
+  if (__any(!(top < 0.6f))) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = cap_log2 * tanh_any(v[i]);
+    for (int i = 0; i < N; ++i) v[i] = c[0] * tanh_any(v[i]);
   } else {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = cap_log2 * tanh_small(v[i]);
+    for (int i = 0; i < N; ++i) {
+      const float y = v[i] * v[i];
+      v[i] *= fmaf(y, fmaf(y, fmaf(y, fmaf(y, fmaf(y, c[5], c[4]), c[3]), c[2]), c[1]), c[0]);
+    }
   }
 }
 
@@ -448,8 +449,8 @@ __global__ __launch_bounds__(64 * WQ * WK) void k_attend(AttendArgs a) {
     for (int i = 0; i < SUB * 16; ++i) sv[i] = S[i >> 4][i & 15];
     // scores in units of log 2: value * cs
     float cs = a.c1;
-    if (a.cap_log2 > 0.0f) {
-      cap_scores(sv, a.cap_x, a.cap_log2);
+    if (a.cap_x > 0.0f) {
+      cap_scores(sv, a.cap_x, a.cap_c);
       cs = 1.0f;
     }
     if (MAP && a.slopes) {
@@ -798,8 +799,8 @@ __global__ __launch_bounds__(64 * NW) void k_accumulate(AttendArgs a, float deca
 #pragma unroll
         for (int i = 0; i < 16; ++i) sv[i] = S[i];
         float cs = a.c1;
-        if (a.cap_log2 > 0.0f) {
-          cap_scores(sv, a.cap_x, a.cap_log2);
+        if (a.cap_x > 0.0f) {
+          cap_scores(sv, a.cap_x, a.cap_c);
           cs = 1.0f;
         }
 #pragma unroll
@@ -856,7 +857,8 @@ __global__ __launch_bounds__(256) void k_store_values(StoreValuesArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// Eviction.  k_evict_offsets: the row offsets of the thinned frames, one block.
+// Eviction.  k_evict_offsets: the row offsets of the thinned frames, one block (frames
+// of one size need none: their offsets are products).
 // k_evict: a wave takes one (frame, layer, KV head).  The cut is the largest key
 // u with at least `keep` rows at or above it, found bit by bit over the weights'
 // order-preserving 32-bit image; rows above it stay, and of the rows at it the
@@ -917,10 +919,21 @@ __global__ __launch_bounds__(256) void k_evict(EvictArgs a) {
   if (it >= items) return;
   const int64_t f = it / LH;
   const int lh = (int)(it % LH);
-  const int64_t r0 = a.src.frame_off[f], n = a.src.frame_off[f + 1] - r0;
-  const int64_t s0 = (int64_t)lh * a.src_max_rows + r0, d0 = (int64_t)lh * a.dst_max_rows + a.dst.frame_off[f];
-  const float* w = a.src_weights + s0;
+  const int64_t r0 = a.rpf > 0 ? a.src_row0 + f * a.rpf : a.src.frame_off[f];
+  const int64_t n = a.rpf > 0 ? a.rpf : a.src.frame_off[f + 1] - r0;
   const int64_t keep = f < a.n_thin ? min(n, (int64_t)a.keep) : n;
+  int64_t o0;
+  if (a.rpf > 0) {
+    o0 = min(f, a.n_thin) * min(a.rpf, (int64_t)a.keep) + max(f - a.n_thin, (int64_t)0) * a.rpf;
+    if (lh == 0 && lane == 0) {
+      if (f == 0) a.dst.frame_off[0] = 0;
+      a.dst.frame_off[f + 1] = (int32_t)(o0 + keep);
+    }
+  } else {
+    o0 = a.dst.frame_off[f];
+  }
+  const int64_t s0 = (int64_t)lh * a.src_max_rows + r0, d0 = (int64_t)lh * a.dst_max_rows + o0;
+  const float* w = a.src_weights + s0;
   uint32_t cut = 0;
   int64_t ties = n;                                      // rows at the cut that stay (keep == n: all)
   if (keep < n) {
@@ -1067,9 +1080,12 @@ hipError_t launch_store_values(const StoreValuesArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_evict(EvictArgs a, hipStream_t st) {
-  hipLaunchKernelGGL(k_evict_offsets, dim3(1), dim3(1024), 0, st, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (a.n_frames == 0) a.rpf = 0;
+  if (a.rpf <= 0) {
+    hipLaunchKernelGGL(k_evict_offsets, dim3(1), dim3(1024), 0, st, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
   a.item_blocks = cdiv(a.n_frames * a.L * a.Hk, 4);
   const int64_t copy = std::max<int64_t>(1, std::min<int64_t>(cdiv(a.n_frames * a.Hk * a.D * (1 + a.L) / 4, 1024), 4096));
   const dim3 grid((unsigned)(a.item_blocks + copy));

@@ -305,7 +305,8 @@ struct AttendStream {
 struct AttendArgs {
   int S, Hk, G;
   float c1;                    // log2(e) / sqrt(d)
-  float cap_x, cap_log2;       // 1 / (cap sqrt(d)), cap log2(e); 0: scores are not capped
+  float cap_x;                 // 1 / (cap sqrt(d)); 0: scores are not capped
+  float cap_c[6];              // cap log2(e) times the polynomial of tanh(z) / z in z^2 (see cap_scores)
   const float* slopes;         // [H_q] or null
   float* part_o;               // partial sums [rows][d] and their (maximum, sum)
   float* part_ml;
@@ -325,6 +326,7 @@ struct EvictArgs {
   int L, Hk, D;
   int64_t n_frames, n_thin;
   int keep;
+  int64_t rpf, src_row0;       // rows of every frame and the first one's place, or 0: by the offsets
   int64_t src_max_rows, dst_max_rows;
   IndexDev src, dst;
   const uint16_t* src_values;

@@ -6,6 +6,7 @@ given as ``torch.bfloat16`` or as raw ``int16``/``uint16`` bit patterns.
 from __future__ import annotations
 
 import ctypes as C
+import math
 
 import torch
 
@@ -88,6 +89,7 @@ class ShallowIndex:
             L.check(L.lib().ss_index_create(C.byref(self.desc), None, 0, C.byref(h)))
         dev = torch.device(device) if device is not None else torch.device("cuda", torch.cuda.current_device())
         self.arena = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        self._key_rows = self._value_rows = self._weight_rows = None    # views, made when first asked for
         self._h = C.c_void_p()
         L.check(L.lib().ss_index_create(C.byref(self.desc), self.arena.data_ptr(), nbytes, C.byref(self._h)))
         self.n_layers, self.n_q_heads, self.n_kv_heads, self.head_dim = n_layers, n_q_heads, n_kv_heads, head_dim
@@ -162,7 +164,11 @@ class ShallowIndex:
         nbytes = L.lib().ss_values_required_bytes(C.byref(self.desc))
         arena = torch.empty(nbytes, dtype=torch.uint8, device=self.arena.device)
         L.check(L.lib().ss_index_attach_values(self.handle, arena.data_ptr(), nbytes))
+        d = self.desc
+        at = (d.n_layers * d.n_kv_heads * d.max_rows * d.head_dim * 2 + 255) // 256 * 256
         self.value_arena = arena
+        self._value_rows = self._rows_view(arena, 0, torch.bfloat16, self.head_dim)
+        self._weight_rows = self._rows_view(arena, at, torch.float32)
 
     def append_kv(self, layer_keys, layer_values, n_frames: int, n_tokens: int, stream=None) -> int:
         """:meth:`append` for an index that keeps values; ``layer_values[l]`` is laid
@@ -178,33 +184,32 @@ class ShallowIndex:
         _used_on(stream, *layer_keys, *layer_values)
         return first.value
 
-    def _rows_view(self, arena, at: int, dtype, width: int):
+    def _rows_view(self, arena, at: int, dtype, *width: int) -> torch.Tensor:
+        """An arena part as ``[L][H_kv][max_rows]`` rows."""
         d = self.desc
-        n = d.n_layers * d.n_kv_heads * d.max_rows * width * dtype.itemsize
-        t = arena[at:at + n].view(dtype).view(d.n_layers, d.n_kv_heads, d.max_rows, width)
-        return t[:, :, :self.n_rows]
-
-    def _values_arena(self):
-        if getattr(self, "value_arena", None) is None:
-            raise ValueError("the index keeps no values (attach_values)")
-        return self.value_arena
+        n = d.n_layers * d.n_kv_heads * d.max_rows * math.prod(width) * dtype.itemsize
+        return arena[at:at + n].view(dtype).view(d.n_layers, d.n_kv_heads, d.max_rows, *width)
 
     @property
     def keys(self) -> torch.Tensor:
         """View of the stored keys, bfloat16 ``[L][H_kv][n_rows][d]`` (read only)."""
-        return self._rows_view(self.arena, 0, torch.bfloat16, self.head_dim)
+        if self._key_rows is None:
+            self._key_rows = self._rows_view(self.arena, 0, torch.bfloat16, self.head_dim)
+        return self._key_rows[:, :, :self.n_rows]
 
     @property
     def values(self) -> torch.Tensor:
         """View of the stored values, laid out as :attr:`keys` (read only)."""
-        return self._rows_view(self._values_arena(), 0, torch.bfloat16, self.head_dim)
+        if self._value_rows is None:
+            raise ValueError("the index keeps no values (attach_values)")
+        return self._value_rows[:, :, :self.n_rows]
 
     @property
     def weights(self) -> torch.Tensor:
         """View of the rows' attention weights, fp32 ``[L][H_kv][n_rows]`` (may be written)."""
-        d = self.desc
-        at = (d.n_layers * d.n_kv_heads * d.max_rows * d.head_dim * 2 + 255) // 256 * 256
-        return self._rows_view(self._values_arena(), at, torch.float32, 1)[..., 0]
+        if self._weight_rows is None:
+            raise ValueError("the index keeps no values (attach_values)")
+        return self._weight_rows[:, :, :self.n_rows]
 
     def evict_into(self, dst: "ShallowIndex", frame_hi: int, keep_rows: int, stream=None) -> None:
         """Replace what ``dst`` holds by this index's detailed window, thinned: each
