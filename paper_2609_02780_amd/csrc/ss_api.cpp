@@ -720,9 +720,14 @@ size_t plan_attend(ss::AttendArgs& a, ss::AttendPlan& p, ss::RowsArgs& rows, ss_
   const double scale = 1.0 / std::sqrt((double)d.head_dim), log2e = 1.4426950408889634;
   a.c1 = (float)(scale * log2e);
   if (prm->softcap > 0.0f) {
-    a.cap_x = (float)(scale / (double)prm->softcap);
     constexpr double fit[6] = {0.999999998, -0.333332833, 0.13331689, -0.0537687049, 0.0207536292, -0.00585216861};
-    for (int k = 0; k < 6; ++k) a.cap_c[k] = (float)((double)prm->softcap * log2e * fit[k]);
+    constexpr double near_fit[4] = {0.9999999653, -0.3333242244, 0.1329579934, -0.04895823077};
+    const double cap = (double)prm->softcap, x = scale / cap;
+    a.cap.x = (float)x;
+    for (int k = 0; k < 6; ++k) a.cap.fit[k] = (float)(cap * log2e * fit[k]);
+    // powers of x up to the seventh have to stay in range
+    a.cap.near_limit = cap <= 1e3 ? (float)(0.35 / x) : 0.0f;
+    for (int k = 0; k < 4; ++k) a.cap.near_fit[k] = (float)(cap * log2e * near_fit[k] * std::pow(x, 2 * k + 1));
   }
   a.slopes = prm->slopes;
   p.listed = prm->frames != nullptr;
@@ -787,13 +792,18 @@ size_t plan_attend(ss::AttendArgs& a, ss::AttendPlan& p, ss::RowsArgs& rows, ss_
   }
 
   if (accumulate) {
-    // 32 keys a wave at a time; as many shares as keep the card's waves busy
+    // A wave takes 32 keys at a time, every wave the same number of turns.  Few query
+    // rows (bound by reading the keys): many short blocks, which end evenly (16 / 32 / 64
+    // / 128 a CU: 140 / 133 / 132 / 144 us for one token over 1 hour).  More rows: one
+    // round of the two blocks that a CU holds with 256 rows staged in LDS.
     p.shape = m_max <= 32 ? 0 : 1;
-    const int64_t waves = p.shape == 0 ? 4 : 8, want = (p.shape == 0 ? 8 : 4) * kCus;
+    const int64_t waves = p.shape == 0 ? 4 : 8, slots = (p.shape == 0 ? 64 : 2) * kCus;
+    int64_t groups = 0;
+    for (int i = 0; i < S; ++i) groups += (visible[i] + 31) / 32 * a.Hk;
+    const int64_t turns = std::max<int64_t>(1, (groups + slots * waves - 1) / (slots * waves));
     for (int i = 0; i < S; ++i) {
       ss::AttendStream& st = a.st[i];
-      const int64_t groups = (visible[i] + 31) / 32;
-      st.n_split = (int32_t)std::max<int64_t>(1, std::min((groups + waves - 1) / waves, want / std::max(1, S * a.Hk)));
+      st.n_split = (int32_t)std::max<int64_t>(1, ((visible[i] + 31) / 32 + turns * waves - 1) / (turns * waves));
       st.item0 = p.items;
       p.items += st.n_split * a.Hk;
     }
@@ -847,10 +857,8 @@ size_t plan_attend(ss::AttendArgs& a, ss::AttendPlan& p, ss::RowsArgs& rows, ss_
     st.item0 = p.items;
     p.items += (int)(st.n_split * blocks_of[i]);
     st.part0 = parts;
-    if (st.n_split > 1) {
-      parts += st.n_split * M * a.Hk;
-      p.join = true;
-    }
+    p.join_parts = std::max(p.join_parts, st.n_split);
+    if (st.n_split > 1) parts += st.n_split * M * a.Hk;
   }
   a.part_o = reinterpret_cast<float*>(take((size_t)parts * p.D * 4));
   a.part_ml = reinterpret_cast<float*>(take((size_t)parts * 8));

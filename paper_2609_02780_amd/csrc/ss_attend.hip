@@ -60,12 +60,20 @@ __device__ __forceinline__ float other_half(float v) {
 // piece lands at lds + 16 l (4 l).  Written as asm because the compiler makes every
 // later LDS read wait for all such loads; the waits are counted by hand below.  No
 // register is written, and the caller waits before the pieces are read.
+// (base and lds are the same in every lane; readfirstlane keeps them in scalar registers.)
+__device__ __forceinline__ const void* in_scalar(const void* p) {
+  const uint64_t x = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
+  return reinterpret_cast<const void*>((uint64_t)hi << 32 | lo);
+}
 __device__ __forceinline__ void load_lds16(const void* base, uint32_t off, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)),
+               "v"(off), "s"(in_scalar(base))
                : "memory");
 }
 __device__ __forceinline__ void load_lds4(const void* base, uint32_t off, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(off), "s"(base)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)),
+               "v"(off), "s"(in_scalar(base))
                : "memory");
 }
 // At most N of this wave's loads are still under way, and its LDS reads are done;
@@ -89,26 +97,30 @@ __device__ __forceinline__ float tanh_any(float x) {
   const float t = (1.0f - e) * __builtin_amdgcn_rcpf(1.0f + e);
   return fabsf(x) < 1.0f ? x * p * __builtin_amdgcn_rcpf(q) : copysignf(t, x);
 }
-// v[i] <- cap tanh(v[i] x) in units of log 2, x = scale / cap.  Where all of a wave's
-// |v x| are below 0.6, the usual case of a cap, tanh(z) / z is the polynomial in z^2 that
-// is off by 2^-28.6 at most there (a least-maximum fit); c holds it times the cap.
+// v[i] <- cap tanh(v[i] x) in units of log 2, x = scale / cap: by polynomials of least
+// maximum error in z^2, z = v x, for tanh(z) / z: of degree 3 where all of a wave's |z|
+// are below 0.35 (off by 2^-24.9 at most), of degree 5 below 0.6 (2^-28.6).  Scores far
+// below their cap are the usual case.
 template <int N>
-__device__ __forceinline__ void cap_scores(float (&v)[N], float x, const float (&c)[6]) {
+__device__ __forceinline__ void cap_scores(float (&v)[N], const CapArgs& a) {
   float top = 0.0f;
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    v[i] *= x;
-    top = fmaxf(top, fabsf(v[i]));
-  }
-  if (__any(!(top < 0.6f))) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = c[0] * tanh_any(v[i]);
-  } else {
+  for (int i = 0; i < N; ++i) top = fmaxf(top, fabsf(v[i]));
+  if (!__any(!(top < a.near_limit))) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const float y = v[i] * v[i];
-      v[i] *= fmaf(y, fmaf(y, fmaf(y, fmaf(y, fmaf(y, c[5], c[4]), c[3]), c[2]), c[1]), c[0]);
+      v[i] *= fmaf(y, fmaf(y, fmaf(y, a.near_fit[3], a.near_fit[2]), a.near_fit[1]), a.near_fit[0]);
     }
+  } else if (!__any(!(top * a.x < 0.6f))) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float z = v[i] * a.x, y = z * z;
+      v[i] = z * fmaf(y, fmaf(y, fmaf(y, fmaf(y, fmaf(y, a.fit[5], a.fit[4]), a.fit[3]), a.fit[2]), a.fit[1]), a.fit[0]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = a.fit[0] * tanh_any(v[i] * a.x);
   }
 }
 
@@ -139,33 +151,41 @@ __global__ __launch_bounds__(kRowsThreads) void k_rows(RowsArgs a) {
     if (blockIdx.x == 0 && tid == 0) st.n_vis[0] = st.n_rows;
     return;
   }
-  __shared__ int ids[kMaxListed];         // stored frame of each entry, kept ones in order, then INT_MAX
+  __shared__ int ids[kMaxListed];         // stored frame of each entry, ascending; no frame: INT_MAX
   __shared__ int pre[kMaxListed];         // rows before each
-  __shared__ int part[kRowsThreads];
+  __shared__ int part[kWaves];
   int P2 = 1;
   while (P2 < a.n_listed) P2 <<= 1;
-  for (int i = tid; i < P2; i += kRowsThreads) {
-    int v = 0x7FFFFFFF;
-    if (i < a.n_listed) {
-      const int64_t f = st.list[i];
-      if ((!st.kinds || st.kinds[i] == 0) && f >= st.f_lo && f < st.f_hi) v = (int)(f - st.frame_base);
-    }
-    ids[i] = v;
-  }
-  for (int k = 2; k <= P2; k <<= 1)
-    for (int j = k >> 1; j > 0; j >>= 1) {
-      __syncthreads();
-      for (int i = tid; i < P2; i += kRowsThreads) {
-        const int o = i ^ j;
-        if (o > i) {
-          const int x = ids[i], y = ids[o];
-          if ((x > y) == ((i & k) == 0)) {
-            ids[i] = y;
-            ids[o] = x;
+  auto entry = [&](int i) -> int {
+    if (i >= a.n_listed || (st.kinds && st.kinds[i] != 0)) return 0x7FFFFFFF;
+    const int64_t f = st.list[i];
+    return f >= st.f_lo && f < st.f_hi ? (int)(f - st.frame_base) : 0x7FFFFFFF;
+  };
+  if (P2 <= kRowsThreads) {
+    // each entry's place is the number of entries before it
+    const int mine = entry(tid);
+    pre[tid] = mine;
+    __syncthreads();
+    int at = 0;
+    for (int j = 0; j < P2; ++j) at += pre[j] < mine || (pre[j] == mine && j < tid);
+    if (tid < P2) ids[at] = mine;
+  } else {
+    for (int i = tid; i < P2; i += kRowsThreads) ids[i] = entry(i);
+    for (int k = 2; k <= P2; k <<= 1)
+      for (int j = k >> 1; j > 0; j >>= 1) {
+        __syncthreads();
+        for (int i = tid; i < P2; i += kRowsThreads) {
+          const int o = i ^ j;
+          if (o > i) {
+            const int x = ids[i], y = ids[o];
+            if ((x > y) == ((i & k) == 0)) {
+              ids[i] = y;
+              ids[o] = x;
+            }
           }
         }
       }
-    }
+  }
   __syncthreads();
   // rows before each distinct frame: a run of entries per thread, then the threads' sums
   const int run = (P2 + kRowsThreads - 1) / kRowsThreads;
@@ -176,21 +196,26 @@ __global__ __launch_bounds__(kRowsThreads) void k_rows(RowsArgs a) {
   };
   int sum = 0;
   for (int i = tid * run; i < min(P2, (tid + 1) * run); ++i) sum += rows_of(i);
-  part[tid] = sum;
-  __syncthreads();
-  for (int d = 1; d < kRowsThreads; d <<= 1) {
-    const int v = tid >= d ? part[tid - d] : 0;
-    __syncthreads();
-    part[tid] += v;
-    __syncthreads();
+  int upto = sum;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int v = __shfl_up(upto, d);
+    if (lane >= d) upto += v;
   }
-  int at = part[tid] - sum;
+  if (lane == 63) part[wave] = upto;
+  __syncthreads();
+  int at = upto - sum, all = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wave) at += part[w];
+    all += part[w];
+  }
   for (int i = tid * run; i < min(P2, (tid + 1) * run); ++i) {
     pre[i] = at;
     at += rows_of(i);
   }
   __syncthreads();
-  if (blockIdx.x == 0 && tid == 0) st.n_vis[0] = part[kRowsThreads - 1];
+  if (blockIdx.x == 0 && tid == 0) st.n_vis[0] = all;
   for (int i = blockIdx.x * kWaves + wave; i < P2; i += gridDim.x * kWaves) {
     const int n = rows_of(i);
     if (n == 0) continue;
@@ -284,12 +309,16 @@ __global__ __launch_bounds__(64 * WQ * WK) void k_attend(AttendArgs a) {
   const unsigned char* vo = reinterpret_cast<const unsigned char*>(st.own_v + (int64_t)hk * st.own_cap * D);
 
   // arguments that the loop needs, kept in registers (they would be read again behind every barrier)
-  int n_own = st.n_own, draft0 = st.n_own - st.n_q;    // own tokens before draft0 are seen by every query
-  const int32_t* rowmap = st.rowmap;
-  uint32_t age_off = st.age_off;
-  asm volatile("" : "+s"(n_own), "+s"(draft0), "+s"(rowmap), "+s"(age_off));
+  auto keep = [](auto x) {
+    asm volatile("" : "+v"(x));
+    if constexpr (sizeof(x) == 4) return (decltype(x))__builtin_amdgcn_readfirstlane((int)x);
+    else return (decltype(x))in_scalar(x);
+  };
+  const int n_own = keep(st.n_own), draft0 = keep(st.n_own - st.n_q);   // own tokens before draft0 are seen by every query
+  const int32_t* rowmap = keep(st.rowmap);
+  const uint32_t age_off = keep(st.age_off);
 
-  // this lane's query column
+  // this lane's query column (behind the last one: that one again, not written)
   const int c = c_lo + wq * 32 + c32, cc = min(c, M - 1);
   const int qi = cc % st.n_q;
   const float slope2 = (MAP && a.slopes) ? a.slopes[hk * a.G + cc / st.n_q] * kLog2e : 0.0f;
@@ -449,8 +478,8 @@ __global__ __launch_bounds__(64 * WQ * WK) void k_attend(AttendArgs a) {
     for (int i = 0; i < SUB * 16; ++i) sv[i] = S[i >> 4][i & 15];
     // scores in units of log 2: value * cs
     float cs = a.c1;
-    if (a.cap_x > 0.0f) {
-      cap_scores(sv, a.cap_x, a.cap_c);
+    if (a.cap.x > 0.0f) {
+      cap_scores(sv, a.cap);
       cs = 1.0f;
     }
     if (MAP && a.slopes) {
@@ -541,8 +570,6 @@ __global__ __launch_bounds__(64 * WQ * WK) void k_attend(AttendArgs a) {
       // softmax of tile t) begins with tile t + 1 in LDS and all readers of tile t - 1
       // done, whose buffer tile t + 3 then takes: each group orders its part of it at
       // the start of its next softmax (between the products it cost 4% more).
-      const bool second = wave >= 4;
-      const int fill = second ? 3 : 2;
       auto end_even = [&](int t) {      // of half 2t: tile t + 1 has come, t + 2 may be under way
         if (t + 2 < t1) wait_loads<NL, true>();
         else wait_loads<0, true>();
@@ -554,6 +581,8 @@ __global__ __launch_bounds__(64 * WQ * WK) void k_attend(AttendArgs a) {
       key_buffer(t0);
       read_keys(0, fr[0]);
       scores_from(0);
+      const bool second = wave >= 4;
+      const int fill = second ? 3 : 2;
       if (second) end_even(t0);
       for (int t = t0; t < t1; ++t) {
         // first: half 2t begins here, second: half 2t + 1
@@ -683,53 +712,64 @@ __global__ __launch_bounds__(64 * WQ * WK) void k_attend(AttendArgs a) {
   }
 }
 
-// k_join: the parts of one query row, brought to one maximum and added in their
-// order.  A block takes one row: 256 / (D / 4) groups of lanes share the parts.
-template <int D>
+// k_join: the parts of one query row, brought to one maximum and added in a fixed
+// order: GPR groups of D / 4 lanes share a row's parts (8 where there are many, 1 where
+// a few: then a block takes several rows).
+template <int D, int GPR>
 __global__ __launch_bounds__(256) void k_join(AttendArgs a) {
   const AttendStream& st = a.st[blockIdx.y];
   const int M = a.G * st.n_q, n = st.n_split;
-  const int row = blockIdx.x;
-  if (n == 1 || row >= a.Hk * M) return;
+  constexpr int L4 = D / 4, ROWS = 256 / L4 / GPR;
+  const int tid = threadIdx.x, g = tid / L4 % GPR, d4 = (tid % L4) * 4;
+  const int row = blockIdx.x * ROWS + tid / (L4 * GPR);
+  if (n == 1 || blockIdx.x * ROWS >= a.Hk * M) return;      // the whole block
+  const bool live = row < a.Hk * M;
   const int hk = row / M, c = row % M;
-  constexpr int L4 = D / 4, NGR = 256 / L4;
-  __shared__ float so[NGR][D];
-  __shared__ float sl[NGR];
-  __shared__ float sm[4];
-  const int tid = threadIdx.x, g = tid / L4, d4 = (tid % L4) * 4;
-  const int64_t p0 = st.part0 + (int64_t)hk * n * M + c;
+  const int64_t p0 = live ? st.part0 + (int64_t)hk * n * M + c : 0;
   float mt = neg_inf();
-  for (int i = tid; i < n; i += 256) mt = fmaxf(mt, a.part_ml[(p0 + (int64_t)i * M) * 2]);
+  for (int i = tid % (L4 * GPR); live && i < n; i += L4 * GPR) mt = fmaxf(mt, a.part_ml[(p0 + (int64_t)i * M) * 2]);
+  constexpr int WIDE = L4 * GPR < 64 ? L4 * GPR : 64;
 #pragma unroll
-  for (int x = 32; x > 0; x >>= 1) mt = fmaxf(mt, __shfl_xor(mt, x));
-  if ((tid & 63) == 0) sm[tid >> 6] = mt;
-  __syncthreads();
-  mt = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
+  for (int x = WIDE / 2; x > 0; x >>= 1) mt = fmaxf(mt, __shfl_xor(mt, x));
+  if constexpr (L4 * GPR > 64) {
+    __shared__ float sm[4];
+    constexpr int NWV = L4 * GPR / 64;
+    if ((tid & 63) == 0) sm[tid >> 6] = mt;
+    __syncthreads();
+    const int w0 = tid / (L4 * GPR) * NWV;
+#pragma unroll
+    for (int x = 0; x < NWV; ++x) mt = fmaxf(mt, sm[w0 + x]);
+  }
   const float mu = mt == neg_inf() ? 0.0f : mt;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   float l = 0.0f;
 #pragma unroll 4
-  for (int i = g; i < n; i += NGR) {
+  for (int i = g; live && i < n; i += GPR) {
     const int64_t p = p0 + (int64_t)i * M;
     const float w = exp2_fast(a.part_ml[p * 2] - mu);
     l = fmaf(a.part_ml[p * 2 + 1], w, l);
     o += *reinterpret_cast<const f32x4*>(a.part_o + p * D + d4) * w;
   }
-  *reinterpret_cast<f32x4*>(&so[g][d4]) = o;
-  if (tid % L4 == 0) sl[g] = l;
-  __syncthreads();
-  if (g > 0) return;
+  if constexpr (GPR > 1) {
+    __shared__ __align__(16) float so[256 / L4][D];
+    __shared__ float sl[256 / L4];
+    *reinterpret_cast<f32x4*>(&so[tid / L4][d4]) = o;
+    if (tid % L4 == 0) sl[tid / L4] = l;
+    __syncthreads();
+    if (g > 0) return;
 #pragma unroll
-  for (int x = 1; x < NGR; ++x) {
-    o += *reinterpret_cast<const f32x4*>(&so[x][d4]);
-    l += sl[x];
+    for (int x = 1; x < GPR; ++x) {
+      o += *reinterpret_cast<const f32x4*>(&so[tid / L4 + x][d4]);
+      l += sl[tid / L4 + x];
+    }
   }
+  if (!live) return;
   const float inv = l > 0.0f ? 1.0f / l : 0.0f;
   bf16x4 v;
 #pragma unroll
   for (int e = 0; e < 4; ++e) v[e] = (__bf16)(o[e] * inv);
   *reinterpret_cast<bf16x4*>(st.out + (int64_t)row * D + d4) = v;
-  if (tid == 0 && st.lse) st.lse[row] = l > 0.0f ? (mt + __builtin_amdgcn_logf(l)) * kLn2 : neg_inf();
+  if (d4 == 0 && st.lse) st.lse[row] = l > 0.0f ? (mt + __builtin_amdgcn_logf(l)) * kLn2 : neg_inf();
 }
 
 // ---------------------------------------------------------------------------
@@ -799,8 +839,8 @@ __global__ __launch_bounds__(64 * NW) void k_accumulate(AttendArgs a, float deca
 #pragma unroll
         for (int i = 0; i < 16; ++i) sv[i] = S[i];
         float cs = a.c1;
-        if (a.cap_x > 0.0f) {
-          cap_scores(sv, a.cap_x, a.cap_c);
+        if (a.cap.x > 0.0f) {
+          cap_scores(sv, a.cap);
           cs = 1.0f;
         }
 #pragma unroll
@@ -1030,7 +1070,8 @@ hipError_t attend_impl(const AttendArgs& a, const AttendPlan& p, hipStream_t st)
     default: e = attend_go<D, 8, 1, 64, 4>(a, p.map, p.items, st); break;
   }
   if (e != hipSuccess) return e;
-  if (p.join) hipLaunchKernelGGL((k_join<D>), dim3(p.join_rows, a.S), dim3(256), 0, st, a);
+  if (p.join_parts > 4) hipLaunchKernelGGL((k_join<D, 8>), dim3(cdiv(p.join_rows * 8, 1024 / D), a.S), dim3(256), 0, st, a);
+  else if (p.join_parts > 1) hipLaunchKernelGGL((k_join<D, 1>), dim3(cdiv(p.join_rows, 1024 / D), a.S), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 

@@ -302,11 +302,15 @@ struct AttendStream {
   int32_t n_q, n_own, own_cap;
   int32_t n_split, item0;
 };
+struct CapArgs {               // see cap_scores
+  float x;                     // 1 / (cap sqrt(d)); 0: scores are not capped
+  float near_limit;            // scores (q.k) below it take near_fit
+  float near_fit[4], fit[6];   // cap log2(e) times the polynomials of tanh(z) / z, near_fit in q.k
+};
 struct AttendArgs {
   int S, Hk, G;
   float c1;                    // log2(e) / sqrt(d)
-  float cap_x;                 // 1 / (cap sqrt(d)); 0: scores are not capped
-  float cap_c[6];              // cap log2(e) times the polynomial of tanh(z) / z in z^2 (see cap_scores)
+  CapArgs cap;
   const float* slopes;         // [H_q] or null
   float* part_o;               // partial sums [rows][d] and their (maximum, sum)
   float* part_ml;
@@ -314,7 +318,8 @@ struct AttendArgs {
 };
 struct AttendPlan {
   int D, shape, items;         // shape: which tiling of k_attend / k_accumulate
-  bool map, listed, join;
+  bool map, listed;
+  int join_parts;              // largest n_split of the batch
   int join_rows;               // largest H_q n_q of the batch
 };
 hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t st);

@@ -540,6 +540,7 @@ class HistoryAttention:
                                    or slopes.device != self._device):
             raise ValueError(f"slopes must be a contiguous fp32 tensor [{x.n_q_heads}] on {self._device}")
         self.softcap, self.slopes = float(softcap), slopes
+        self._least = torch.empty(256, dtype=torch.uint8, device=self._device)
         self._handles = L.ptr_array([y.handle.value for y in self.indices])
 
     def _on_device(self, t, what: str, *at):
@@ -630,7 +631,8 @@ class HistoryAttention:
         need = L.lib().ss_attend_workspace_bytes(self._handles, S, nqa, own_ref, C.byref(prm))
         if need == 0:
             raise L.SSError(L.SS_ERR_INVALID_ARGUMENT, L.lib().ss_last_error().decode())
-        ws = torch.empty(need, dtype=torch.uint8, device=self._device)
+        # the least workspace is not written: calls share it
+        ws = self._least if need == 256 else torch.empty(need, dtype=torch.uint8, device=self._device)
         out = [torch.empty(q.shape, dtype=torch.bfloat16, device=self._device) for q in queries]
         lse = [torch.empty(q.shape[:2], dtype=torch.float32, device=self._device) for q in queries]
         L.check(L.lib().ss_attend(self._handles, S, qp, nqa, own_ref, C.byref(prm), ws.data_ptr(), need,
@@ -656,7 +658,7 @@ class HistoryAttention:
         need = L.lib().ss_attend_accumulate_workspace_bytes(self._handles, S, nqa, C.byref(prm))
         if need == 0:
             raise L.SSError(L.SS_ERR_INVALID_ARGUMENT, L.lib().ss_last_error().decode())
-        ws = torch.empty(need, dtype=torch.uint8, device=self._device)
+        ws = self._least if need == 256 else torch.empty(need, dtype=torch.uint8, device=self._device)
         L.check(L.lib().ss_attend_accumulate(self._handles, S, qp, nqa, L.ptr_array([t.data_ptr() for t in lse]),
                                              C.byref(prm), decay, ws.data_ptr(), need, _stream_handle(stream)))
         _used_on(stream, ws, *queries, *lse, self.slopes, frames, kinds)
