@@ -514,6 +514,8 @@ typedef struct {
  *   out      host array of device pointers to bf16 [H_q][n_q][d] (16-byte aligned);
  *   lse      NULL, or a host array of device pointers to fp32 [H_q][n_q]: the
  *            natural log of the softmax's denominator, ln sum_j exp(s_j).
+ * Outputs may not overlap each other or an input (an out that is also one of the
+ * queries is refused).
  * A query that sees nothing gives out = 0 and lse = -inf.  Scores, maxima and sums
  * are fp32; p is rounded to bf16 before it meets the values.  A result depends on
  * its stream's arguments and on the batch's sizes (how the rows are shared out),

@@ -1317,6 +1317,11 @@ ss_status ss_attend(ss_index* const* idx, int32_t n_streams, const void* const* 
         return fail(SS_ERR_INVALID_ARGUMENT, "out[%d] NULL or not 16-byte aligned", s);
       if (lse && (!lse[s] || !aligned(lse[s], 4)))
         return fail(SS_ERR_INVALID_ARGUMENT, "lse[%d] NULL or misaligned", s);
+      for (int t = 0; t < n_streams; ++t)
+        if (out[s] == queries[t]) return fail(SS_ERR_INVALID_ARGUMENT, "out[%d] is queries[%d]", s, t);
+      for (int t = 0; t < s; ++t)
+        if (out[s] == out[t] || (lse && lse[s] == lse[t]))
+          return fail(SS_ERR_INVALID_ARGUMENT, "streams %d and %d have one output", t, s);
       if (own_count(own, s) == 0) continue;
       if (!own->keys || !own->values || !own->keys[s] || !own->values[s] || !aligned(own->keys[s], 16) ||
           !aligned(own->values[s], 16))

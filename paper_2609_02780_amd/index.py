@@ -216,6 +216,8 @@ class ShallowIndex:
         frame before ``frame_hi`` keeps the ``keep_rows`` rows of the largest weight for
         each (layer, KV head), in their order (ties to the earlier row); later frames
         come whole."""
+        if dst.arena.device != self.arena.device:
+            raise ValueError(f"dst lives on {dst.arena.device}, this index on {self.arena.device}")
         L.check(L.lib().ss_index_evict(self.handle, dst.handle, frame_hi, keep_rows, _stream_handle(stream)))
 
     def export(self, stream=None) -> dict:

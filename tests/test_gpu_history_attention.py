@@ -241,6 +241,69 @@ def test_large_scores():
         check((out[0], lse[0]), want(st, 0, q, softcap=cap), cap)
 
 
+def test_far_addresses():
+    """Rows whose places lie beyond 2^32 bytes of the arenas, in every operator."""
+    import paper_2609_02780_amd as P
+    rng = np.random.default_rng(15)
+    heads, rows = (16, 8, 128), 1_300_000                  # a KV head: 333 MB, a layer: 2.7 GB
+    ix = P.ShallowIndex(2, *heads, 40, rows)
+    ix.attach_values()
+    st = Stream(rng, heads, [], L=2)
+    st.ix, st.rows = ix, [33] * 20
+    st.k = [bf(rng, 8, 660, 128) for _ in range(2)]
+    st.v = [bf(rng, 8, 660, 128) for _ in range(2)]
+    ix.append_kv([dev(x) for x in st.k], [dev(x) for x in st.v], 20, 33)
+    q = bf(rng, 16, 5, 128)
+    lists = torch.tensor([[19, 3, 7]], device="cuda")
+    for att, fr in ((P.HistoryAttention([ix]), None), (P.HistoryAttention([ix]), lists)):
+        out, lse = att(1, [dev(q)], frames=fr)
+        check((out[0], lse[0]), want(st, 1, q, frames=None if fr is None else fr[0].tolist()))
+        att.accumulate(1, [dev(q)], lse, frames=fr, decay=0.0)
+        k, _, keep, _ = st.seen(1, None if fr is None else fr[0].tolist())
+        w, b = R.weights(R.f64(q), k, lse[0].cpu().numpy(), 2)
+        got = ix.weights[1].double().cpu().numpy()
+        assert (np.abs(got[:, keep] - w) <= b).all() and not got[:, ~keep].any()
+    dst = P.ShallowIndex(2, *heads, 40, rows)
+    dst.attach_values()
+    wt = torch.rand_like(ix.weights)
+    ix.weights.copy_(wt)
+    ix.evict_into(dst, 20, 9)
+    for l in range(2):
+        for g in (0, 7):
+            pos = R.kept_rows(wt[l, g].cpu().numpy(), st.rows, 20, 9)
+            assert np.array_equal(host(dst.keys[l, g]).view(np.uint16), st.k[l][g, pos])
+            assert np.array_equal(host(dst.values[l, g]).view(np.uint16), st.v[l][g, pos])
+
+
+def test_long_own_text():
+    """Own tokens by the thousands in front of few queries, and a whole long prompt."""
+    import paper_2609_02780_amd as P
+    rng = np.random.default_rng(16)
+    for heads, nq, text in (((8, 2, 64), 3, 9000), ((4, 1, 128), 1500, 0)):
+        st = Stream(rng, heads, [(3, 20)])
+        own = Own(rng, heads, text + nq, room=70)
+        q = bf(rng, heads[0], nq, heads[2], scale=1.5)
+        log("case", heads, nq, text)
+        out, lse = P.HistoryAttention([st.ix], slopes=torch.full((heads[0],), 0.5, device="cuda"))(0, [dev(q)], own=[own.arg])
+        check((out[0], lse[0]), want(st, 0, q, own, slopes=np.full(heads[0], 0.5)))
+
+
+def test_many_listed_frames():
+    """Lists longer than one sorting block, in any order, with repeats, padding and frames out of range."""
+    import paper_2609_02780_amd as P
+    rng = np.random.default_rng(17)
+    st = Stream(rng, (4, 2, 64), [(900, 3), (300, 5)])
+    q = bf(rng, 4, 4, 64)
+    att = P.HistoryAttention([st.ix], slopes=torch.full((4,), 0.01, device="cuda"))
+    for n in (1, 2, 511, 512, 513, 3000, 4096):
+        ids = rng.integers(-5, 1210, n)
+        kinds = (rng.random(n) < 0.3).astype(np.int32)
+        log("listed", n)
+        out, lse = att(0, [dev(q)], frames=torch.from_numpy(ids[None]).cuda(), kinds=torch.from_numpy(kinds[None]).cuda())
+        ref = want(st, 0, q, frames=[int(i) for i, k in zip(ids, kinds) if k == 0], slopes=np.full(4, np.float64(np.float32(0.01))))
+        check((out[0], lse[0]), ref, n)
+
+
 def test_window_and_compaction():
     """Frames that left the detailed window are not seen, before and after compaction
     (bit for bit the same), and weights and values move along."""

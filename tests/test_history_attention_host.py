@@ -51,8 +51,8 @@ class Call:
         self.own = L.OwnTokens(C.cast(self.ok_k, C.c_void_p), C.cast(self.ok_v, C.c_void_p),
                                C.cast(self.n_own, C.c_void_p), C.cast(self.cap, C.c_void_p),
                                C.cast(self.par, C.c_void_p))
-        self.out = (C.c_void_p * S)(*[FAKE] * S)
-        self.lse = (C.c_void_p * S)(*[FAKE] * S)
+        self.out = (C.c_void_p * S)(*[FAKE + 4096 + 256 * s for s in range(S)])
+        self.lse = (C.c_void_p * S)(*[FAKE + 8192 + 256 * s for s in range(S)])
         self.ws, self.ws_bytes, self.decay = FAKE, 0, 1.0     # a workspace of 0 bytes: the last check fails
         for k, v in kw.items():
             setattr(self, k, v)
@@ -162,6 +162,10 @@ def test_attend_refusals(L):
         assert status(lambda c: setattr(c, "ws", None), fn=fn) == L.SS_ERR_WORKSPACE
     assert status(put("out", 0, None)) == inv
     assert status(put("out", 0, FAKE + 4)) == inv
+    assert status(put("out", 0, FAKE)) == inv and "queries" in err(L)
+    for name in ("out", "lse"):
+        assert status(lambda c: getattr(c, name).__setitem__(1, getattr(c, name)[0]), idx=[kv.value] * 2) == inv
+        assert "one output" in err(L)
     for n in (1, 2, -1, (1 << 20) + 1):
         assert status(put("n_own", 0, n)) == inv
     assert status(put("n_own", 0, 0)) == L.SS_ERR_WORKSPACE
@@ -187,6 +191,27 @@ def test_attend_refusals(L):
     c.n_q[0] = 0
     assert c.bytes() == 0
     for h in (kv, plain, other):
+        L.lib().ss_index_destroy(h)
+
+
+def test_workspace_of_every_shape(L):
+    """The planner ends, and asks for whole 256-byte pieces, over the documented sizes."""
+    rng = np.random.default_rng(1)
+    for n_q_heads, n_kv, d in ((1, 1, 64), (16, 1, 128), (16, 16, 64), (28, 4, 128), (8, 8, 128)):
+        h = make(L, n_q_heads=n_q_heads, n_kv_heads=n_kv, head_dim=d)
+        for _ in range(60):
+            S = int(rng.choice([1, 2, 16, 17, 33]))
+            c = Call(L, [h.value] * S)
+            for s in range(S):
+                c.n_q[s] = int(rng.choice([1, 2, 31, 64, 1000, 4096, rng.integers(1, 4097)]))
+                c.n_own[s] = int(rng.choice([0, c.n_q[s], 1 << 20, rng.integers(c.n_q[s], 1 << 20)]))
+                c.cap[s] = 1 << 20
+            if rng.random() < 0.5:
+                c.prm.frames, c.prm.n_listed = FAKE, int(rng.integers(1, 4097))
+            n = c.bytes()
+            assert n >= 256 and n % 256 == 0
+            m = L.lib().ss_attend_accumulate_workspace_bytes(c.idx, S, c.n_q, C.byref(c.prm))
+            assert m >= 256 and m % 256 == 0
         L.lib().ss_index_destroy(h)
 
 
