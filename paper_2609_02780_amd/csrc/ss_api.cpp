@@ -801,12 +801,28 @@ size_t plan_attend(ss::AttendArgs& a, ss::AttendPlan& p, ss::RowsArgs& rows, ss_
     int64_t groups = 0;
     for (int i = 0; i < S; ++i) groups += (visible[i] + 31) / 32 * a.Hk;
     const int64_t turns = std::max<int64_t>(1, (groups + slots * waves - 1) / (slots * waves));
+    int64_t blocks = 0;
     for (int i = 0; i < S; ++i) {
       ss::AttendStream& st = a.st[i];
       st.n_split = (int32_t)std::max<int64_t>(1, ((visible[i] + 31) / 32 + turns * waves - 1) / (turns * waves));
-      st.item0 = p.items;
-      p.items += st.n_split * a.Hk;
+      blocks += st.n_split * a.Hk;
     }
+    // Few keys and many query rows: the query rows are shared out as far as that fills
+    // the round, at least 64 a share (983 tokens of 16 heads over 5,000 rows: 710 us
+    // with one share).
+    int64_t parts = 0;
+    for (int i = 0; i < S; ++i) {
+      ss::AttendStream& st = a.st[i];
+      st.q_split = p.shape == 0 ? 1 : (int32_t)std::max<int64_t>(1, std::min(slots / blocks, (int64_t)a.G * st.n_q / 64));
+      st.item0 = p.items;
+      p.items += st.n_split * a.Hk * st.q_split;
+      st.part0 = parts;
+      if (st.q_split > 1) {
+        parts += st.q_split * a.Hk * visible[i];
+        p.add_rows = std::max(p.add_rows, a.Hk * visible[i]);
+      }
+    }
+    a.part_o = reinterpret_cast<float*>(take((size_t)parts * 4));
     return align256(off);
   }
 
@@ -821,7 +837,7 @@ size_t plan_attend(ss::AttendArgs& a, ss::AttendPlan& p, ss::RowsArgs& rows, ss_
   // token over 1 hour 276 / 281 / 289 / 316, 64 tokens 691 / 706 / 736 / 793; 1,024
   // tokens over 10 minutes (112 column blocks): 224 items 1,593, 336 items 1,996, 1,008
   // items 1,690.
-  const int64_t kItemTiles = tile.keys == 128 ? 2 : 8, kJoinTiles = 8;
+  const int64_t kItemTiles = tile.keys == 128 ? 2 : 4, kJoinTiles = tile.keys == 128 ? 8 : 4;
   int64_t tiles[ss::kAttendStreams], blocks_of[ss::kAttendStreams], longest_tiles = 1, whole = 0;
   for (int i = 0; i < S; ++i) {
     tiles[i] = (visible[i] + tile.keys - 1) / tile.keys + (a.st[i].n_own + tile.keys - 1) / tile.keys;

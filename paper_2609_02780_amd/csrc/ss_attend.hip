@@ -777,8 +777,9 @@ __global__ __launch_bounds__(256) void k_join(AttendArgs a) {
 // query rows of a KV head of exp(s - lse).  S = Q K^T with the keys as columns: a
 // wave keeps 32 keys in registers as the B operand, straight from memory, and
 // walks the query rows, staged in LDS PM at a time; a row's sum then stays in the
-// two lanes that hold it, added in one order, so nothing is atomic.
-// ---------------------------------------------------------------------------
+// two lanes that hold it, added in one order, so nothing is atomic.  Where the keys
+// alone do not fill the card, the query rows are shared out too: each share's sums go
+// to the workspace and k_add adds them in order.
 template <int D, int PM, int NW, bool MAP>
 __global__ __launch_bounds__(64 * NW) void k_accumulate(AttendArgs a, float decay) {
   constexpr int RB = D * 2, CH = D / 8, KST = D / 16;
@@ -791,8 +792,14 @@ __global__ __launch_bounds__(64 * NW) void k_accumulate(AttendArgs a, float deca
   while (s + 1 < a.S && item >= a.st[s + 1].item0) ++s;
   const AttendStream& st = a.st[s];
   item -= st.item0;
+  const int share = item % st.q_split;
+  item /= st.q_split;
   const int split = item % st.n_split, hk = item / st.n_split;
   const int M = a.G * st.n_q;
+  // this share's query rows: whole groups of 32
+  const int M32 = (M + 31) / 32;
+  const int m0 = (int)((int64_t)M32 * share / st.q_split) * 32;
+  const int m1 = min(M, (int)((int64_t)M32 * (share + 1) / st.q_split) * 32);
   const int n_vis = MAP ? __builtin_amdgcn_readfirstlane(*st.n_vis) : st.n_rows;
   const int T = (n_vis + 31) / 32;
   const int t0 = (int)((int64_t)T * split / st.n_split), t1 = (int)((int64_t)T * (split + 1) / st.n_split);
@@ -801,9 +808,9 @@ __global__ __launch_bounds__(64 * NW) void k_accumulate(AttendArgs a, float deca
   float* wh = st.weights + (int64_t)hk * st.w_stride;
   const float* ages = reinterpret_cast<const float*>(reinterpret_cast<const char*>(st.rowmap) + st.age_off);
 
-  for (int p0 = 0; p0 < M; p0 += PM) {
-    const int np = min(PM, M - p0), np32 = (np + 31) & ~31;
-    if (p0 > 0) __syncthreads();
+  for (int p0 = m0; p0 < m1; p0 += PM) {
+    const int np = min(PM, m1 - p0), np32 = (np + 31) & ~31;
+    if (p0 > m0) __syncthreads();
     for (int i = tid; i < np32 * CH; i += 64 * NW) {
       const int r = i / CH, ch = i % CH;
       u32x4 v = {0u, 0u, 0u, 0u};
@@ -817,7 +824,7 @@ __global__ __launch_bounds__(64 * NW) void k_accumulate(AttendArgs a, float deca
       if (MAP && a.slopes) s_slope[r] = r < np ? a.slopes[hk * a.G + (p0 + r) / st.n_q] * kLog2e : 0.0f;
     }
     __syncthreads();
-    const float dk = p0 == 0 ? decay : 1.0f;
+    const float dk = p0 > m0 ? 1.0f : (st.q_split > 1 ? 0.0f : decay);
     for (int t = t0 + wave; t < t1; t += NW) {
       const int j = min(t * 32 + c32, n_vis - 1);
       const int row = MAP ? st.rowmap[j] : j;
@@ -857,10 +864,25 @@ __global__ __launch_bounds__(64 * NW) void k_accumulate(AttendArgs a, float deca
       }
       sum += other_half(sum);
       if (half == 0 && t * 32 + c32 < n_vis) {
-        float* w = wh + row;
+        float* w = st.q_split > 1 ? a.part_o + st.part0 + ((int64_t)share * a.Hk + hk) * n_vis + j : wh + row;
         *w = dk == 0.0f ? sum : fmaf(dk, *w, sum);
       }
     }
+  }
+}
+
+// w[row] = decay w[row] + the shares' sums, in their order.
+__global__ __launch_bounds__(256) void k_add(AttendArgs a, bool map, float decay) {
+  const AttendStream& st = a.st[blockIdx.y];
+  if (st.q_split == 1) return;
+  const int n_vis = map ? *st.n_vis : st.n_rows;
+  const int64_t n = (int64_t)a.Hk * n_vis;
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int j = (int)(i % n_vis);
+    float sum = 0.0f;
+    for (int q = 0; q < st.q_split; ++q) sum += a.part_o[st.part0 + q * n + i];
+    float* w = st.weights + (i / n_vis) * st.w_stride + (map ? st.rowmap[j] : j);
+    *w = decay == 0.0f ? sum : fmaf(decay, *w, sum);
   }
 }
 
@@ -1084,6 +1106,9 @@ hipError_t accumulate_impl(const AttendArgs& a, const AttendPlan& p, float decay
     if (p.map) hipLaunchKernelGGL((k_accumulate<D, 256, 8, true>), dim3(p.items), dim3(512), 0, st, a, decay);
     else hipLaunchKernelGGL((k_accumulate<D, 256, 8, false>), dim3(p.items), dim3(512), 0, st, a, decay);
   }
+  if (p.add_rows > 0)
+    hipLaunchKernelGGL(k_add, dim3((unsigned)std::min<int64_t>(cdiv(p.add_rows, 256), 4096), a.S), dim3(256), 0, st, a, p.map,
+                       decay);
   return hipGetLastError();
 }
 

@@ -301,6 +301,7 @@ struct AttendStream {
   int32_t row0, n_rows;        // the detailed rows in the arena run
   int32_t n_q, n_own, own_cap;
   int32_t n_split, item0;
+  int32_t q_split;             // accumulation: shares of the query rows
 };
 struct CapArgs {               // see cap_scores
   float x;                     // 1 / (cap sqrt(d)); 0: scores are not capped
@@ -321,6 +322,7 @@ struct AttendPlan {
   bool map, listed;
   int join_parts;              // largest n_split of the batch
   int join_rows;               // largest H_q n_q of the batch
+  int64_t add_rows;            // accumulation: largest H_kv x visible rows of a stream with q_split > 1, else 0
 };
 hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t st);
 hipError_t launch_accumulate(const AttendArgs& a, const AttendPlan& p, float decay, hipStream_t st);

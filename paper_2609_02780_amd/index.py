@@ -544,21 +544,24 @@ class HistoryAttention:
         self.softcap, self.slopes = float(softcap), slopes
         self._least = torch.empty(256, dtype=torch.uint8, device=self._device)
         self._handles = L.ptr_array([y.handle.value for y in self.indices])
+        # types and calls looked up once: a small call's time is its host time
+        S = len(self.indices)
+        self._lib, self._ptrs, self._ints = L.lib(), C.c_void_p * S, C.c_int32 * S
 
     def _on_device(self, t, what: str, *at):
         if t.device != self._device:
             raise ValueError(f"{what % at} lives on {t.device}, the indices on {self._device}")
 
     def _params(self, layer: int, frames, kinds):
-        p = L.AttendParams(layer, self.softcap, self.slopes.data_ptr() if self.slopes is not None else None,
-                           None, None, 0)
         if torch.cuda.current_device() != self._device.index:
             raise ValueError(f"the indices live on {self._device}, which is not the current device")
-        S = len(self.indices)
+        p = L.AttendParams(layer, self.softcap, self.slopes.data_ptr() if self.slopes is not None else None,
+                           None, None, 0)
         if frames is None:
             if kinds is not None:
                 raise ValueError("kinds without frames")
             return p
+        S = len(self.indices)
         for t, dt, what in ((frames, torch.int64, "frames"), (kinds, torch.int32, "kinds")):
             if t is None:
                 continue
@@ -577,14 +580,22 @@ class HistoryAttention:
         if len(queries) != S:
             raise ValueError(f"expected queries for {S} streams, got {len(queries)}")
         x = self.indices[0]
-        ptrs, n_q = [], []
+        heads, d = x.n_q_heads, x.head_dim
+        ptrs, n_q = self._ptrs(), self._ints()
         for s, q in enumerate(queries):
             if q.dim() != 3:
-                raise ValueError(f"queries[{s}] must be [{x.n_q_heads}][n_q][{x.head_dim}]")
-            ptrs.append(_check_bf16(q, (x.n_q_heads, q.shape[1], x.head_dim), "queries[%d]", s))
+                raise ValueError(f"queries[{s}] must be [{heads}][n_q][{d}]")
+            n = q.shape[1]
+            ptrs[s] = _check_bf16(q, (heads, n, d), "queries[%d]", s)
             self._on_device(q, "queries[%d]", s)
-            n_q.append(q.shape[1])
-        return L.ptr_array(ptrs), (C.c_int32 * S)(*n_q), n_q
+            n_q[s] = n
+        return ptrs, n_q
+
+    def _workspace(self, need: int) -> torch.Tensor:
+        if need == 0:
+            raise L.SSError(L.SS_ERR_INVALID_ARGUMENT, self._lib.ss_last_error().decode())
+        # the least workspace is not written: calls share it
+        return self._least if need == 256 else torch.empty(need, dtype=torch.uint8, device=self._device)
 
     def __call__(self, layer: int, queries, own=None, tree=None, frames=None, kinds=None, stream=None):
         """``queries[s]``: ``[H_q][n_q][d]`` bfloat16.  ``own``: per stream ``None`` or
@@ -595,15 +606,14 @@ class HistoryAttention:
         ``kinds``: device int64 / int32 ``[n_streams][n_listed]``, the only frames to see
         (as :class:`Retriever` and :func:`assemble_evidence` return them).  Returns
         ``(out, lse)``: per stream bfloat16 ``[H_q][n_q][d]`` and fp32 ``[H_q][n_q]``."""
-        S, x = len(self.indices), self.indices[0]
-        qp, nqa, n_q = self._queries(queries)
+        S, x, lib = len(self.indices), self.indices[0], self._lib
+        qp, n_q = self._queries(queries)
         prm = self._params(layer, frames, kinds)
         ot, used = None, []
         if own is not None:
             if len(own) != S:
                 raise ValueError(f"expected own tokens (or None) for {S} streams")
-            kp, vp = (L._P * S)(), (L._P * S)()
-            no, cap = (C.c_int32 * S)(), (C.c_int32 * S)()
+            kp, vp, no, cap = self._ptrs(), self._ptrs(), self._ints(), self._ints()
             for s, o in enumerate(own):
                 if o is None:
                     continue
@@ -615,11 +625,11 @@ class HistoryAttention:
                 self._on_device(v, "own[%d] values", s)
                 no[s], cap[s] = n, shape[1]
                 used += [k, v]
-            ot = L.OwnTokens(C.cast(kp, L._P), C.cast(vp, L._P), C.cast(no, L._P), C.cast(cap, L._P), None)
+            ot = L.OwnTokens(C.addressof(kp), C.addressof(vp), C.addressof(no), C.addressof(cap), None)
         if tree is not None:
             if ot is None or len(tree) != S:
                 raise ValueError(f"tree needs own tokens and an entry for each of {S} streams")
-            pp = (L._P * S)()
+            pp = self._ptrs()
             for s, t in enumerate(tree):
                 if t is None:
                     continue
@@ -628,19 +638,22 @@ class HistoryAttention:
                 self._on_device(t, "tree[%d]", s)
                 pp[s] = t.data_ptr()
                 used.append(t)
-            ot.parents = C.cast(pp, L._P)
+            ot.parents = C.addressof(pp)
         own_ref = C.byref(ot) if ot is not None else None
-        need = L.lib().ss_attend_workspace_bytes(self._handles, S, nqa, own_ref, C.byref(prm))
-        if need == 0:
-            raise L.SSError(L.SS_ERR_INVALID_ARGUMENT, L.lib().ss_last_error().decode())
-        # the least workspace is not written: calls share it
-        ws = self._least if need == 256 else torch.empty(need, dtype=torch.uint8, device=self._device)
-        out = [torch.empty(q.shape, dtype=torch.bfloat16, device=self._device) for q in queries]
-        lse = [torch.empty(q.shape[:2], dtype=torch.float32, device=self._device) for q in queries]
-        L.check(L.lib().ss_attend(self._handles, S, qp, nqa, own_ref, C.byref(prm), ws.data_ptr(), need,
-                                  _stream_handle(stream), L.ptr_array([t.data_ptr() for t in out]),
-                                  L.ptr_array([t.data_ptr() for t in lse])))
-        _used_on(stream, ws, *out, *lse, *queries, *used, self.slopes, frames, kinds)
+        prm_ref = C.byref(prm)
+        ws = self._workspace(lib.ss_attend_workspace_bytes(self._handles, S, n_q, own_ref, prm_ref))
+        first = queries[0].shape
+        if S > 1 and all(q.shape == first for q in queries):
+            out = list(torch.empty((S, *first), dtype=torch.bfloat16, device=self._device).unbind(0))
+            lse = list(torch.empty((S, *first[:2]), dtype=torch.float32, device=self._device).unbind(0))
+        else:
+            out = [torch.empty(q.shape, dtype=torch.bfloat16, device=self._device) for q in queries]
+            lse = [torch.empty(q.shape[:2], dtype=torch.float32, device=self._device) for q in queries]
+        L.check(lib.ss_attend(self._handles, S, qp, n_q, own_ref, prm_ref, ws.data_ptr(), ws.numel(),
+                              _stream_handle(stream), self._ptrs(*[t.data_ptr() for t in out]),
+                              self._ptrs(*[t.data_ptr() for t in lse])))
+        if stream is not None:
+            _used_on(stream, ws, *out, *lse, *queries, *used, self.slopes, frames, kinds)
         return out, lse
 
     def accumulate(self, layer: int, queries, lse, frames=None, kinds=None, decay: float = 1.0, stream=None) -> None:
@@ -648,22 +661,23 @@ class HistoryAttention:
         indices' :attr:`ShallowIndex.weights`, which are scaled by ``decay`` first (0
         overwrites).  ``lse``: per stream what the attention of the same queries,
         ``frames`` and ``kinds`` returned."""
-        S = len(self.indices)
-        qp, nqa, _ = self._queries(queries)
+        S, lib = len(self.indices), self._lib
+        qp, n_q = self._queries(queries)
         prm = self._params(layer, frames, kinds)
         if len(lse) != S:
             raise ValueError(f"expected lse for {S} streams, got {len(lse)}")
+        lp = self._ptrs()
         for s, (t, q) in enumerate(zip(lse, queries)):
             if t.dtype != torch.float32 or t.shape != q.shape[:2] or not t.is_contiguous():
                 raise ValueError(f"lse[{s}] must be a contiguous fp32 tensor {list(q.shape[:2])}")
             self._on_device(t, "lse[%d]", s)
-        need = L.lib().ss_attend_accumulate_workspace_bytes(self._handles, S, nqa, C.byref(prm))
-        if need == 0:
-            raise L.SSError(L.SS_ERR_INVALID_ARGUMENT, L.lib().ss_last_error().decode())
-        ws = self._least if need == 256 else torch.empty(need, dtype=torch.uint8, device=self._device)
-        L.check(L.lib().ss_attend_accumulate(self._handles, S, qp, nqa, L.ptr_array([t.data_ptr() for t in lse]),
-                                             C.byref(prm), decay, ws.data_ptr(), need, _stream_handle(stream)))
-        _used_on(stream, ws, *queries, *lse, self.slopes, frames, kinds)
+            lp[s] = t.data_ptr()
+        prm_ref = C.byref(prm)
+        ws = self._workspace(lib.ss_attend_accumulate_workspace_bytes(self._handles, S, n_q, prm_ref))
+        L.check(lib.ss_attend_accumulate(self._handles, S, qp, n_q, lp, prm_ref, decay, ws.data_ptr(), ws.numel(),
+                                         _stream_handle(stream)))
+        if stream is not None:
+            _used_on(stream, ws, *queries, *lse, self.slopes, frames, kinds)
 
 
 def set_profile_events(start, stop) -> None:
