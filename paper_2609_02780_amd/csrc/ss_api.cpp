@@ -791,13 +791,23 @@ size_t plan_attend(ss::AttendArgs& a, ss::AttendPlan& p, ss::RowsArgs& rows, ss_
     }
   }
 
+  // Rows that one block alone reads, and that the 256 MB Infinity Cache could not hold
+  // until the next call, are read past the caches: 35 columns over 1 hour 246 -> 236 us,
+  // one token for each of 8 streams (1.7 GB) 290 -> 257; 64 MB in turn are served from it (52
+  // columns over 10 minutes of 49 rows, d 64: 33 us, past it 37).
+  {
+    int64_t bytes = 0;
+    for (int i = 0; i < S; ++i) bytes += visible[i] * a.Hk * p.D * (accumulate ? 2 : 4);
+    a.once = bytes > (int64_t)256 << 20 && m_max <= kAttendTiles[2].columns;
+  }
+
   if (accumulate) {
     // A wave takes 32 keys at a time, every wave the same number of turns.  Few query
-    // rows (bound by reading the keys): many short blocks, which end evenly (16 / 32 / 64
-    // / 128 a CU: 140 / 133 / 132 / 144 us for one token over 1 hour).  More rows: one
-    // round of the two blocks that a CU holds with 256 rows staged in LDS.
+    // rows (bound by reading the keys): several short blocks for each that a CU holds, which
+    // end evenly (8 / 16 / 32 / 64 a CU: 113 / 113 / 114 / 127 us for one token over 1
+    // hour).  More rows: one round of the two blocks that a CU holds with 256 rows staged.
     p.shape = m_max <= 32 ? 0 : 1;
-    const int64_t waves = p.shape == 0 ? 4 : 8, slots = (p.shape == 0 ? 64 : 2) * kCus;
+    const int64_t waves = p.shape == 0 ? 4 : 8, slots = (p.shape == 0 ? 16 : 2) * kCus;
     int64_t groups = 0;
     for (int i = 0; i < S; ++i) groups += (visible[i] + 31) / 32 * a.Hk;
     const int64_t turns = std::max<int64_t>(1, (groups + slots * waves - 1) / (slots * waves));

@@ -66,10 +66,18 @@ __device__ __forceinline__ const void* in_scalar(const void* p) {
   const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
   return reinterpret_cast<const void*>((uint64_t)hi << 32 | lo);
 }
+// ONCE: not kept in the caches.
+template <bool ONCE>
 __device__ __forceinline__ void load_lds16(const void* base, uint32_t off, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)),
-               "v"(off), "s"(in_scalar(base))
-               : "memory");
+  if constexpr (ONCE)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(
+                     __builtin_amdgcn_readfirstlane(lds)),
+                 "v"(off), "s"(in_scalar(base))
+                 : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)),
+                 "v"(off), "s"(in_scalar(base))
+                 : "memory");
 }
 __device__ __forceinline__ void load_lds4(const void* base, uint32_t off, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)),
@@ -345,7 +353,10 @@ __global__ __launch_bounds__(64 * WQ * WK) void k_attend(AttendArgs a) {
   const int i_hi = (i_lo + (c_hi - c_lo) >= st.n_q) ? st.n_q - 1 : i_lo + (c_hi - c_lo);
   const int own_end = st.n_own > 0 ? st.n_own - st.n_q + i_hi + 1 : 0;
   const int Tt = Th + (own_end + BN - 1) / BN;
-  const int t0 = (int)((int64_t)Tt * split / st.n_split), t1 = (int)((int64_t)Tt * (split + 1) / st.n_split);
+  // this item's tiles: split, split + n_split, ...; the items of a KV head, side by side in
+  // time, so read one dense window of it.  t below counts them.
+  constexpr int t0 = 0;
+  const int t1 = split < Tt ? (Tt - split + st.n_split - 1) / st.n_split : 0;
 
   const unsigned char* kh = reinterpret_cast<const unsigned char*>(st.keys + hk * st.head_stride);
   const unsigned char* vh = reinterpret_cast<const unsigned char*>(st.values + hk * st.head_stride);
@@ -361,6 +372,9 @@ __global__ __launch_bounds__(64 * WQ * WK) void k_attend(AttendArgs a) {
   const int n_own = keep(st.n_own), draft0 = keep(st.n_own - st.n_q);   // own tokens before draft0 are seen by every query
   const int32_t* rowmap = keep(st.rowmap);
   const uint32_t age_off = keep(st.age_off);
+  const int n_split = keep(st.n_split);
+  const bool once = keep((int)a.once) != 0;
+  auto tile_of = [&](int t) { return split + t * n_split; };
 
   // this lane's query column (behind the last one: that one again, not written)
   const int c = c_lo + wq * 32 + c32, cc = min(c, M - 1);
@@ -376,7 +390,7 @@ __global__ __launch_bounds__(64 * WQ * WK) void k_attend(AttendArgs a) {
   // ancestors of the drafted tokens of this block's columns, bit e of word w: draft 32 w + e
   uint32_t* anc = reinterpret_cast<uint32_t*>(smem + MERGE_AT + T::META);
   const bool tree = st.parents != nullptr;
-  if (tree && t1 > Th) {
+  if (tree && t1 > 0 && tile_of(t1 - 1) >= Th) {
     int* par = reinterpret_cast<int*>(smem);          // before the ring is used
     for (int i = tid; i < st.n_q; i += 64 * NW) par[i] = st.parents[i];
     const int words = (st.n_q + 31) / 32;
@@ -401,16 +415,17 @@ __global__ __launch_bounds__(64 * WQ * WK) void k_attend(AttendArgs a) {
   auto meta_at = [&](int t, int g) -> uint32_t { return (uint32_t)(MERGE_AT + ((t & 7) * T::NG + g) * 256); };
   auto load_meta = [&](int t) {
     const int g = wave % T::NG;
-    const int j = max(0, min(t * BN + g * 32 + c32, n_vis - 1));
+    const int j = max(0, min(tile_of(t) * BN + g * 32 + c32, n_vis - 1));
     // lanes 0..31 the rows' places, 32..63 their ages
     const uint32_t off = (uint32_t)j * 4u + (half ? age_off : 0u);
     load_lds4(rowmap, off, lds0 + meta_at(t, g));
   };
   auto issue = [&](int t) {
-    const bool hist = t < Th;
+    const int tile = tile_of(t);
+    const bool hist = tile < Th;
     const unsigned char* kb = hist ? kh : ko;
     const unsigned char* vb = hist ? vh : vo;
-    const int n = hist ? n_vis : n_own, j0 = (hist ? t : t - Th) * BN;
+    const int n = hist ? n_vis : n_own, j0 = (hist ? tile : tile - Th) * BN;
     const uint32_t buf = lds0 + (uint32_t)((t - t0) % NS) * 2u * T::KB;
 #pragma unroll
     for (int k = 0; k < NI; ++k) {
@@ -418,8 +433,14 @@ __global__ __launch_bounds__(64 * WQ * WK) void k_attend(AttendArgs a) {
       int j = min(j0 + r, n - 1);
       if (MAP && hist) j = *reinterpret_cast<const int*>(smem + meta_at(t, r >> 5) + (r & 31) * 4);
       const uint32_t row = (uint32_t)j * RB;
-      load_lds16(kb, row + ((pos ^ key_swizzle<D>(r)) << 4), buf + idx * 1024);
-      load_lds16(vb, row + ((pos ^ value_swizzle<D>(r)) << 4), buf + T::KB + idx * 1024);
+      const uint32_t ko_ = row + ((pos ^ key_swizzle<D>(r)) << 4), vo_ = row + ((pos ^ value_swizzle<D>(r)) << 4);
+      if (WQ < 8 && once) {
+        load_lds16<true>(kb, ko_, buf + idx * 1024);
+        load_lds16<true>(vb, vo_, buf + T::KB + idx * 1024);
+      } else {
+        load_lds16<false>(kb, ko_, buf + idx * 1024);
+        load_lds16<false>(vb, vo_, buf + T::KB + idx * 1024);
+      }
     }
     if (MAP) load_meta(t + 2);
   };
@@ -515,8 +536,9 @@ __global__ __launch_bounds__(64 * WQ * WK) void k_attend(AttendArgs a) {
     }
   };
   auto softmax = [&](int t) {
-    const bool hist = t < Th;
-    const int n = hist ? n_vis : own_end, j0 = (hist ? t : t - Th) * BN;
+    const int tile = tile_of(t);
+    const bool hist = tile < Th;
+    const int n = hist ? n_vis : own_end, j0 = (hist ? tile : tile - Th) * BN;
     float sv[SUB * 16];
 #pragma unroll
     for (int i = 0; i < SUB * 16; ++i) sv[i] = S[i >> 4][i & 15];
@@ -830,6 +852,11 @@ __global__ __launch_bounds__(64 * NW) void k_accumulate(AttendArgs a, float deca
   __shared__ __align__(1024) unsigned char sq[PM * RB];
   __shared__ __align__(16) float s_lse[PM];
   __shared__ __align__(16) float s_slope[MAP ? PM : 4];
+  // Few query rows: the pass is bound by reading the keys, which then come through LDS in
+  // whole lines, two groups of 32 a wave, one under way while the other is multiplied.
+  constexpr bool STAGED = !MAP && NW == 4;
+  constexpr int NI = 32 * RB / 1024, RPI = 64 / CH;
+  __shared__ __align__(1024) unsigned char sk[STAGED ? NW * 2 * 32 * RB : 16];
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, c32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int item = blockIdx.x, s = 0;
@@ -845,9 +872,9 @@ __global__ __launch_bounds__(64 * NW) void k_accumulate(AttendArgs a, float deca
   const int m0 = (int)((int64_t)M32 * share / st.q_split) * 32;
   const int m1 = min(M, (int)((int64_t)M32 * (share + 1) / st.q_split) * 32);
   const int n_vis = MAP ? __builtin_amdgcn_readfirstlane(*st.n_vis) : st.n_rows;
-  const int T = (n_vis + 31) / 32;
-  const int t0 = (int)((int64_t)T * split / st.n_split), t1 = (int)((int64_t)T * (split + 1) / st.n_split);
-  if (t0 >= t1) return;                                  // the whole block
+  // groups of 32 keys: NW at a time, the items of a KV head in turn (one dense window)
+  const int T = (n_vis + 31) / 32, step = st.n_split * NW;
+  if (split * NW >= T) return;                           // the whole block
   const uint16_t* kh = st.keys + hk * st.head_stride;
   float* wh = st.weights + (int64_t)hk * st.w_stride;
   const float* ages = reinterpret_cast<const float*>(reinterpret_cast<const char*>(st.rowmap) + st.age_off);
@@ -869,14 +896,40 @@ __global__ __launch_bounds__(64 * NW) void k_accumulate(AttendArgs a, float deca
     }
     __syncthreads();
     const float dk = p0 > m0 ? 1.0f : (st.q_split > 1 ? 0.0f : decay);
-    for (int t = t0 + wave; t < t1; t += NW) {
+    const uint32_t ring = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(SS_LDS unsigned char*)sk) + wave * 2 * 32 * RB;
+    auto issue = [&](int t, int b) {
+#pragma unroll
+      for (int k = 0; k < NI; ++k) {
+        const int r = k * RPI + lane / CH, jr = min(t * 32 + r, n_vis - 1);
+        const uint32_t at = (uint32_t)jr * RB + ((lane % CH ^ key_swizzle<D>(r)) << 4), to = ring + b * 32 * RB + k * 1024;
+        if (a.once) load_lds16<true>(kh, at, to);
+        else load_lds16<false>(kh, at, to);
+      }
+    };
+    int b = 0;
+    if (STAGED && split * NW + wave < T) issue(split * NW + wave, 0);
+    for (int t = split * NW + wave; t < T; t += step, b ^= 1) {
       const int j = min(t * 32 + c32, n_vis - 1);
       const int row = MAP ? st.rowmap[j] : j;
       const float age = MAP ? ages[j] : 0.0f;
       u32x4 kf[KST];
+      if constexpr (STAGED) {
+        if (t + step < T) {
+          wait_loads<63, false>();            // the other buffer has been read
+          issue(t + step, b ^ 1);
+          wait_loads<NI, false>();
+        } else {
+          wait_loads<0, false>();
+        }
 #pragma unroll
-      for (int i = 0; i < KST; ++i)
-        kf[i] = *reinterpret_cast<const u32x4*>(kh + (int64_t)row * D + 16 * i + 8 * half);
+        for (int i = 0; i < KST; ++i)
+          kf[i] = *(const SS_LDS u32x4*)(uintptr_t)(ring + b * 32 * RB + c32 * RB +
+                                                    (((2 * i + half) ^ key_swizzle<D>(c32)) << 4));
+      } else {
+#pragma unroll
+        for (int i = 0; i < KST; ++i)
+          kf[i] = *reinterpret_cast<const u32x4*>(kh + (int64_t)row * D + 16 * i + 8 * half);
+      }
       float sum = 0.0f;
       for (int q0 = 0; q0 < np32; q0 += 32) {
         const int r = q0 + c32;
@@ -968,7 +1021,8 @@ __global__ __launch_bounds__(256) void k_store_values(StoreValuesArgs a) {
 // k_evict: a wave takes one (frame, layer, KV head).  The cut is the largest key
 // u with at least `keep` rows at or above it, found bit by bit over the weights'
 // order-preserving 32-bit image; rows above it stay, and of the rows at it the
-// first ones.  The kept rows are then copied, 16 bytes a lane.
+// first ones.  The kept rows are then copied, 16 bytes a lane, past the caches (1 hour to
+// 32 rows a frame: 388 us, 5.3 TB/s read and written; through the caches 417 to 430).
 // ---------------------------------------------------------------------------
 __global__ __launch_bounds__(1024) void k_evict_offsets(EvictArgs a) {
   __shared__ int64_t wsum[16];
@@ -1096,15 +1150,15 @@ __global__ __launch_bounds__(256) void k_evict(EvictArgs a) {
       for (int y = 0; y < 4; ++y)
         if (x + y * RPW < c) {
           const int64_t r = s0 + s_row[wave][x + y * RPW];
-          k[y] = *reinterpret_cast<const u32x4*>(a.src.keys + r * D + ch * 8);
-          v[y] = *reinterpret_cast<const u32x4*>(a.src_values + r * D + ch * 8);
+          k[y] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(a.src.keys + r * D + ch * 8));
+          v[y] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(a.src_values + r * D + ch * 8));
         }
 #pragma unroll
       for (int y = 0; y < 4; ++y)
         if (x + y * RPW < c) {
           const int64_t r = d0 + out + x + y * RPW;
-          *reinterpret_cast<u32x4*>(a.dst.keys + r * D + ch * 8) = k[y];
-          *reinterpret_cast<u32x4*>(a.dst_values + r * D + ch * 8) = v[y];
+          __builtin_nontemporal_store(k[y], reinterpret_cast<u32x4*>(a.dst.keys + r * D + ch * 8));
+          __builtin_nontemporal_store(v[y], reinterpret_cast<u32x4*>(a.dst_values + r * D + ch * 8));
         }
     }
     __builtin_amdgcn_wave_barrier();

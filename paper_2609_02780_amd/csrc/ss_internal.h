@@ -310,6 +310,7 @@ struct CapArgs {               // see cap_scores
 };
 struct AttendArgs {
   int S, Hk, G;
+  bool once;                   // the rows are read past the caches
   float c1;                    // log2(e) / sqrt(d)
   CapArgs cap;
   const float* slopes;         // [H_q] or null
