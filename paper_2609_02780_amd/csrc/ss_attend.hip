@@ -110,17 +110,26 @@ __device__ __forceinline__ float tanh_any(float x) {
 // are below 0.35 (off by 2^-24.9 at most), of degree 5 below 0.6 (2^-28.6).  Scores far
 // below their cap are the usual case.
 template <int N>
-__device__ __forceinline__ void cap_scores(float (&v)[N], const CapArgs& a) {
+__device__ __forceinline__ float top_of(const float (&v)[N]) {
   float top = 0.0f;
 #pragma unroll
   for (int i = 0; i < N; ++i) top = fmaxf(top, fabsf(v[i]));
-  if (!__any(!(top < a.near_limit))) {
+  return top;
+}
+template <int N>
+__device__ __forceinline__ bool near_cap(const float (&v)[N], const CapArgs& a) {
+  return !__any(!(top_of(v) < a.near_limit));
+}
+__device__ __forceinline__ float near_factor(float v, const CapArgs& a) {
+  const float y = v * v;
+  return fmaf(y, fmaf(y, fmaf(y, a.near_fit[3], a.near_fit[2]), a.near_fit[1]), a.near_fit[0]);
+}
+template <int N>
+__device__ __forceinline__ void cap_scores(float (&v)[N], const CapArgs& a) {
+  if (near_cap(v, a)) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float y = v[i] * v[i];
-      v[i] *= fmaf(y, fmaf(y, fmaf(y, a.near_fit[3], a.near_fit[2]), a.near_fit[1]), a.near_fit[0]);
-    }
-  } else if (!__any(!(top * a.x < 0.6f))) {
+    for (int i = 0; i < N; ++i) v[i] *= near_factor(v[i], a);
+  } else if (!__any(!(top_of(v) * a.x < 0.6f))) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const float z = v[i] * a.x, y = z * z;
@@ -942,21 +951,27 @@ __global__ __launch_bounds__(64 * NW) void k_accumulate(AttendArgs a, float deca
         float sv[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) sv[i] = S[i];
-        float cs = a.c1;
-        if (a.cap.x > 0.0f) {
-          cap_scores(sv, a.cap);
-          cs = 1.0f;
-        }
+        // adds exp of sv * factor(i) - lse (and the bias)
+        auto add = [&](auto factor) {
 #pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4) {
-          f32x4 z = *reinterpret_cast<const f32x4*>(&s_lse[q0 + 8 * q4 + 4 * half]);
-          if (MAP && a.slopes) {
-            const f32x4 sl = *reinterpret_cast<const f32x4*>(&s_slope[q0 + 8 * q4 + 4 * half]);
+          for (int q4 = 0; q4 < 4; ++q4) {
+            f32x4 z = *reinterpret_cast<const f32x4*>(&s_lse[q0 + 8 * q4 + 4 * half]);
+            if (MAP && a.slopes) {
+              const f32x4 sl = *reinterpret_cast<const f32x4*>(&s_slope[q0 + 8 * q4 + 4 * half]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) z[e] = fmaf(sl[e], age, z[e]);
+              for (int e = 0; e < 4; ++e) z[e] = fmaf(sl[e], age, z[e]);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum += exp2_fast(fmaf(sv[q4 * 4 + e], factor(q4 * 4 + e), -z[e]));
           }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) sum += exp2_fast(fmaf(sv[q4 * 4 + e], cs, -z[e]));
+        };
+        if (a.cap.x == 0.0f) {
+          add([&](int) { return a.c1; });
+        } else if (near_cap(sv, a.cap)) {
+          add([&](int i) { return near_factor(sv[i], a.cap); });    // its last product is the fma's
+        } else {
+          cap_scores(sv, a.cap);
+          add([](int) { return 1.0f; });
         }
       }
       sum += other_half(sum);
