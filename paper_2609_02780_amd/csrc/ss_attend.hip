@@ -304,12 +304,19 @@ __device__ __forceinline__ int value_swizzle(int r) {
 
 // k_attend<D, WQ, WK, BN, NS, MAP>: one item = (stream, KV head, block of 32 WQ
 // query columns, share of the key tiles).  WQ waves along the columns x WK along
-// the keys; a tile of BN keys and values is staged in LDS, NS tiles in flight.
+// the keys; a tile of BN keys and values is staged in LDS, up to NS tiles at a time.
 // The M = G n_q query rows of a KV head are one run of memory, so column c is
 // token c % n_q of head c / n_q.  The tiles of a stream are those of its visible
 // rows and then those of the question's own tokens.
 // MAP: rows come through rowmap, with a bias by age; without, row j is row j.
-// ---------------------------------------------------------------------------
+//
+// What bounds it.  Few columns: reading keys and values (one token over 705,600 rows of 4
+// KV heads, d 128: 246 us, 5.9 TB/s; WQ = 1: each wave loads what it reads, no barriers).
+// Many columns: the matrix unit and the power it may draw (1,024 tokens of 28 heads over
+// 117,600 rows: 1.44 ms, 1.2 PFLOP/s; a block's tile of 64 keys x 256 columns takes
+// 3,200 clocks, 2,048 of them matrix work, at the 1.5 to 1.8 GHz the card then holds).
+// 32 columns a wave keep O^T, the queries, a tile's scores and two steps of LDS reads in
+// 200 registers, so that two waves fit a SIMD and can take turns.
 template <int D, int WQ, int WK, int BN, int NS, bool MAP>
 struct AttendShape {
   static constexpr int NW = WQ * WK, BM = 32 * WQ, RB = D * 2, CH = D / 8, RPI = 64 / CH;

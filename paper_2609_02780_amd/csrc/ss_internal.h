@@ -1,5 +1,5 @@
 // Internal declarations shared by the C-ABI layer (ss_api.cpp) and the gfx950
-// kernels (ss_kernels.hip).  Not part of the public interface.
+// kernels (ss_kernels.hip, ss_attend.hip).  Not part of the public interface.
 #pragma once
 
 #include <hip/hip_runtime.h>
