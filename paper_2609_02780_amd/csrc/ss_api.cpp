@@ -1244,14 +1244,15 @@ ss_status ss_index_compact(ss_index* idx, void* stream) {
     ss::CompactArgs a{};
     const ss_index_desc& d = idx->desc;
     a.dev = idx->dev;
-    a.values = idx->values;
-    a.weights = idx->weights;
     a.L = d.n_layers; a.Hk = d.n_kv_heads; a.D = d.head_dim; a.max_rows = d.max_rows;
     a.row_shift = rs;
     a.keep_rows = idx->n_rows - rs;
     a.frame_shift = fs;
     a.keep_frames = idx->n_frames - idx->first_detail;
-    const hipError_t e = ss::launch_compact(a, static_cast<hipStream_t>(stream));
+    hipError_t e = ss::launch_compact(a, static_cast<hipStream_t>(stream));
+    if (e == hipSuccess && idx->values)
+      e = ss::launch_move_values({a.L * a.Hk, a.D, a.max_rows, a.row_shift, a.keep_rows, idx->values, idx->weights},
+                                 static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return fail(SS_ERR_DEVICE, "compaction launch failed: %s", hipGetErrorString(e));
     idx->off.swap(off);
     idx->frame_base = idx->first_detail;

@@ -1037,6 +1037,29 @@ __global__ __launch_bounds__(256) void k_store_values(StoreValuesArgs a) {
   for (int64_t i = i0; i < a.rows; i += step) w[i] = 0.0f;
 }
 
+// k_move_values: values and weights of the rows that stay move to the start of their run,
+// in place.  Pieces o, o + shift, o + 2 shift, ... each take the place of the one before;
+// one thread walks such a chain in order, four reads ahead, and no two threads meet.
+template <class U>
+__device__ __forceinline__ void move_down(U* run, int64_t shift, int64_t keep) {
+  const int64_t step = (int64_t)gridDim.x * 256, len = min(shift, keep);
+  for (int64_t o = blockIdx.x * 256ll + threadIdx.x; o < len; o += step)
+    for (int64_t k = o; k < keep; k += 4 * shift) {
+      U x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (k + i * shift < keep) x[i] = run[k + (i + 1) * shift];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (k + i * shift < keep) run[k + i * shift] = x[i];
+    }
+}
+__global__ __launch_bounds__(256) void k_move_values(MoveValuesArgs a) {
+  const int64_t row0 = blockIdx.y * a.max_rows, unit = a.D / 8;       // 16-byte pieces of a row
+  move_down(reinterpret_cast<u32x4*>(a.values + row0 * a.D), a.row_shift * unit, a.keep_rows * unit);
+  move_down(a.weights + row0, a.row_shift, a.keep_rows);
+}
+
 // ---------------------------------------------------------------------------
 // Eviction.  k_evict_offsets: the row offsets of the thinned frames, one block (frames
 // of one size need none: their offsets are products).
@@ -1262,6 +1285,14 @@ hipError_t launch_store_values(const StoreValuesArgs& a, hipStream_t st) {
   const int64_t pieces = a.rows * (a.D / 8);
   const int blocks = (int)std::max<int64_t>(1, std::min<int64_t>(cdiv(pieces, 1024), 1024));
   hipLaunchKernelGGL(k_store_values, dim3(blocks, a.L * a.Hk), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_move_values(const MoveValuesArgs& a, hipStream_t st) {
+  const int64_t pieces = std::min(a.row_shift, a.keep_rows) * (a.D / 8);
+  if (pieces <= 0) return hipSuccess;
+  const int blocks = (int)std::min<int64_t>(cdiv(pieces, 256), 4096);
+  hipLaunchKernelGGL(k_move_values, dim3(blocks, a.lh), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 

@@ -239,8 +239,6 @@ hipError_t launch_evidence(const EvidenceArgs& a, hipStream_t st);
 // row_shift.
 struct CompactArgs {
   IndexDev dev;
-  uint16_t* values;      // null without a value cache
-  float* weights;
   int L, Hk, D;
   int64_t max_rows;
   int64_t row_shift, keep_rows;
@@ -264,6 +262,16 @@ struct StoreValuesArgs {
   float* weights;                    // [L][H_kv][max_rows], zeroed for the new rows
 };
 hipError_t launch_store_values(const StoreValuesArgs& a, hipStream_t st);
+
+// Compaction of the value cache: rows [row_shift, row_shift + keep_rows) of every (layer, KV
+// head) go to [0, keep_rows).
+struct MoveValuesArgs {
+  int lh, D;                         // (layer, KV head) runs
+  int64_t max_rows, row_shift, keep_rows;
+  uint16_t* values;
+  float* weights;
+};
+hipError_t launch_move_values(const MoveValuesArgs& a, hipStream_t st);
 
 // The rows that a call sees, laid out in the workspace: see k_rows.
 struct RowsStream {

@@ -4984,7 +4984,7 @@ struct MoveSeg {
   int block0;                    // first block of this array
   uint32_t sub;                  // subtracted from each 4-byte unit (row offsets are rebased as they move)
 };
-constexpr int kMoveSegs = 7, kMoveIt = 4;
+constexpr int kMoveSegs = 5, kMoveIt = 4;
 struct MoveArgs {
   int n, n16;                    // arrays; the first n16 move in 16-byte units, the others in 4-byte ones
   MoveSeg s[kMoveSegs];
@@ -5664,12 +5664,10 @@ hipError_t launch_compact(const CompactArgs& a, hipStream_t st) {
   };
   const int lg = a.L * a.Hk;
   add(a.dev.keys, a.max_rows * a.D / 8, lg, a.D / 8, a.row_shift, a.keep_rows, 0u);   // 16-byte units of bf16 rows
-  if (a.values) add(a.values, a.max_rows * a.D / 8, lg, a.D / 8, a.row_shift, a.keep_rows, 0u);
   add(a.dev.desc, 0, 1, (int64_t)a.Hk * a.D / 4, a.frame_shift, a.keep_frames, 0u);
   add(a.dev.pooled, 0, 1, (int64_t)a.L * a.Hk * a.D / 4, a.frame_shift, a.keep_frames, 0u);
   m.n16 = m.n;
   add(a.dev.counts, a.max_rows, lg, 1, a.row_shift, a.keep_rows, 0u);
-  if (a.weights) add(a.weights, a.max_rows, lg, 1, a.row_shift, a.keep_rows, 0u);
   add(a.dev.frame_off, 0, 1, 1, a.frame_shift, a.keep_frames + 1, (uint32_t)a.row_shift);
   if (blocks > 0) hipLaunchKernelGGL(k_move, dim3(blocks), dim3(256), 0, st, m);
   return hipGetLastError();

@@ -586,6 +586,7 @@ class HistoryAttention:
             if q.dim() != 3:
                 raise ValueError(f"queries[{s}] must be [{heads}][n_q][{d}]")
             n = q.shape[1]
+            self.indices[s].handle          # raises when the index was closed
             ptrs[s] = _check_bf16(q, (heads, n, d), "queries[%d]", s)
             self._on_device(q, "queries[%d]", s)
             n_q[s] = n

@@ -342,6 +342,25 @@ def test_window_and_compaction():
     assert not st.ix.weights[:, :, -24:].any()
 
 
+@pytest.mark.parametrize("gone", [1, 3, 15, 29, 30])
+def test_compaction_moves_values_and_weights(gone):
+    """Kept parts longer and shorter than the dropped one, also none at all."""
+    import paper_2609_02780_amd as P
+    rng = np.random.default_rng(gone)
+    st = Stream(rng, (8, 2, 128), [(30, 7)], L=2)
+    w0 = torch.rand_like(st.ix.weights)
+    st.ix.weights.copy_(w0)
+    P.LongClusters(st.ix, 7, 30, 0.5).absorb(gone, gone)
+    st.ix.compact()
+    assert st.ix.n_rows == (30 - gone) * 7 and st.ix.window() == (gone, gone)
+    assert torch.equal(st.ix.weights, w0[:, :, gone * 7:])
+    assert np.array_equal(host(st.ix.values), np.stack(st.v)[:, :, gone * 7:].view(np.int16))
+    assert np.array_equal(host(st.ix.keys), np.stack(st.k)[:, :, gone * 7:].view(np.int16))
+    q = bf(rng, 8, 2, 128)
+    out, lse = P.HistoryAttention([st.ix])(1, [dev(q)])
+    check((out[0], lse[0]), want(st, 1, q, first=gone))
+
+
 @pytest.mark.parametrize("heads", [(4, 2, 64), (28, 4, 128), (16, 1, 128), (3, 1, 64)], ids=str)
 @pytest.mark.parametrize("nq,runs", [(1, [(1, 1)]), (1, [(50, 49)]), (3, [(9, 33), (5, 128)]), (40, [(20, 31)]),
                                      (150, [(3, 65)])], ids=str)
@@ -535,6 +554,62 @@ def test_streams_and_graphs():
         for (g, r, f), e in zip(graphs, wants):
             assert torch.equal(r[0][0], e[0]) and torch.equal(r[1][0], e[1]), rep
         assert torch.equal(st.ix.weights, wants[1][2]), rep
+
+
+def test_two_calls_at_once():
+    """Calls that run at the same time on two streams, and two graphs replayed together,
+    share nothing."""
+    import paper_2609_02780_amd as P
+    rng = np.random.default_rng(55)
+    st = Stream(rng, (28, 4, 128), [(300, 49)])
+    att = P.HistoryAttention([st.ix], slopes=torch.full((28,), 0.01, device="cuda"))
+    qs = [dev(bf(rng, 28, n, 128)) for n in (1, 40)]
+    wants = [att(0, [q]) for q in qs]
+    torch.cuda.synchronize()
+    sides = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for rep in range(5):
+        got = []
+        for side, q in zip(sides, qs):
+            with torch.cuda.stream(side):
+                got.append([att(0, [q]) for _ in range(4)])
+        torch.cuda.synchronize()
+        for g, w in zip(got, wants):
+            for x in g:
+                assert torch.equal(x[0][0], w[0][0]) and torch.equal(x[1][0], w[1][0]), rep
+    graphs = []
+    for q in qs:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            r = att(0, [q])
+        graphs.append((g, r))
+    for rep in range(4):
+        for side, (g, r) in zip(sides, graphs):
+            with torch.cuda.stream(side):
+                g.replay()
+        torch.cuda.synchronize()
+        for (g, r), w in zip(graphs, wants):
+            assert torch.equal(r[0][0], w[0][0]) and torch.equal(r[1][0], w[1][0]), rep
+            r[0][0].zero_()
+
+
+def test_longest_prompt():
+    """4,096 queries, the most of a call, each seeing another number of own tokens."""
+    import paper_2609_02780_amd as P
+    rng = np.random.default_rng(56)
+    heads = (2, 1, 64)
+    st = Stream(rng, heads, [(2, 9)])
+    own, q = Own(rng, heads, 4096), bf(rng, 2, 4096, 64, scale=1.5)
+    out, lse = P.HistoryAttention([st.ix])(0, [dev(q)], own=[own.arg])
+    check((out[0], lse[0]), want(st, 0, q, own))
+
+
+def test_closed_index():
+    import paper_2609_02780_amd as P
+    st = Stream(np.random.default_rng(57), (4, 2, 64), [(2, 8)])
+    att = P.HistoryAttention([st.ix])
+    st.ix.close()
+    with pytest.raises(RuntimeError):
+        att(0, [dev(bf(np.random.default_rng(1), 4, 1, 64))])
 
 
 def test_together():
