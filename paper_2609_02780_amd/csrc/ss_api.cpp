@@ -839,14 +839,16 @@ size_t plan_attend(ss::AttendArgs& a, ss::AttendPlan& p, ss::RowsArgs& rows, ss_
   p.shape = 0;
   while (p.shape < 3 && kAttendTiles[p.shape].columns < m_max) ++p.shape;
   const AttendTile tile = kAttendTiles[p.shape];
-  // Shares of the key axis.  A CU holds one block, so items run in rounds of kCus, and
-  // a round costs its longest item: `per` tiles and what starting and ending an item
-  // costs (kItemTiles).  For each number of rounds the smallest `per` that fits it is
-  // found, and the cheapest number taken, or no sharing at all where that saves the
-  // second launch (kJoinTiles).  Measured, us, one / two / four / eight rounds: one
-  // token over 1 hour 276 / 281 / 289 / 316, 64 tokens 691 / 706 / 736 / 793; 1,024
-  // tokens over 10 minutes (112 column blocks): 224 items 1,593, 336 items 1,996, 1,008
-  // items 1,690.
+  // Shares of the key axis.  A CU holds one block (by LDS; at d = 64 two, which pays except for
+  // the widest tiling: 52 columns over 1 hour 149 -> 122 us, 400 over 10 minutes 90 ->
+  // 103), so items run in rounds of `slots`, and a round costs its longest item: `per`
+  // tiles and what starting and ending an item costs (kItemTiles).  For each number of
+  // rounds the smallest `per` that fits it is found, and the cheapest number taken, or no
+  // sharing at all where that saves the second launch (kJoinTiles).  Measured, us, one /
+  // two / four / eight rounds: one token over 1 hour 276 / 281 / 289 / 316, 64 tokens 691
+  // / 706 / 736 / 793; 1,024 tokens over 10 minutes (112 column blocks): 224 items 1,593,
+  // 336 items 1,996, 1,008 items 1,690.
+  const int64_t slots = p.D == 64 && p.shape < 3 ? 2 * kCus : kCus;
   const int64_t kItemTiles = tile.keys == 128 ? 2 : 4, kJoinTiles = tile.keys == 128 ? 8 : 4;
   int64_t tiles[ss::kAttendStreams], blocks_of[ss::kAttendStreams], longest_tiles = 1, whole = 0;
   for (int i = 0; i < S; ++i) {
@@ -860,13 +862,13 @@ size_t plan_attend(ss::AttendArgs& a, ss::AttendPlan& p, ss::RowsArgs& rows, ss_
     for (int i = 0; i < S; ++i) n += std::max<int64_t>(1, (tiles[i] + per - 1) / per) * blocks_of[i];
     return n;
   };
-  const int64_t rounds_whole = (whole + kCus - 1) / kCus;
+  const int64_t rounds_whole = (whole + slots - 1) / slots;
   int64_t per = longest_tiles, cost = rounds_whole * (longest_tiles + kItemTiles);
   for (int64_t r = rounds_whole; r <= rounds_whole + 7; ++r) {
-    int64_t lo = 1, hi = longest_tiles;             // items_at(hi) = whole <= r kCus
+    int64_t lo = 1, hi = longest_tiles;             // items_at(hi) = whole <= r slots
     while (lo < hi) {
       const int64_t mid = (lo + hi) / 2;
-      if (items_at(mid) <= r * kCus) hi = mid;
+      if (items_at(mid) <= r * slots) hi = mid;
       else lo = mid + 1;
     }
     const int64_t c = r * (lo + kItemTiles) + kJoinTiles;
