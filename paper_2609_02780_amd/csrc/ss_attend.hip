@@ -144,8 +144,8 @@ __device__ __forceinline__ void cap_scores(float (&v)[N], const CapArgs& a) {
 // ---------------------------------------------------------------------------
 // k_rows: the rows that a call sees, when they are not simply the detailed ones.
 // With a list of frames: the listed frames of the detailed window, each once, in
-// temporal order, their rows laid end to end; without (a bias needs the rows'
-// ages): every detailed row.  rowmap[j] is the j-th row's place in the arena run,
+// temporal order, their rows laid end to end; without (a bias over frames of several
+// sizes needs the rows' ages): every detailed row.  rowmap[j] is the j-th row's place in the arena run,
 // age[j] the frames from it to the end of the stream.
 // Each block of a list orders it anew (up to 512 entries by comparing all pairs, up to
 // 4,096 by sorting in LDS) and writes its share of the frames, so one launch does; a
@@ -308,7 +308,8 @@ __device__ __forceinline__ int value_swizzle(int r) {
 // The M = G n_q query rows of a KV head are one run of memory, so column c is
 // token c % n_q of head c / n_q.  The tiles of a stream are those of its visible
 // rows and then those of the question's own tokens.
-// MAP: rows come through rowmap, with a bias by age; without, row j is row j.
+// MAP: rows come through rowmap, with their ages; without, row j is row j, and a bias
+// takes its age from the frames' one size.
 //
 // What bounds it.  Few columns: reading keys and values (one token over 705,600 rows of 4
 // KV heads, d 128: 246 us, 5.9 TB/s; WQ = 1: each wave loads what it reads, no barriers).
@@ -389,13 +390,14 @@ __global__ __launch_bounds__(64 * WQ * WK) void k_attend(AttendArgs a) {
   const int32_t* rowmap = keep(st.rowmap);
   const uint32_t age_off = keep(st.age_off);
   const int n_split = keep(st.n_split);
+  const int rpf = keep(st.rpf), age0 = keep(st.age0);
   const bool once = keep((int)a.once) != 0;
   auto tile_of = [&](int t) { return split + t * n_split; };
 
   // this lane's query column (behind the last one: that one again, not written)
   const int c = c_lo + wq * 32 + c32, cc = min(c, M - 1);
   const int qi = cc % st.n_q;
-  const float slope2 = (MAP && a.slopes) ? a.slopes[hk * a.G + cc / st.n_q] * kLog2e : 0.0f;
+  const float slope2 = a.slopes ? a.slopes[hk * a.G + cc / st.n_q] * kLog2e : 0.0f;
   u32x4 qf[KST];
   {
     const uint16_t* q = st.q + ((int64_t)hk * M + cc) * D + 8 * half;
@@ -573,6 +575,21 @@ __global__ __launch_bounds__(64 * WQ * WK) void k_attend(AttendArgs a) {
           const f32x4 ag = hist ? *reinterpret_cast<const f32x4*>(age + 8 * q4 + 4 * half) : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int e = 0; e < 4; ++e) sv[u * 16 + q4 * 4 + e] = fmaf(-slope2, ag[e], sv[u * 16 + q4 * 4 + e] * cs);
+        }
+      }
+      cs = 1.0f;
+    } else if (!MAP && WQ < 8 && a.slopes) {      // (the widest tiling takes the map: its loop is 1.3% shorter for it)
+      // frames of rpf rows: a group of 32 keys starts at row `rem` of its frame
+      const float inv = 1.0f / (float)rpf;
+#pragma unroll
+      for (int u = 0; u < SUB; ++u) {
+        const int jb = j0 + (wk + u * WK) * 32, f0 = jb / rpf, rem = jb - f0 * rpf + 4 * half;
+        const float b0 = hist ? -slope2 * (float)(age0 - f0) : 0.0f, step = hist ? slope2 : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int x = rem + 8 * (i >> 2) + (i & 3);          // below rpf + 32
+          const float on = rpf >= 32 ? (x >= rpf ? step : 0.0f) : step * floorf(((float)x + 0.5f) * inv);
+          sv[u * 16 + i] = fmaf(sv[u * 16 + i], cs, b0) + on;
         }
       }
       cs = 1.0f;
@@ -867,7 +884,7 @@ __global__ __launch_bounds__(64 * NW) void k_accumulate(AttendArgs a, float deca
   constexpr int RB = D * 2, CH = D / 8, KST = D / 16;
   __shared__ __align__(1024) unsigned char sq[PM * RB];
   __shared__ __align__(16) float s_lse[PM];
-  __shared__ __align__(16) float s_slope[MAP ? PM : 4];
+  __shared__ __align__(16) float s_slope[PM];
   // Few query rows: the pass is bound by reading the keys, which then come through LDS in
   // whole lines, two groups of 32 a wave, one under way while the other is multiplied.
   constexpr bool STAGED = !MAP && NW == 4;
@@ -908,7 +925,7 @@ __global__ __launch_bounds__(64 * NW) void k_accumulate(AttendArgs a, float deca
       // a row that saw nothing (-inf) and padding give nothing
       float x = r < np ? st.lse[(int64_t)hk * M + p0 + r] * kLog2e : neg_inf();
       s_lse[r] = x == neg_inf() ? -neg_inf() : x;
-      if (MAP && a.slopes) s_slope[r] = r < np ? a.slopes[hk * a.G + (p0 + r) / st.n_q] * kLog2e : 0.0f;
+      if (a.slopes) s_slope[r] = r < np ? a.slopes[hk * a.G + (p0 + r) / st.n_q] * kLog2e : 0.0f;
     }
     __syncthreads();
     const float dk = p0 > m0 ? 1.0f : (st.q_split > 1 ? 0.0f : decay);
@@ -927,7 +944,7 @@ __global__ __launch_bounds__(64 * NW) void k_accumulate(AttendArgs a, float deca
     for (int t = split * NW + wave; t < T; t += step, b ^= 1) {
       const int j = min(t * 32 + c32, n_vis - 1);
       const int row = MAP ? st.rowmap[j] : j;
-      const float age = MAP ? ages[j] : 0.0f;
+      const float age = !a.slopes ? 0.0f : MAP ? ages[j] : (float)(st.age0 - j / st.rpf);
       u32x4 kf[KST];
       if constexpr (STAGED) {
         if (t + step < T) {
@@ -963,7 +980,7 @@ __global__ __launch_bounds__(64 * NW) void k_accumulate(AttendArgs a, float deca
 #pragma unroll
           for (int q4 = 0; q4 < 4; ++q4) {
             f32x4 z = *reinterpret_cast<const f32x4*>(&s_lse[q0 + 8 * q4 + 4 * half]);
-            if (MAP && a.slopes) {
+            if (a.slopes) {
               const f32x4 sl = *reinterpret_cast<const f32x4*>(&s_slope[q0 + 8 * q4 + 4 * half]);
 #pragma unroll
               for (int e = 0; e < 4; ++e) z[e] = fmaf(sl[e], age, z[e]);

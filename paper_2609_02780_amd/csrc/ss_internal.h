@@ -307,6 +307,7 @@ struct AttendStream {
   int64_t part0;               // first partial row in the workspace
   uint32_t age_off;            // bytes from rowmap to the rows' ages
   int32_t row0, n_rows;        // the detailed rows in the arena run
+  int32_t rpf, age0;           // without a row map: rows of every frame, age of the first (for a bias)
   int32_t n_q, n_own, own_cap;
   int32_t n_split, item0;
   int32_t q_split;             // accumulation: shares of the query rows

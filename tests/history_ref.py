@@ -8,6 +8,9 @@ Bounds count roundings of at most u = 2^-24 (fp32) and h = 2^-8 (bfloat16), rela
           capped score for its tanh);
   p       exp of a score that is off by e is off by e relative (2 e bounds e^e - 1 here),
           one bfloat16 rounding: h;
+  flush   a p below the smallest normal fp32 number, 2^-126, may come out as 0: each of the
+          terms of a weight, the only sums that are not taken against a maximum, is then off
+          by less than 2^-126 (far rows under a steep bias have weights of 1e-80);
   sums    n terms of one sign added in any order: at most n u relative, a tree or lane
           split only fewer; the maximum's rescaling adds one rounding a tile;
   out     a weighted mean of the values: each relative error r of the p's moves it by at
@@ -69,7 +72,7 @@ def attend(q, k, v, mask, G, softcap=0.0, slopes=None, age=None):
 def weights(q, k, lse, G, softcap=0.0, slopes=None, age=None):
     """sum over heads and queries of exp(s - lse), [H_kv][n], and its bound."""
     Hq, nq, _ = q.shape
-    w, b = np.zeros(k.shape[:2]), np.zeros(k.shape[:2])
+    w, b = np.zeros(k.shape[:2]), np.full(k.shape[:2], G * nq * 2.0 ** -126)
     for h in range(Hq):
         s, err = scores(q[h], k[h // G], softcap, None if slopes is None else slopes[h], age)
         z = np.asarray(lse[h], dtype=np.float64)

@@ -241,6 +241,30 @@ def test_large_scores():
         check((out[0], lse[0]), want(st, 0, q, softcap=cap), cap)
 
 
+@pytest.mark.parametrize("rows", [1, 2, 3, 31, 32, 33, 127, 700])
+def test_bias_over_equal_frames(rows):
+    """Ages from the frames' one size, and (with a list, or wide questions) from the map."""
+    import paper_2609_02780_amd as P
+    rng = np.random.default_rng(rows)
+    heads = (8, 2, 64)
+    st = Stream(rng, heads, [(max(2, 900 // rows), rows)])
+    slopes = np.linspace(-0.05, 0.4, 8).astype(np.float32)
+    att = P.HistoryAttention([st.ix], 9.0, torch.from_numpy(slopes).cuda())
+    every = torch.arange(len(st.rows), device="cuda")[None]
+    for nq in (1, 10, 20, 40):
+        q = bf(rng, 8, nq, 64, scale=1.5)
+        own = Own(rng, heads, nq + 3)
+        log("rows", rows, "n_q", nq)
+        ref = want(st, 0, q, own, softcap=9.0, slopes=slopes.astype(np.float64))
+        for fr in (None, every):
+            out, lse = att(0, [dev(q)], own=[own.arg], frames=fr)
+            check((out[0], lse[0]), ref, (rows, nq))
+            att.accumulate(0, [dev(q)], lse, frames=fr, decay=0.0)
+            k, _, _, age = st.seen(0)
+            w, b = R.weights(R.f64(q), k, lse[0].cpu().numpy(), 4, 9.0, slopes.astype(np.float64), age)
+            assert (np.abs(st.ix.weights[0].double().cpu().numpy() - w) <= b).all()
+
+
 def test_far_addresses():
     """Rows whose places lie beyond 2^32 bytes of the arenas, in every operator."""
     import paper_2609_02780_amd as P
