@@ -636,6 +636,94 @@ def test_closed_index():
         att(0, [dev(bf(np.random.default_rng(1), 4, 1, 64))])
 
 
+def random_call(seed):
+    """A batch of streams of random shape and state, a random call on it, its weights and an
+    eviction, all against the 64-bit forms."""
+    import paper_2609_02780_amd as P
+    rng = np.random.default_rng([seed, 99])
+    pick = lambda *x: x[int(rng.integers(len(x)))]
+    heads = pick((4, 2, 64), (28, 4, 128), (16, 1, 64), (3, 1, 128), (8, 8, 64), (10, 2, 128))
+    L, S = int(rng.integers(1, 4)), pick(1, 1, 2, 3, 5)
+    layer = int(rng.integers(L))
+    sts, firsts = [], []
+    for s in range(S):
+        runs = [(int(rng.integers(1, 30)), int(pick(1, 7, 16, 33, 50, 128, 200))) for _ in range(pick(1, 1, 2, 3))]
+        st = Stream(rng, heads, runs, L=L, n_recent=int(rng.integers(0, 4)))
+        first = 0
+        if len(runs) == 1 and len(st.rows) > 4 and rng.random() < 0.4:      # some frames left, perhaps the arena too
+            first = int(rng.integers(1, len(st.rows) - 3))
+            P.LongClusters(st.ix, runs[0][1], 40, 0.3).absorb(first, first)
+            if rng.random() < 0.5:
+                st.ix.compact()
+        sts.append(st)
+        firsts.append(first)
+    nqs = [int(pick(1, 1, 2, 5, 9, 20, 33, 70, 140)) for _ in range(S)]
+    qs = [bf(rng, heads[0], n, heads[2], scale=float(pick(0.3, 1.5, 4.0))) for n in nqs]
+    cap = float(pick(0.0, 0.0, 2.0, 15.0, 50.0))
+    slopes = (rng.random(heads[0]) * 0.5 - 0.1).astype(np.float32) if rng.random() < 0.5 else None
+    owns = [Own(rng, heads, n + int(pick(0, 1, 40, 200)), room=int(rng.integers(0, 9))) if rng.random() < 0.6 else None
+            for n in nqs]
+    pars = [np.array([int(rng.integers(-2, n + 2)) for _ in range(n)], np.int32) if o is not None and rng.random() < 0.4
+            else None for n, o in zip(nqs, owns)]
+    lists = kinds = None
+    if rng.random() < 0.5:
+        m = int(pick(1, 3, 20, 70))
+        lists = rng.integers(-2, 60, (S, m))
+        kinds = (rng.random((S, m)) < 0.2).astype(np.int32) if rng.random() < 0.5 else np.zeros((S, m), np.int32)
+    log("seed", seed, heads, L, [x.rows[:1] + [len(x.rows)] for x in sts], firsts, nqs, cap, slopes is not None,
+        [o and o.n for o in owns], [p is not None for p in pars], None if lists is None else lists.shape)
+    att = P.HistoryAttention([x.ix for x in sts], cap, None if slopes is None else torch.from_numpy(slopes).cuda())
+    kw = {} if lists is None else {"frames": torch.from_numpy(lists).cuda(), "kinds": torch.from_numpy(kinds).cuda()}
+    qd = [dev(q) for q in qs]
+    out, lse = att(layer, qd, own=[o and o.arg for o in owns],
+                   tree=[None if p is None else torch.from_numpy(p).cuda() for p in pars], **kw)
+    s64 = None if slopes is None else slopes.astype(np.float64)
+    seen = [None if lists is None else [int(f) for f, k in zip(lists[s], kinds[s]) if k == 0] for s in range(S)]
+    for s in range(S):
+        check((out[s], lse[s]), want(sts[s], layer, qs[s], owns[s], pars[s], seen[s], firsts[s], cap, s64), s)
+    before = []
+    for x in sts:
+        w = torch.rand(x.ix.weights.shape, device="cuda")
+        x.ix.weights.copy_(w)
+        before.append(w.double().cpu().numpy())
+    decay = float(pick(0.0, 0.5, 1.0))
+    att.accumulate(layer, qd, lse, decay=decay, **kw)
+    for s, x in enumerate(sts):
+        k, _, keep, age = x.seen(layer, seen[s], firsts[s])
+        w, b = R.weights(R.f64(qs[s]), k, lse[s].cpu().numpy(), heads[0] // heads[1], cap, s64, age)
+        got, b0 = x.ix.weights.double().cpu().numpy(), before[s]
+        gone = len(x.frame) - got.shape[-1]                  # rows that compaction dropped
+        live = (x.frame >= firsts[s])[gone:]
+        ref = np.where(live, decay * b0[layer], b0[layer])
+        tol = 2 * R.U * b0[layer]
+        keep = keep[gone:]
+        ref[:, keep] += w
+        tol[:, keep] += b + 2 * R.U * (w + b0[layer][:, keep])
+        assert (np.abs(got[layer] - ref) <= tol).all(), ("weights", s)
+        others = [l for l in range(L) if l != layer]
+        assert np.array_equal(got[others], b0[others])
+    x, first = sts[0], firsts[0]
+    hi = int(rng.integers(first, max(first, len(x.rows) - x.ix.desc.n_recent) + 1))
+    keep_rows = int(pick(1, 3, 20, 64, 300))
+    dst = P.ShallowIndex(L, *heads, len(x.rows), len(x.frame))
+    dst.attach_values()
+    x.ix.evict_into(dst, hi, keep_rows)
+    w = x.ix.weights.cpu().numpy()
+    tail = x.rows[first:]
+    start = sum(x.rows[:first]) - (len(x.frame) - w.shape[-1])
+    for l in range(L):
+        for g in range(heads[1]):
+            pos = R.kept_rows(w[l, g, start:], tail, hi - first, keep_rows)
+            assert np.array_equal(dst.weights[l, g].cpu().numpy(), w[l, g, start:][pos])
+            assert np.array_equal(host(dst.keys[l, g]).view(np.uint16), x.k[l][g, sum(x.rows[:first]):][pos])
+            assert np.array_equal(host(dst.values[l, g]).view(np.uint16), x.v[l][g, sum(x.rows[:first]):][pos])
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_random_calls(seed):
+    random_call(seed)
+
+
 def test_together():
     """A question on a stream, as it is served: append, retrieve, assemble the evidence,
     attend over the history and over the evidence, note the weights, evict, and draft
