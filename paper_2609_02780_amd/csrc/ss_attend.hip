@@ -312,9 +312,10 @@ __device__ __forceinline__ int value_swizzle(int r) {
 // takes its age from the frames' one size.
 //
 // What bounds it.  Few columns: reading keys and values (one token over 705,600 rows of 4
-// KV heads, d 128: 246 us, 5.9 TB/s; WQ = 1: each wave loads what it reads, no barriers).
+// KV heads, d 128: 219 to 240 us, 6.0 to 6.6 TB/s; WQ = 1: each wave loads what it reads, no
+// barriers).
 // Many columns: the matrix unit and the power it may draw (1,024 tokens of 28 heads over
-// 117,600 rows: 1.44 ms, 1.2 PFLOP/s; a block's tile of 64 keys x 256 columns takes
+// 117,600 rows: 1.44 to 1.53 ms, 1.1 to 1.2 PFLOP/s by card; a block's tile of 64 keys x 256 columns takes
 // 3,200 clocks, 2,048 of them matrix work, at the 1.5 to 1.8 GHz the card then holds).
 // 32 columns a wave keep O^T, the queries, a tile's scores and two steps of LDS reads in
 // 200 registers, so that two waves fit a SIMD and can take turns.
@@ -879,6 +880,9 @@ __global__ __launch_bounds__(256) void k_join(AttendArgs a) {
 // two lanes that hold it, added in one order, so nothing is atomic.  Where the keys
 // alone do not fill the card, the query rows are shared out too: each share's sums go
 // to the workspace and k_add adds them in order.
+// One token: bound by reading the keys, which a block without a map takes through LDS in
+// whole lines (705,600 rows of 4 KV heads, d 128: 116 to 119 us, 6.1 TB/s).  More: by cap,
+// bias and exp on the vector unit (32 tokens of 28 heads, 117,600 rows, 105 M scores: 56 us).
 template <int D, int PM, int NW, bool MAP>
 __global__ __launch_bounds__(64 * NW) void k_accumulate(AttendArgs a, float decay) {
   constexpr int RB = D * 2, CH = D / 8, KST = D / 16;
