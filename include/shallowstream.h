@@ -516,6 +516,9 @@ typedef struct {
  *            natural log of the softmax's denominator, ln sum_j exp(s_j).
  * Outputs may not overlap each other or an input (an out that is also one of the
  * queries is refused).
+ * Queries, stored rows and own tokens must be finite: a value that is not can reach
+ * queries of its stream that do not see it (p = 0 times it).  What is not read may hold
+ * anything: own tokens from n_own on, frames outside the list, rows behind the last.
  * A query that sees nothing gives out = 0 and lse = -inf.  Scores, maxima and sums
  * are fp32; p is rounded to bf16 before it meets the values.  A result depends on
  * its stream's arguments and on the batch's sizes (how the rows are shared out),
