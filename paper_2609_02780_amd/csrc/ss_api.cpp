@@ -704,6 +704,57 @@ struct AttendTile {
 constexpr AttendTile kAttendTiles[4] = {{32, 128}, {64, 128}, {128, 64}, {256, 64}};
 constexpr int kCus = 256;
 
+// Key tiles of a stream, and its items before the key axis is shared.
+int64_t key_tiles(const ss::AttendStream& st, int64_t visible, const AttendTile& tile) {
+  return (visible + tile.keys - 1) / tile.keys + (st.n_own + tile.keys - 1) / tile.keys;
+}
+int64_t column_blocks(const ss::AttendArgs& a, const ss::AttendStream& st, const AttendTile& tile) {
+  return ((int64_t)a.G * st.n_q + tile.columns - 1) / tile.columns * a.Hk;
+}
+
+// Shares of the key axis: the key tiles of an item.  A CU holds one block (by LDS; at d = 64 two, which
+// pays except for the widest tiling: 52 columns over 1 hour 149 -> 122 us, 400 over 10 minutes 90 ->
+// 103), so items run in rounds of `slots`, and a round costs its longest item: `per`
+// tiles and what starting and ending an item costs (kItemTiles).  For each number of
+// rounds the smallest `per` that fits it is found, and the cheapest number taken, or no
+// sharing at all where that saves the second launch (kJoinTiles).  Measured, us, one /
+// two / four / eight rounds: one token over 1 hour 276 / 281 / 289 / 316, 64 tokens 691
+// / 706 / 736 / 793; 1,024 tokens over 10 minutes (112 column blocks): 224 items 1,593,
+// 336 items 1,996, 1,008 items 1,690.
+int64_t attend_share(const ss::AttendArgs& a, int D, int shape, const int64_t* visible) {
+  const AttendTile tile = kAttendTiles[shape];
+  const int64_t slots = D == 64 && shape < 3 ? 2 * kCus : kCus;
+  const int64_t kItemTiles = tile.keys == 128 ? 2 : 4, kJoinTiles = tile.keys == 128 ? 8 : 4;
+  int64_t tiles[ss::kAttendStreams], blocks_of[ss::kAttendStreams], longest_tiles = 1, whole = 0;
+  for (int i = 0; i < a.S; ++i) {
+    tiles[i] = key_tiles(a.st[i], visible[i], tile);
+    blocks_of[i] = column_blocks(a, a.st[i], tile);
+    longest_tiles = std::max(longest_tiles, tiles[i]);
+    whole += blocks_of[i];
+  }
+  auto items_at = [&](int64_t per) {
+    int64_t n = 0;
+    for (int i = 0; i < a.S; ++i) n += std::max<int64_t>(1, (tiles[i] + per - 1) / per) * blocks_of[i];
+    return n;
+  };
+  const int64_t rounds_whole = (whole + slots - 1) / slots;
+  int64_t per = longest_tiles, cost = rounds_whole * (longest_tiles + kItemTiles);
+  for (int64_t r = rounds_whole; r <= rounds_whole + 7; ++r) {
+    int64_t lo = 1, hi = longest_tiles;             // items_at(hi) = whole <= r slots
+    while (lo < hi) {
+      const int64_t mid = (lo + hi) / 2;
+      if (items_at(mid) <= r * slots) hi = mid;
+      else lo = mid + 1;
+    }
+    const int64_t c = r * (lo + kItemTiles) + kJoinTiles;
+    if (c < cost) {
+      cost = c;
+      per = lo;
+    }
+  }
+  return per;
+}
+
 // Fills the arguments of one group of streams [s0, s0 + S); pointers into the
 // workspace when `ws` is given.  Returns the group's workspace bytes.
 size_t plan_attend(ss::AttendArgs& a, ss::AttendPlan& p, ss::RowsArgs& rows, ss_index* const* idx, int s0, int S,
@@ -735,12 +786,42 @@ size_t plan_attend(ss::AttendArgs& a, ss::AttendPlan& p, ss::RowsArgs& rows, ss_
   int m_max = 0;
   for (int i = 0; i < S; ++i) m_max = std::max(m_max, a.G * n_q[s0 + i]);
   p.join_rows = m_max * a.Hk;
+  int64_t visible[ss::kAttendStreams];   // most rows each stream can see
+  for (int i = 0; i < S; ++i) {
+    const ss_index* x = idx[s0 + i];
+    const int64_t f_lo = std::min(x->first_detail, x->n_frames);
+    a.st[i].n_q = n_q[s0 + i];
+    a.st[i].n_own = own_count(own, s0 + i);
+    visible[i] = x->n_rows - row_of(x, f_lo);
+    if (!p.listed) continue;
+    int64_t longest = x->rpf;
+    if (x->rpf <= 0) {
+      longest = 0;
+      for (int64_t f = f_lo; f < x->n_frames; ++f) longest = std::max(longest, row_of(x, f + 1) - row_of(x, f));
+    }
+    visible[i] = std::min<int64_t>(visible[i], longest * prm->n_listed);
+  }
+  int64_t per = 0;                       // key tiles of an item of k_attend
+  if (!accumulate) {
+    // The fewest columns that hold the query rows, since every column block reads the keys
+    // again.  But where an item of a wide tiling has few tiles (up to 1,024 / d of 64 keys), starting it
+    // and joining the parts of its many columns cost more than reading twice: two
+    // waves' columns.  Us, wide / two waves: 448 columns over 67 frames of 196 rows (7 tiles) 41 / 38, over
+    // 134 (13) 48 / 51; 252 over 134 (7) 40 / 37, over 200 (10) 45 / 47; d = 64, 256 over
+    // 300 (15) 42 / 40, 128 of two KV heads over 300 (4) 35 / 26.
+    p.shape = 0;
+    while (p.shape < 3 && kAttendTiles[p.shape].columns < m_max) ++p.shape;
+    per = attend_share(a, p.D, p.shape, visible);
+    if (p.shape > 1 && per * p.D <= 1024) {
+      p.shape = 1;
+      per = attend_share(a, p.D, p.shape, visible);
+    }
+  }
   // A bias needs each row's frame: a quotient where all frames have the same rows, else a
   // map (one token over 1 hour 260 -> 242 us without it).  k_attend's widest tiling has only
   // the map.
   p.map = p.listed;
-  for (int i = 0; i < S; ++i)
-    p.map |= prm->slopes && (idx[s0 + i]->rpf <= 0 || (!accumulate && m_max > kAttendTiles[2].columns));
+  for (int i = 0; i < S; ++i) p.map |= prm->slopes && (idx[s0 + i]->rpf <= 0 || (!accumulate && p.shape == 3));
   size_t off = 0;
   auto take = [&](size_t bytes) -> char* {
     off = align256(off);
@@ -748,7 +829,6 @@ size_t plan_attend(ss::AttendArgs& a, ss::AttendPlan& p, ss::RowsArgs& rows, ss_
     off += bytes;
     return r;
   };
-  int64_t visible[ss::kAttendStreams];   // most rows each stream can see
   for (int i = 0; i < S; ++i) {
     const ss_index* x = idx[s0 + i];
     ss::AttendStream& st = a.st[i];
@@ -764,18 +844,7 @@ size_t plan_attend(ss::AttendArgs& a, ss::AttendPlan& p, ss::RowsArgs& rows, ss_
     st.n_rows = (int32_t)n;
     st.rpf = std::max(x->rpf, 1);
     st.age0 = (int32_t)(x->n_frames - f_lo);
-    st.n_q = n_q[s0 + i];
-    st.n_own = own_count(own, s0 + i);
-    visible[i] = n;
     if (!p.map) continue;
-    if (p.listed) {
-      int64_t longest = x->rpf;
-      if (x->rpf <= 0) {
-        longest = 0;
-        for (int64_t f = f_lo; f < x->n_frames; ++f) longest = std::max(longest, row_of(x, f + 1) - row_of(x, f));
-      }
-      visible[i] = std::min<int64_t>(n, longest * prm->n_listed);
-    }
     const size_t one = align256((size_t)(visible[i] + 1) * 4);
     char* map = take(2 * one + 256);
     ss::RowsStream& r = rows.st[i];
@@ -804,7 +873,7 @@ size_t plan_attend(ss::AttendArgs& a, ss::AttendPlan& p, ss::RowsArgs& rows, ss_
   {
     int64_t bytes = 0;
     for (int i = 0; i < S; ++i) bytes += visible[i] * a.Hk * p.D * (accumulate ? 2 : 4);
-    a.once = bytes > (int64_t)256 << 20 && m_max <= kAttendTiles[2].columns;
+    a.once = bytes > (int64_t)256 << 20 && m_max <= kAttendTiles[accumulate ? 2 : std::min(p.shape, 2)].columns;
   }
 
   if (accumulate) {
@@ -842,54 +911,13 @@ size_t plan_attend(ss::AttendArgs& a, ss::AttendPlan& p, ss::RowsArgs& rows, ss_
     return align256(off);
   }
 
-  p.shape = 0;
-  while (p.shape < 3 && kAttendTiles[p.shape].columns < m_max) ++p.shape;
-  const AttendTile tile = kAttendTiles[p.shape];
-  // Shares of the key axis.  A CU holds one block (by LDS; at d = 64 two, which pays except for
-  // the widest tiling: 52 columns over 1 hour 149 -> 122 us, 400 over 10 minutes 90 ->
-  // 103), so items run in rounds of `slots`, and a round costs its longest item: `per`
-  // tiles and what starting and ending an item costs (kItemTiles).  For each number of
-  // rounds the smallest `per` that fits it is found, and the cheapest number taken, or no
-  // sharing at all where that saves the second launch (kJoinTiles).  Measured, us, one /
-  // two / four / eight rounds: one token over 1 hour 276 / 281 / 289 / 316, 64 tokens 691
-  // / 706 / 736 / 793; 1,024 tokens over 10 minutes (112 column blocks): 224 items 1,593,
-  // 336 items 1,996, 1,008 items 1,690.
-  const int64_t slots = p.D == 64 && p.shape < 3 ? 2 * kCus : kCus;
-  const int64_t kItemTiles = tile.keys == 128 ? 2 : 4, kJoinTiles = tile.keys == 128 ? 8 : 4;
-  int64_t tiles[ss::kAttendStreams], blocks_of[ss::kAttendStreams], longest_tiles = 1, whole = 0;
-  for (int i = 0; i < S; ++i) {
-    tiles[i] = (visible[i] + tile.keys - 1) / tile.keys + (a.st[i].n_own + tile.keys - 1) / tile.keys;
-    blocks_of[i] = (a.G * a.st[i].n_q + tile.columns - 1) / tile.columns * a.Hk;
-    longest_tiles = std::max(longest_tiles, tiles[i]);
-    whole += blocks_of[i];
-  }
-  auto items_at = [&](int64_t per) {
-    int64_t n = 0;
-    for (int i = 0; i < S; ++i) n += std::max<int64_t>(1, (tiles[i] + per - 1) / per) * blocks_of[i];
-    return n;
-  };
-  const int64_t rounds_whole = (whole + slots - 1) / slots;
-  int64_t per = longest_tiles, cost = rounds_whole * (longest_tiles + kItemTiles);
-  for (int64_t r = rounds_whole; r <= rounds_whole + 7; ++r) {
-    int64_t lo = 1, hi = longest_tiles;             // items_at(hi) = whole <= r slots
-    while (lo < hi) {
-      const int64_t mid = (lo + hi) / 2;
-      if (items_at(mid) <= r * slots) hi = mid;
-      else lo = mid + 1;
-    }
-    const int64_t c = r * (lo + kItemTiles) + kJoinTiles;
-    if (c < cost) {
-      cost = c;
-      per = lo;
-    }
-  }
   int64_t parts = 0;
   for (int i = 0; i < S; ++i) {
     ss::AttendStream& st = a.st[i];
-    const int64_t M = (int64_t)a.G * st.n_q;
-    st.n_split = (int32_t)std::max<int64_t>(1, (tiles[i] + per - 1) / per);
+    const int64_t M = (int64_t)a.G * st.n_q, tiles = key_tiles(st, visible[i], kAttendTiles[p.shape]);
+    st.n_split = (int32_t)std::max<int64_t>(1, (tiles + per - 1) / per);
     st.item0 = p.items;
-    p.items += (int)(st.n_split * blocks_of[i]);
+    p.items += (int)(st.n_split * column_blocks(a, st, kAttendTiles[p.shape]));
     st.part0 = parts;
     p.join_parts = std::max(p.join_parts, st.n_split);
     if (st.n_split > 1) parts += st.n_split * M * a.Hk;

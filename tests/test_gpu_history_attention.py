@@ -627,6 +627,34 @@ def test_longest_prompt():
     check((out[0], lse[0]), want(st, 0, q, own))
 
 
+@pytest.mark.parametrize("mixed", [False, True])
+@pytest.mark.parametrize("heads,nq", [((8, 2, 128), 30), ((8, 2, 128), 75), ((16, 8, 64), 60), ((8, 2, 64), 75)], ids=str)
+def test_many_columns_over_many_tiles(heads, nq, mixed):
+    """120 and 300 query rows a KV head, each item with more than 1,024 / d tiles of 64 keys: 16
+    streams share the card, so the 70 tiles are cut into 8 parts at most where d = 128, 4 where d = 64."""
+    import paper_2609_02780_amd as P
+    rng = np.random.default_rng([heads[0], heads[2], nq, mixed])
+    st = Stream(rng, heads, [(30, 65), (41, 62)] if mixed else [(70, 64)])
+    S = 16
+    qs = [bf(rng, heads[0], nq, heads[2], scale=1.5) for _ in range(S)]
+    owns = [Own(rng, heads, nq + 9 * s) for s in range(S)]
+    slopes = np.linspace(-0.01, 0.2, heads[0]).astype(np.float32)
+    par = np.array([rng.integers(-1, i) if i else -1 for i in range(nq)], dtype=np.int32)
+    listed = [f for f in range(len(st.rows)) if f % 9 != 4] + [3, 3, -1, 400]
+    listed = (listed + [-1] * 71)[:71]
+    for what, softcap, sl, frames, tree in (("plain", 0.0, None, None, None), ("cap", 6.0, None, None, None),
+                                            ("bias", 0.0, slopes, None, None), ("all", 30.0, slopes, listed, None),
+                                            ("tree", 0.0, slopes, None, par)):
+        log("case", heads, nq, mixed, what)
+        att = P.HistoryAttention([st.ix] * S, softcap, None if sl is None else torch.from_numpy(sl).cuda())
+        fr = None if frames is None else torch.tensor([frames] * S, device="cuda")
+        out, lse = att(0, [dev(q) for q in qs], own=[o.arg for o in owns], frames=fr,
+                       tree=None if tree is None else [torch.from_numpy(tree).cuda()] * S)
+        for s in (0, 9, 15):
+            check((out[s], lse[s]), want(st, 0, qs[s], owns[s], tree, frames, 0, softcap,
+                                         None if sl is None else sl.astype(np.float64)), (what, s))
+
+
 def test_closed_index():
     import paper_2609_02780_amd as P
     st = Stream(np.random.default_rng(57), (4, 2, 64), [(2, 8)])
