@@ -695,9 +695,7 @@ ss_status check_attend(ss_index* const* idx, int32_t n_streams, const int32_t* n
   return SS_OK;
 }
 
-// Launch shapes of k_attend (query columns of a block, keys of a tile) by the
-// columns M = G n_q of a KV head: the fewest that hold them, since every column
-// block reads the keys again.
+// Launch shapes of k_attend: query columns of a block, keys of a tile.
 struct AttendTile {
   int columns, keys;
 };
