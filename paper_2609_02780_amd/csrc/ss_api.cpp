@@ -699,7 +699,10 @@ ss_status check_attend(ss_index* const* idx, int32_t n_streams, const int32_t* n
 struct AttendTile {
   int columns, keys;
 };
-constexpr AttendTile kAttendTiles[4] = {{32, 128}, {64, 128}, {128, 64}, {256, 64}};
+constexpr int kAttendColumns[4] = {32, 64, 128, 256};
+AttendTile attend_tile(int D, int shape) {
+  return {kAttendColumns[shape], shape == 0 || (shape == 1 && D == 64) ? 128 : 64};
+}
 constexpr int kCus = 256;
 
 // Key tiles of a stream, and its items before the key axis is shared.
@@ -710,9 +713,9 @@ int64_t column_blocks(const ss::AttendArgs& a, const ss::AttendStream& st, const
   return ((int64_t)a.G * st.n_q + tile.columns - 1) / tile.columns * a.Hk;
 }
 
-// Shares of the key axis: the key tiles of an item.  A CU holds one block (by LDS; at d = 64 two, which
-// pays except for the widest tiling: 52 columns over 1 hour 149 -> 122 us, 400 over 10 minutes 90 ->
-// 103), so items run in rounds of `slots`, and a round costs its longest item: `per`
+// Shares of the key axis: the key tiles of an item.  A CU holds two blocks, but one by LDS of
+// the narrowest tiling at d = 128, and of the widest the second does not pay (52 columns of d = 64 over 1 hour
+// 149 -> 122 us, 400 over 10 minutes 90 -> 103), so items run in rounds of `slots`, and a round costs its longest item: `per`
 // tiles and what starting and ending an item costs (kItemTiles).  For each number of
 // rounds the smallest `per` that fits it is found, and the cheapest number taken, or no
 // sharing at all where that saves the second launch (kJoinTiles).  Measured, us, one /
@@ -720,8 +723,8 @@ int64_t column_blocks(const ss::AttendArgs& a, const ss::AttendStream& st, const
 // / 706 / 736 / 793; 1,024 tokens over 10 minutes (112 column blocks): 224 items 1,593,
 // 336 items 1,996, 1,008 items 1,690.
 int64_t attend_share(const ss::AttendArgs& a, int D, int shape, const int64_t* visible) {
-  const AttendTile tile = kAttendTiles[shape];
-  const int64_t slots = D == 64 && shape < 3 ? 2 * kCus : kCus;
+  const AttendTile tile = attend_tile(D, shape);
+  const int64_t slots = shape == 3 || (shape == 0 && D == 128) ? kCus : 2 * kCus;
   const int64_t kItemTiles = tile.keys == 128 ? 2 : 4, kJoinTiles = tile.keys == 128 ? 8 : 4;
   int64_t tiles[ss::kAttendStreams], blocks_of[ss::kAttendStreams], longest_tiles = 1, whole = 0;
   for (int i = 0; i < a.S; ++i) {
@@ -804,11 +807,11 @@ size_t plan_attend(ss::AttendArgs& a, ss::AttendPlan& p, ss::RowsArgs& rows, ss_
     // The fewest columns that hold the query rows, since every column block reads the keys
     // again.  But where an item of a wide tiling has few tiles (up to 1,024 / d of 64 keys), starting it
     // and joining the parts of its many columns cost more than reading twice: two
-    // waves' columns.  Us, wide / two waves: 448 columns over 67 frames of 196 rows (7 tiles) 41 / 38, over
-    // 134 (13) 48 / 51; 252 over 134 (7) 40 / 37, over 200 (10) 45 / 47; d = 64, 256 over
-    // 300 (15) 42 / 40, 128 of two KV heads over 300 (4) 35 / 26.
+    // waves' columns.  Us, wide / two waves: 448 columns over 67 frames of 196 rows (7 tiles) 41 / 37, over
+    // 134 (13) 48 / 52; 252 over 134 (7) 40 / 37, over 300 (15) 55 / 56; 112 over 300 (8) 42 / 40, over
+    // 3,600 (87) 284 / 345; d = 64, 256 over 300 (15) 42 / 40, 100 over 3,600 (87) 182 / 188.
     p.shape = 0;
-    while (p.shape < 3 && kAttendTiles[p.shape].columns < m_max) ++p.shape;
+    while (p.shape < 3 && kAttendColumns[p.shape] < m_max) ++p.shape;
     per = attend_share(a, p.D, p.shape, visible);
     if (p.shape > 1 && per * p.D <= 1024) {
       p.shape = 1;
@@ -871,7 +874,7 @@ size_t plan_attend(ss::AttendArgs& a, ss::AttendPlan& p, ss::RowsArgs& rows, ss_
   {
     int64_t bytes = 0;
     for (int i = 0; i < S; ++i) bytes += visible[i] * a.Hk * p.D * (accumulate ? 2 : 4);
-    a.once = bytes > (int64_t)256 << 20 && m_max <= kAttendTiles[accumulate ? 2 : std::min(p.shape, 2)].columns;
+    a.once = bytes > (int64_t)256 << 20 && m_max <= kAttendColumns[accumulate ? 2 : std::min(p.shape, 2)];
   }
 
   if (accumulate) {
@@ -912,10 +915,10 @@ size_t plan_attend(ss::AttendArgs& a, ss::AttendPlan& p, ss::RowsArgs& rows, ss_
   int64_t parts = 0;
   for (int i = 0; i < S; ++i) {
     ss::AttendStream& st = a.st[i];
-    const int64_t M = (int64_t)a.G * st.n_q, tiles = key_tiles(st, visible[i], kAttendTiles[p.shape]);
+    const int64_t M = (int64_t)a.G * st.n_q, tiles = key_tiles(st, visible[i], attend_tile(p.D, p.shape));
     st.n_split = (int32_t)std::max<int64_t>(1, (tiles + per - 1) / per);
     st.item0 = p.items;
-    p.items += (int)(st.n_split * column_blocks(a, st, kAttendTiles[p.shape]));
+    p.items += (int)(st.n_split * column_blocks(a, st, attend_tile(p.D, p.shape)));
     st.part0 = parts;
     p.join_parts = std::max(p.join_parts, st.n_split);
     if (st.n_split > 1) parts += st.n_split * M * a.Hk;

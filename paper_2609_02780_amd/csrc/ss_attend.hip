@@ -317,6 +317,9 @@ __device__ __forceinline__ int value_swizzle(int r) {
 // Many columns: the matrix unit and the power it may draw (1,024 tokens of 28 heads over
 // 117,600 rows: 1.44 to 1.53 ms, 1.1 to 1.2 PFLOP/s by card; a block's tile of 64 keys x 256 columns takes
 // 3,200 clocks, 2,048 of them matrix work, at the 1.5 to 1.8 GHz the card then holds).
+// Between, blocks of four waves, two a CU: one's softmax runs beside the other's products and
+// loads (56 columns over 705,600 rows, 4 KV heads, d 128: 251 us with one block of eight, 224; 112
+// columns 303 -> 284; at d 64 one block of eight waves and tiles of 128 keys keep up to 64 columns: 125 us, 140).
 // 32 columns a wave keep O^T, the queries, a tile's scores and two steps of LDS reads in
 // 200 registers, so that two waves fit a SIMD and can take turns.
 template <int D, int WQ, int WK, int BN, int NS, bool MAP>
@@ -334,14 +337,15 @@ struct AttendShape {
   static constexpr int LDS = (RING > MERGE ? RING : MERGE) + META + ANC;
   static constexpr int NL = 2 * NI + (MAP ? 1 : 0);   // loads a wave issues for a tile
   static_assert(NI >= 1 && NI * 1024 * NW == BN * RB && SUB >= 1 && NG <= NW && LDS <= 160 * 1024);
+  static_assert(NS == 2 || (NS == 4 && NW == 8));
 };
 
 template <int D, int WQ, int WK, int BN, int NS, bool MAP>
-__global__ __launch_bounds__(64 * WQ * WK) void k_attend(AttendArgs a) {
+__global__ __launch_bounds__(64 * WQ * WK, 2) void k_attend(AttendArgs a) {
   using T = AttendShape<D, WQ, WK, BN, NS, MAP>;
   constexpr int NW = T::NW, BM = T::BM, RB = T::RB, CH = T::CH, RPI = T::RPI, NI = T::NI, SUB = T::SUB, NL = T::NL;
   constexpr int KST = D / 16, DT = D / 32;
-  constexpr bool PP = NS == 4 && NW == 8;               // two groups of waves take turns
+  constexpr bool PP = NS == 4;                          // two groups of waves take turns
   constexpr int MERGE_AT = (T::RING > T::MERGE ? T::RING : T::MERGE);
   __shared__ __align__(1024) unsigned char smem[T::LDS];
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(SS_LDS unsigned char*)smem);
@@ -705,22 +709,13 @@ __global__ __launch_bounds__(64 * WQ * WK) void k_attend(AttendArgs a) {
       }
       if (!second) wait_loads<63, true>();
     } else {
-      if (NS > 2 && t0 + 1 < t1) issue(t0 + 1);
       for (int t = t0; t < t1; ++t) {
-        if constexpr (NS == 2) {
-          if (t + 1 < t1) {
-            wait_loads<63, T::BAR>();       // every reader is done with the buffer that is filled next
-            issue(t + 1);
-            wait_loads<NL, T::BAR>();
-          } else {
-            wait_loads<0, T::BAR>();
-          }
+        if (t + 1 < t1) {
+          wait_loads<63, T::BAR>();         // every reader is done with the buffer that is filled next
+          issue(t + 1);
+          wait_loads<NL, T::BAR>();
         } else {
-          if (t + 1 < t1)
-            wait_loads<NL, T::BAR>();
-          else
-            wait_loads<0, T::BAR>();
-          if (t + 2 < t1) issue(t + 2);
+          wait_loads<0, T::BAR>();
         }
         key_buffer(t);
         read_keys(0, fr[0]);
@@ -1251,8 +1246,11 @@ hipError_t attend_impl(const AttendArgs& a, const AttendPlan& p, hipStream_t st)
   hipError_t e;
   switch (p.shape) {
     case 0: e = attend_go<D, 1, 4, 128, 2>(a, p.map, p.items, st); break;
-    case 1: e = attend_go<D, 2, 4, 128, 2>(a, p.map, p.items, st); break;
-    case 2: e = attend_go<D, 4, 2, 64, 4>(a, p.map, p.items, st); break;
+    case 1:
+      if constexpr (D == 128) e = attend_go<D, 2, 2, 64, 2>(a, p.map, p.items, st);
+      else e = attend_go<D, 2, 4, 128, 2>(a, p.map, p.items, st);
+      break;
+    case 2: e = attend_go<D, 4, 1, 64, 2>(a, p.map, p.items, st); break;
     default: e = attend_go<D, 8, 1, 64, 4>(a, p.map, p.items, st); break;
   }
   if (e != hipSuccess) return e;
