@@ -612,14 +612,17 @@ __global__ __launch_bounds__(64 * WQ * WK, 2) void k_attend(AttendArgs a) {
         for (int i = 0; i < 16; ++i)
           if (u * WK * 32 + 8 * (i >> 2) + (i & 3) > last) sv[u * 16 + i] = neg_inf();
       if (tree && !hist) {
+        // bits of 32 keys from two words; what lies before the drafts is seen, what lies behind them masked above
+        const int words = (n_own - draft0 + 31) >> 5;
+        auto word = [&](int k) -> uint32_t { return k < 0 ? ~0u : anc[min(k, words - 1) * BM + wq * 32 + c32]; };
 #pragma unroll
-        for (int u = 0; u < SUB; ++u)
+        for (int u = 0; u < SUB; ++u) {
+          const int e = j0 + (wk + u * WK) * 32 - draft0;
+          const uint32_t bits = __builtin_amdgcn_alignbit(word((e >> 5) + 1), word(e >> 5), e & 31) >> (4 * half);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int e = jb + u * WK * 32 + 8 * (i >> 2) + (i & 3) - draft0;
-            if (e >= 0 && !((anc[(min(e, n_own - draft0 - 1) >> 5) * BM + wq * 32 + c32] >> (e & 31)) & 1u))
-              sv[u * 16 + i] = neg_inf();
-          }
+          for (int i = 0; i < 16; ++i)
+            if (!(bits >> (8 * (i >> 2) + (i & 3)) & 1u)) sv[u * 16 + i] = neg_inf();
+        }
       }
     }
     // p of all scores against the subtracted maximum, packed as pb; returns their sum
