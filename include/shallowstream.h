@@ -510,7 +510,8 @@ typedef struct {
  *            (16-byte aligned), n_q host array of 1..4096;
  *   own      NULL: the history alone;
  *   ws       device workspace of ss_attend_workspace_bytes() bytes, which a call
- *            leaves dirty: calls that may overlap need one each;
+ *            leaves dirty: calls that may overlap need one each, unless the size
+ *            is 256, the least: those calls write nothing to it;
  *   out      host array of device pointers to bf16 [H_q][n_q][d] (16-byte aligned);
  *   lse      NULL, or a host array of device pointers to fp32 [H_q][n_q]: the
  *            natural log of the softmax's denominator, ln sum_j exp(s_j).
@@ -536,7 +537,7 @@ ss_status ss_attend(ss_index* const* idx, int32_t n_streams, const void* const* 
  * the sum only for rows that the call sees (params->frames).  decay is in 0..1: 1
  * adds up, 0 overwrites.  queries, n_q and params as in ss_attend; lse its output
  * (a host array; a token with lse = -inf adds nothing).  No index may occur twice
- * in a call. */
+ * in a call.  ws as in ss_attend. */
 size_t ss_attend_accumulate_workspace_bytes(ss_index* const* idx, int32_t n_streams, const int32_t* n_q,
                                             const ss_attend_params* params);
 ss_status ss_attend_accumulate(ss_index* const* idx, int32_t n_streams, const void* const* queries,

@@ -704,6 +704,8 @@ AttendTile attend_tile(int D, int shape) {
   return {kAttendColumns[shape], shape == 0 || (shape == 1 && D == 64) ? 128 : 64};
 }
 constexpr int kCus = 256;
+// What a call that writes no workspace asks for, and no other call.
+constexpr size_t kLeastWorkspace = 256;
 
 // Key tiles of a stream, and its items before the key axis is shared.
 int64_t key_tiles(const ss::AttendStream& st, int64_t visible, const AttendTile& tile) {
@@ -909,7 +911,8 @@ size_t plan_attend(ss::AttendArgs& a, ss::AttendPlan& p, ss::RowsArgs& rows, ss_
       }
     }
     a.part_o = reinterpret_cast<float*>(take((size_t)parts * 4));
-    return align256(off);
+    // up to 64 sums would fit the least workspace, which stands for one that is not written
+    return off > 0 ? std::max(align256(off), 2 * kLeastWorkspace) : 0;
   }
 
   int64_t parts = 0;
@@ -930,7 +933,7 @@ size_t plan_attend(ss::AttendArgs& a, ss::AttendPlan& p, ss::RowsArgs& rows, ss_
 
 size_t attend_ws(ss_index* const* idx, int32_t n_streams, const int32_t* n_q, const ss_own_tokens* own,
                  const ss_attend_params* prm, bool accumulate) {
-  size_t need = 256;
+  size_t need = kLeastWorkspace;
   for (int s0 = 0; s0 < n_streams; s0 += ss::kAttendStreams) {
     ss::AttendArgs a;
     ss::AttendPlan p;
@@ -1402,7 +1405,7 @@ ss_status ss_attend(ss_index* const* idx, int32_t n_streams, const void* const* 
       ss::AttendArgs a;
       ss::AttendPlan p;
       ss::RowsArgs r;
-      need = std::max<size_t>(256, plan_attend(a, p, r, idx, s0, std::min(ss::kAttendStreams, n_streams - s0), n_q, own,
+      need = std::max(kLeastWorkspace, plan_attend(a, p, r, idx, s0, std::min(ss::kAttendStreams, n_streams - s0), n_q, own,
                                                params, false, ws));
       if (ws_bytes < need) return fail(SS_ERR_WORKSPACE, "workspace %zu bytes, %zu needed", ws_bytes, need);
       for (int i = 0; i < a.S; ++i) {
@@ -1456,7 +1459,7 @@ ss_status ss_attend_accumulate(ss_index* const* idx, int32_t n_streams, const vo
       ss::AttendArgs a;
       ss::AttendPlan p;
       ss::RowsArgs r;
-      need = std::max<size_t>(256, plan_attend(a, p, r, idx, s0, std::min(ss::kAttendStreams, n_streams - s0), n_q,
+      need = std::max(kLeastWorkspace, plan_attend(a, p, r, idx, s0, std::min(ss::kAttendStreams, n_streams - s0), n_q,
                                                nullptr, params, true, ws));
       if (ws_bytes < need) return fail(SS_ERR_WORKSPACE, "workspace %zu bytes, %zu needed", ws_bytes, need);
       for (int i = 0; i < a.S; ++i) {

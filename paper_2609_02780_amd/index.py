@@ -595,7 +595,7 @@ class HistoryAttention:
     def _workspace(self, need: int) -> torch.Tensor:
         if need == 0:
             raise L.SSError(L.SS_ERR_INVALID_ARGUMENT, self._lib.ss_last_error().decode())
-        # the least workspace is not written: calls share it
+        # a need of 256, the least, is of a call that writes no workspace: those share one
         return self._least if need == 256 else torch.empty(need, dtype=torch.uint8, device=self._device)
 
     def __call__(self, layer: int, queries, own=None, tree=None, frames=None, kinds=None, stream=None):

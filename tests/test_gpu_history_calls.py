@@ -1,0 +1,71 @@
+"""Calls of attention, weights and eviction at once, on other streams and beyond one
+pass or one launch, against serial calls and the 64-bit forms."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+import history_ref as R
+from test_gpu_history_attention import Stream, bf, dev, log
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2609_02780_amd  # noqa: F401  (fails loudly without the built library)
+
+
+@pytest.mark.parametrize("heads,nq,rows", [((16, 1, 128), 8, 32), ((16, 1, 128), 16, 16), ((3, 1, 64), 43, 16),
+                                           ((4, 2, 64), 64, 1)], ids=str)
+def test_small_accumulations_at_once(heads, nq, rows):
+    """Weights of two layers, whose few partial sums would fit the least workspace, from two
+    streams and from two graphs replayed together."""
+    import paper_2609_02780_amd as P
+    rng = np.random.default_rng([heads[0], nq, rows])
+    st = Stream(rng, heads, [(1, rows)], L=2)
+    att = P.HistoryAttention([st.ix])
+    lib, nqs = P.lib(), (C.c_int32 * 1)(nq)
+    prm = att._params(0, None, None)
+    need = lib.ss_attend_accumulate_workspace_bytes(att._handles, 1, nqs, C.byref(prm))
+    assert need > 256                                    # 256: a call that writes none
+    assert att._workspace(need).data_ptr() != att._least.data_ptr()
+    qs = [dev(bf(rng, heads[0], nq, heads[2], scale=1.5)) for _ in range(2)]
+    lses = [att(l, [qs[l]])[1] for l in range(2)]
+    for l in range(2):
+        att.accumulate(l, [qs[l]], lses[l], decay=0.0)
+    want = st.ix.weights.clone()
+    for l in range(2):
+        w, b = R.weights(R.f64(qs[l].view(torch.int16).cpu().numpy()), R.f64(st.k[l]), lses[l][0].cpu().numpy(),
+                         heads[0] // heads[1])
+        assert (np.abs(want[l].double().cpu().numpy() - w) <= b).all(), l
+    sides = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for rep in range(4):
+        st.ix.weights.fill_(7.0)
+        torch.cuda.synchronize()
+        for l, side in enumerate(sides):
+            with torch.cuda.stream(side):
+                for _ in range(6):
+                    att.accumulate(l, [qs[l]], lses[l], decay=0.0)
+        torch.cuda.synchronize()
+        assert torch.equal(st.ix.weights, want), rep
+    graphs = []
+    for l in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            for _ in range(4):
+                att.accumulate(l, [qs[l]], lses[l], decay=0.0)
+        graphs.append(g)
+    for rep in range(4):
+        st.ix.weights.fill_(7.0)
+        torch.cuda.synchronize()
+        for side, g in zip(sides, graphs):
+            with torch.cuda.stream(side):
+                g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(st.ix.weights, want), rep
