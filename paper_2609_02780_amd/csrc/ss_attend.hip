@@ -59,7 +59,7 @@ __device__ __forceinline__ float other_half(float v) {
 // One wave's direct load from global memory to LDS, 16 or 4 bytes a lane: lane l's
 // piece lands at lds + 16 l (4 l).  Written as asm because the compiler makes every
 // later LDS read wait for all such loads; the waits are counted by hand below.  No
-// register is written, and the caller waits before the pieces are read.
+// register but m0 is written, and the caller waits before the pieces are read.
 // (base and lds are the same in every lane; readfirstlane keeps them in scalar registers.)
 __device__ __forceinline__ const void* in_scalar(const void* p) {
   const uint64_t x = reinterpret_cast<uint64_t>(p);
@@ -73,16 +73,16 @@ __device__ __forceinline__ void load_lds16(const void* base, uint32_t off, uint3
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(
                      __builtin_amdgcn_readfirstlane(lds)),
                  "v"(off), "s"(in_scalar(base))
-                 : "memory");
+                 : "m0", "memory");
   else
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)),
                  "v"(off), "s"(in_scalar(base))
-                 : "memory");
+                 : "m0", "memory");
 }
 __device__ __forceinline__ void load_lds4(const void* base, uint32_t off, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)),
                "v"(off), "s"(in_scalar(base))
-               : "memory");
+               : "m0", "memory");
 }
 // At most N of this wave's loads are still under way, and its LDS reads are done;
 // with BAR all waves of the block have come this far.
