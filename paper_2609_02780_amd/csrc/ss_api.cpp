@@ -1509,8 +1509,6 @@ ss_status ss_index_evict(const ss_index* src, ss_index* dst, int64_t frame_hi, i
     }
     if (off.back() > e.max_rows)
       return fail(SS_ERR_CAPACITY, "%lld rows exceed dst's max_rows %lld", (long long)off.back(), (long long)e.max_rows);
-    if (frames * d.n_layers * d.n_kv_heads > (int64_t)1 << 32)
-      return fail(SS_ERR_UNSUPPORTED, "too many frames in one call");
     ss::EvictArgs a{};
     a.L = d.n_layers;
     a.Hk = d.n_kv_heads;

@@ -1092,6 +1092,9 @@ __global__ __launch_bounds__(256) void k_move_values(MoveValuesArgs a) {
 // order-preserving 32-bit image; rows above it stay, and of the rows at it the
 // first ones.  The kept rows are then copied, 16 bytes a lane, past the caches (1 hour to
 // 32 rows a frame: 388 us, 5.3 TB/s read and written; through the caches 417 to 430).
+// A launch holds fewer than 2^32 threads, so more than kEvictItems items (4.5 times 1 hour of
+// 4 layers and 4 KV heads) take several launches; a loop over the items in the kernel
+// made 418 us 444.
 // ---------------------------------------------------------------------------
 __global__ __launch_bounds__(1024) void k_evict_offsets(EvictArgs a) {
   __shared__ int64_t wsum[16];
@@ -1119,6 +1122,8 @@ __global__ __launch_bounds__(1024) void k_evict_offsets(EvictArgs a) {
   }
 }
 
+constexpr int64_t kEvictItems = 1 << 18;
+
 __device__ __forceinline__ uint32_t weight_key(float w) {
   const uint32_t b = __float_as_uint(w + 0.0f);          // -0 counts as 0
   return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
@@ -1144,7 +1149,7 @@ __global__ __launch_bounds__(256) void k_evict(EvictArgs a) {
     if (i0 == 0) a.dst.stats[0] = a.src.stats[0];
     return;
   }
-  const int64_t it = (int64_t)blockIdx.x * 4 + wave;
+  const int64_t it = a.item0 + (int64_t)blockIdx.x * 4 + wave;
   if (it >= items) return;
   const int64_t f = it / LH;
   const int lh = (int)(it % LH);
@@ -1330,12 +1335,18 @@ hipError_t launch_evict(EvictArgs a, hipStream_t st) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  a.item_blocks = cdiv(a.n_frames * a.L * a.Hk, 4);
-  const int64_t copy = std::max<int64_t>(1, std::min<int64_t>(cdiv(a.n_frames * a.Hk * a.D * (1 + a.L) / 4, 1024), 4096));
-  const dim3 grid((unsigned)(a.item_blocks + copy));
-  if (a.D == 128) hipLaunchKernelGGL((k_evict<128>), grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((k_evict<64>), grid, dim3(256), 0, st, a);
-  return hipGetLastError();
+  const int64_t items = a.n_frames * a.L * a.Hk;
+  // the first launch also copies what is kept of the frames themselves
+  int64_t copy = std::max<int64_t>(1, std::min<int64_t>(cdiv(a.n_frames * a.Hk * a.D * (1 + a.L) / 4, 1024), 4096));
+  for (a.item0 = 0; a.item0 < items || copy > 0; a.item0 += kEvictItems, copy = 0) {
+    a.item_blocks = cdiv(std::min(items - a.item0, kEvictItems), 4);
+    const dim3 grid((unsigned)(a.item_blocks + copy));
+    if (a.D == 128) hipLaunchKernelGGL((k_evict<128>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_evict<64>), grid, dim3(256), 0, st, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace ss

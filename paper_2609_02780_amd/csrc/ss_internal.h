@@ -350,7 +350,7 @@ struct EvictArgs {
   uint16_t* dst_values;
   const float* src_weights;
   float* dst_weights;
-  int64_t item_blocks;         // set by the launcher
+  int64_t item0, item_blocks;  // of one launch: set by the launcher
 };
 hipError_t launch_evict(EvictArgs a, hipStream_t st);
 

@@ -69,3 +69,28 @@ def test_small_accumulations_at_once(heads, nq, rows):
                 g.replay()
         torch.cuda.synchronize()
         assert torch.equal(st.ix.weights, want), rep
+
+
+@pytest.mark.parametrize("runs", [[(600, 3)], [(300, 3), (300, 2)]], ids=str)
+def test_evict_in_several_launches(runs):
+    """307,200 (frame, layer, KV head) items, where a launch takes 262,144."""
+    import paper_2609_02780_amd as P
+    rng = np.random.default_rng(len(runs))
+    st = Stream(rng, (16, 16, 64), runs, L=32)
+    n = len(st.frame)
+    w = np.round(rng.random((32, 16, n)).astype(np.float32), 1)
+    st.ix.weights.copy_(torch.from_numpy(w))
+    dst = P.ShallowIndex(32, 16, 16, 64, 600, n)
+    dst.attach_values()
+    dst.arena.fill_(255)
+    dst.value_arena.fill_(255)
+    st.ix.evict_into(dst, 590, 2)
+    rows = [min(r, 2) if f < 590 else r for f, r in enumerate(st.rows)]
+    assert dst.export()["frame_offsets"] == [0] + np.cumsum(rows).tolist()
+    keys, values, weights = (x.view(torch.int16).cpu().numpy().view(np.uint16) for x in (dst.keys, dst.values, dst.weights))
+    for l in range(32):
+        for g in range(16):
+            pos = R.kept_rows(w[l, g], st.rows, 590, 2)
+            assert np.array_equal(keys[l, g], st.k[l][g, pos]), (l, g)
+            assert np.array_equal(values[l, g], st.v[l][g, pos]), (l, g)
+            assert np.array_equal(np.ascontiguousarray(weights[l, g]).view(np.float32), w[l, g, pos]), (l, g)
