@@ -89,6 +89,7 @@ class ShallowIndex:
             L.check(L.lib().ss_index_create(C.byref(self.desc), None, 0, C.byref(h)))
         dev = torch.device(device) if device is not None else torch.device("cuda", torch.cuda.current_device())
         self.arena = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        self.value_arena = None
         self._key_rows = self._value_rows = self._weight_rows = None    # views, made when first asked for
         self._h = C.c_void_p()
         L.check(L.lib().ss_index_create(C.byref(self.desc), self.arena.data_ptr(), nbytes, C.byref(self._h)))
@@ -111,6 +112,11 @@ class ShallowIndex:
         except Exception:
             pass
 
+    def _used_on(self, stream) -> None:
+        """The arenas are read or written by work on a caller-given stream: an index that is
+        dropped right after the call keeps its memory until that work is done."""
+        _used_on(stream, self.arena, self.value_arena)
+
     def info(self) -> tuple[int, int]:
         f, r = C.c_int64(), C.c_int64()
         L.check(L.lib().ss_index_info(self.handle, C.byref(f), C.byref(r)))
@@ -127,6 +133,7 @@ class ShallowIndex:
         """Drop the frames that left the detailed window from the arena (their
         space is reused by later appends)."""
         L.check(L.lib().ss_index_compact(self.handle, _stream_handle(stream)))
+        self._used_on(stream)
 
     def budget_split(self, budget_bytes: int) -> int:
         """The frame where the detailed window must start to fit ``budget_bytes``
@@ -155,6 +162,7 @@ class ShallowIndex:
         L.check(L.lib().ss_index_append(self.handle, L.ptr_array(ptrs), n_frames, n_tokens,
                                         C.byref(comp) if comp is not None else None,
                                         _stream_handle(stream), C.byref(first)))
+        self._used_on(stream)
         return first.value
 
     def attach_values(self) -> None:
@@ -182,6 +190,7 @@ class ShallowIndex:
         L.check(L.lib().ss_index_append_kv(self.handle, L.ptr_array(kp), L.ptr_array(vp), n_frames, n_tokens,
                                            _stream_handle(stream), C.byref(first)))
         _used_on(stream, *layer_keys, *layer_values)
+        self._used_on(stream)
         return first.value
 
     def _rows_view(self, arena, at: int, dtype, *width: int) -> torch.Tensor:
@@ -219,6 +228,8 @@ class ShallowIndex:
         if dst.arena.device != self.arena.device:
             raise ValueError(f"dst lives on {dst.arena.device}, this index on {self.arena.device}")
         L.check(L.lib().ss_index_evict(self.handle, dst.handle, frame_hi, keep_rows, _stream_handle(stream)))
+        self._used_on(stream)
+        dst._used_on(stream)
 
     def export(self, stream=None) -> dict:
         """Stored rows, member counts, descriptors and frame offsets of the frames
@@ -251,7 +262,17 @@ class ShallowIndex:
                                         row0, n_rows, out.data_ptr(), ws.data_ptr(), wsb,
                                         _stream_handle(stream)))
         _used_on(stream, ws, out)
+        self._used_on(stream)
         return out[:n_rows]
+
+
+def _indices_used_on(stream, indices, *tensors) -> None:
+    """:func:`_used_on` for the indices of a call and its other buffers."""
+    if stream is None:
+        return
+    for x in indices:
+        x._used_on(stream)
+    _used_on(stream, *tensors)
 
 
 class Retriever:
@@ -297,7 +318,7 @@ class Retriever:
                                     self._ws.data_ptr(), self._ws.numel(), _stream_handle(stream),
                                     self.frame_ids.data_ptr(), self.votes.data_ptr(), self.mass.data_ptr(),
                                     self.n_out.data_ptr()))
-        _used_on(stream, self._ws)
+        _indices_used_on(stream, self.indices, self._ws, self.frame_ids, self.votes, self.mass, self.n_out)
         return self.frame_ids, self.votes, self.mass, self.n_out
 
     def noalloc(self, queries, stream=None):
@@ -310,6 +331,7 @@ class Retriever:
                                             C.byref(self.params), _stream_handle(stream),
                                             self.frame_ids.data_ptr(), self.votes.data_ptr(),
                                             self.mass.data_ptr(), self.n_out.data_ptr()))
+        _indices_used_on(stream, self.indices, self.frame_ids, self.votes, self.mass, self.n_out)
         return self.frame_ids, self.votes, self.mass, self.n_out
 
     def debug(self, queries, stream=None, stats: bool = True) -> dict:
@@ -377,7 +399,7 @@ class PooledRanker:
                                            self._ws.data_ptr(), self._ws.numel(), _stream_handle(stream),
                                            self.frame_ids.data_ptr(), self.scores.data_ptr(),
                                            self.n_out.data_ptr()))
-        _used_on(stream, self._ws)
+        _indices_used_on(stream, self.indices, self._ws, self.frame_ids, self.scores, self.n_out)
         return self.frame_ids, self.scores, self.n_out
 
 
@@ -397,6 +419,7 @@ class LongClusters:
         self._h = C.c_void_p()
         L.check(L.lib().ss_clusters_create(C.byref(self.desc), self.arena.data_ptr(), nbytes,
                                            _stream_handle(stream), C.byref(self._h)))
+        _used_on(stream, self.arena)
         self._ws = None
         self._qws = None
 
@@ -419,7 +442,7 @@ class LongClusters:
             self._ws = torch.empty(need, dtype=torch.uint8, device=self.arena.device)
         L.check(L.lib().ss_clusters_absorb(self._h, self.index.handle, frame_hi, self._ws.data_ptr(),
                                            self._ws.numel(), _stream_handle(stream)))
-        _used_on(stream, self._ws)
+        _indices_used_on(stream, [self.index], self._ws, self.arena)
 
     def retrieve(self, queries, k_clusters: int, stream=None):
         """``queries[l]``: ``[H_q][n_q][d]`` bfloat16 (only the last layer is
@@ -443,7 +466,7 @@ class LongClusters:
                                              self._qws.data_ptr(), self._qws.numel(), _stream_handle(stream),
                                              ids.data_ptr(), sc.data_ptr(), first.data_ptr(), last.data_ptr(),
                                              n_out.data_ptr()))
-        _used_on(stream, self._qws, ids, sc, first, last, n_out)
+        _indices_used_on(stream, [x], self._qws, self.arena, ids, sc, first, last, n_out)
         return ids, sc, first, last, n_out
 
     def export(self, stream=None) -> dict:
@@ -512,7 +535,7 @@ def assemble_evidence(indices, frame_ids, n_recent: int, n_before: int = 1, n_af
     L.check(L.lib().ss_assemble_evidence(handles, S, fid, n_select, C.byref(ec) if ec is not None else None,
                                          C.byref(prm), _stream_handle(stream), units.data_ptr(), kinds.data_ptr(),
                                          n_units.data_ptr(), max_units))
-    _used_on(stream, units, kinds, n_units)
+    _used_on(stream, units, kinds, n_units, *(c.arena for c in clusters or () if c is not None))
     return units, kinds, n_units
 
 
@@ -654,7 +677,7 @@ class HistoryAttention:
                               _stream_handle(stream), self._ptrs(*[t.data_ptr() for t in out]),
                               self._ptrs(*[t.data_ptr() for t in lse])))
         if stream is not None:
-            _used_on(stream, ws, *out, *lse, *queries, *used, self.slopes, frames, kinds)
+            _indices_used_on(stream, self.indices, ws, *out, *lse, *queries, *used, self.slopes, frames, kinds)
         return out, lse
 
     def accumulate(self, layer: int, queries, lse, frames=None, kinds=None, decay: float = 1.0, stream=None) -> None:
@@ -678,7 +701,7 @@ class HistoryAttention:
         L.check(lib.ss_attend_accumulate(self._handles, S, qp, n_q, lp, prm_ref, decay, ws.data_ptr(), ws.numel(),
                                          _stream_handle(stream)))
         if stream is not None:
-            _used_on(stream, ws, *queries, *lse, self.slopes, frames, kinds)
+            _indices_used_on(stream, self.indices, ws, *queries, *lse, self.slopes, frames, kinds)
 
 
 def set_profile_events(start, stop) -> None:

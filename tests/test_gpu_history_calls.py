@@ -94,3 +94,52 @@ def test_evict_in_several_launches(runs):
             assert np.array_equal(keys[l, g], st.k[l][g, pos]), (l, g)
             assert np.array_equal(values[l, g], st.v[l][g, pos]), (l, g)
             assert np.array_equal(np.ascontiguousarray(weights[l, g]).view(np.float32), w[l, g, pos]), (l, g)
+
+
+def test_arenas_are_kept_for_a_callers_stream(monkeypatch):
+    """Every call that is given a stream tells torch's allocator that the stream uses the arenas,
+    so that an index dropped right after the call keeps its memory until the work is done."""
+    import paper_2609_02780_amd as P
+    rng = np.random.default_rng(81)
+    heads = (8, 2, 64)
+    src, dst = (Stream(rng, heads, [(6, 8)], extra=8).ix for _ in range(2))
+    plain = P.ShallowIndex(1, *heads, 9, 72)
+    cl = P.LongClusters(src, 8, 4, 0.5)
+    q = dev(bf(rng, 8, 5, 64))
+    k, v = dev(bf(rng, 2, 8, 64)), dev(bf(rng, 2, 8, 64))
+    att, ret, ranker = P.HistoryAttention([src]), P.Retriever([src], 8, 2), P.PooledRanker([src], 2)
+    lse, ids = att(0, [q])[1], ret([[q]])[0]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    record, used = torch.Tensor.record_stream, set()
+
+    def note(t, stream):
+        if stream == side:
+            used.add(t.data_ptr())
+        return record(t, stream)
+
+    monkeypatch.setattr(torch.Tensor, "record_stream", note)
+    both = lambda x: {x.arena.data_ptr(), x.value_arena.data_ptr()}
+    cases = {
+        "attention": (lambda: att(0, [q], stream=side), both(src)),
+        "weights": (lambda: att.accumulate(0, [q], lse, stream=side), both(src)),
+        "evict": (lambda: src.evict_into(dst, 6, 3, stream=side), both(src) | both(dst)),
+        "append_kv": (lambda: src.append_kv([k], [v], 1, 8, stream=side), both(src)),
+        "append": (lambda: plain.append([k], 1, 8, stream=side), {plain.arena.data_ptr()}),
+        "retrieve": (lambda: ret([[q]], stream=side), both(src) | {ids.data_ptr()}),
+        "noalloc": (lambda: ret.noalloc([[q]], stream=side), both(src) | {ids.data_ptr()}),
+        "pooled": (lambda: ranker([[q]], stream=side), both(src)),
+        "scores": (lambda: src.debug_scores([q], 0, 0, stream=side), both(src)),
+        "absorb": (lambda: cl.absorb(2, 2, stream=side), both(src) | {cl.arena.data_ptr()}),
+        "clusters": (lambda: cl.retrieve([q], 2, stream=side), both(src) | {cl.arena.data_ptr()}),
+        "evidence": (lambda: P.assemble_evidence([src], ids, 1, clusters=[cl], stream=side,
+                                                 cluster_ids=torch.zeros((1, 1), dtype=torch.int64, device="cuda")),
+                     {cl.arena.data_ptr()}),
+        "compact": (lambda: src.compact(stream=side), both(src)),
+    }
+    for name, (call, arenas) in cases.items():
+        log("call", name)
+        used.clear()
+        call()
+        assert arenas <= used, name
+    torch.cuda.synchronize()
