@@ -5,6 +5,7 @@ given as ``torch.bfloat16`` or as raw ``int16``/``uint16`` bit patterns.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import math
 
@@ -37,6 +38,22 @@ def _used_on(stream, *tensors) -> None:
     for t in tensors:
         if t is not None:
             t.record_stream(stream)
+
+
+_HERE = contextlib.nullcontext()
+
+
+def _memory_of(stream):
+    """The context in which a call allocates what it fills: memory of the stream that
+    the call runs on.  Memory of the current one may still be in use there, by
+    work that was enqueued before its last owner let go of it."""
+    return _HERE if stream is None else torch.cuda.stream(stream)
+
+
+def _returned_from(stream, *tensors) -> None:
+    """Outputs of a call on a caller-given stream will be read on the current one."""
+    if stream is not None:
+        _used_on(torch.cuda.current_stream(), *tensors)
 
 
 def sample_plan(n_rows: int, top_k: int) -> tuple[int, int, int, int]:
@@ -255,13 +272,14 @@ class ShallowIndex:
         qp = [_check_bf16(q, qshape, "queries[%d]", l) for l, q in enumerate(queries)]
         if n_rows is None:
             n_rows = self.n_rows - row0
-        out = torch.empty(max(n_rows, 1), dtype=torch.float32, device=self.arena.device)
         wsb = L.lib().ss_debug_scores_workspace_bytes(self.handle)
-        ws = torch.empty(wsb, dtype=torch.uint8, device=self.arena.device)
+        with _memory_of(stream):
+            out = torch.empty(max(n_rows, 1), dtype=torch.float32, device=self.arena.device)
+            ws = torch.empty(wsb, dtype=torch.uint8, device=self.arena.device)
         L.check(L.lib().ss_debug_scores(self.handle, L.ptr_array(qp), n_q, layer, q_head, head_mode,
                                         row0, n_rows, out.data_ptr(), ws.data_ptr(), wsb,
                                         _stream_handle(stream)))
-        _used_on(stream, ws, out)
+        _returned_from(stream, out)
         self._used_on(stream)
         return out[:n_rows]
 
@@ -457,16 +475,18 @@ class LongClusters:
         if self._qws is None or self._qws.numel() < need:
             self._qws = torch.empty(need, dtype=torch.uint8, device=self.arena.device)
         dev = self.arena.device
-        ids = torch.empty(k_clusters, dtype=torch.int64, device=dev)
-        sc = torch.empty(k_clusters, dtype=torch.float32, device=dev)
-        first = torch.empty(k_clusters, dtype=torch.int64, device=dev)
-        last = torch.empty(k_clusters, dtype=torch.int64, device=dev)
-        n_out = torch.empty(1, dtype=torch.int32, device=dev)
+        with _memory_of(stream):
+            ids = torch.empty(k_clusters, dtype=torch.int64, device=dev)
+            sc = torch.empty(k_clusters, dtype=torch.float32, device=dev)
+            first = torch.empty(k_clusters, dtype=torch.int64, device=dev)
+            last = torch.empty(k_clusters, dtype=torch.int64, device=dev)
+            n_out = torch.empty(1, dtype=torch.int32, device=dev)
         L.check(L.lib().ss_clusters_retrieve(self._h, x.handle, L.ptr_array(ptrs), nq, k_clusters,
                                              self._qws.data_ptr(), self._qws.numel(), _stream_handle(stream),
                                              ids.data_ptr(), sc.data_ptr(), first.data_ptr(), last.data_ptr(),
                                              n_out.data_ptr()))
-        _indices_used_on(stream, [x], self._qws, self.arena, ids, sc, first, last, n_out)
+        _indices_used_on(stream, [x], self._qws, self.arena)
+        _returned_from(stream, ids, sc, first, last, n_out)
         return ids, sc, first, last, n_out
 
     def export(self, stream=None) -> dict:
@@ -528,14 +548,16 @@ def assemble_evidence(indices, frame_ids, n_recent: int, n_before: int = 1, n_af
                 or not frame_ids.is_contiguous():
             raise ValueError("frame_ids must be a contiguous device int64 tensor [n_streams][n_select]")
         fid = frame_ids.data_ptr()
-    units = torch.empty((S, max_units), dtype=torch.int64, device=dev)
-    kinds = torch.empty((S, max_units), dtype=torch.int32, device=dev)
-    n_units = torch.empty(S, dtype=torch.int32, device=dev)
+    with _memory_of(stream):
+        units = torch.empty((S, max_units), dtype=torch.int64, device=dev)
+        kinds = torch.empty((S, max_units), dtype=torch.int32, device=dev)
+        n_units = torch.empty(S, dtype=torch.int32, device=dev)
     handles = L.ptr_array([x.handle.value for x in indices])
     L.check(L.lib().ss_assemble_evidence(handles, S, fid, n_select, C.byref(ec) if ec is not None else None,
                                          C.byref(prm), _stream_handle(stream), units.data_ptr(), kinds.data_ptr(),
                                          n_units.data_ptr(), max_units))
-    _used_on(stream, units, kinds, n_units, *(c.arena for c in clusters or () if c is not None))
+    _used_on(stream, *(c.arena for c in clusters or () if c is not None))
+    _returned_from(stream, units, kinds, n_units)
     return units, kinds, n_units
 
 
@@ -549,6 +571,8 @@ class HistoryAttention:
     scores of query head ``h``, a row's age being the frames from its own to the end
     of the stream.  Keeps no buffers: each call allocates its workspace and outputs,
     so calls on different streams or in different captured graphs share nothing.
+    A caller that gives a ``stream`` orders it behind its inputs, and what reads the
+    outputs behind it.
     """
 
     def __init__(self, indices, softcap: float = 0.0, slopes: torch.Tensor | None = None):
@@ -665,19 +689,22 @@ class HistoryAttention:
             ot.parents = C.addressof(pp)
         own_ref = C.byref(ot) if ot is not None else None
         prm_ref = C.byref(prm)
-        ws = self._workspace(lib.ss_attend_workspace_bytes(self._handles, S, n_q, own_ref, prm_ref))
+        need = lib.ss_attend_workspace_bytes(self._handles, S, n_q, own_ref, prm_ref)
         first = queries[0].shape
-        if S > 1 and all(q.shape == first for q in queries):
-            out = list(torch.empty((S, *first), dtype=torch.bfloat16, device=self._device).unbind(0))
-            lse = list(torch.empty((S, *first[:2]), dtype=torch.float32, device=self._device).unbind(0))
-        else:
-            out = [torch.empty(q.shape, dtype=torch.bfloat16, device=self._device) for q in queries]
-            lse = [torch.empty(q.shape[:2], dtype=torch.float32, device=self._device) for q in queries]
+        with _memory_of(stream):
+            ws = self._workspace(need)
+            if S > 1 and all(q.shape == first for q in queries):
+                out = list(torch.empty((S, *first), dtype=torch.bfloat16, device=self._device).unbind(0))
+                lse = list(torch.empty((S, *first[:2]), dtype=torch.float32, device=self._device).unbind(0))
+            else:
+                out = [torch.empty(q.shape, dtype=torch.bfloat16, device=self._device) for q in queries]
+                lse = [torch.empty(q.shape[:2], dtype=torch.float32, device=self._device) for q in queries]
         L.check(lib.ss_attend(self._handles, S, qp, n_q, own_ref, prm_ref, ws.data_ptr(), ws.numel(),
                               _stream_handle(stream), self._ptrs(*[t.data_ptr() for t in out]),
                               self._ptrs(*[t.data_ptr() for t in lse])))
         if stream is not None:
-            _indices_used_on(stream, self.indices, ws, *out, *lse, *queries, *used, self.slopes, frames, kinds)
+            _indices_used_on(stream, self.indices, *queries, *used, self.slopes, frames, kinds)
+            _returned_from(stream, *out, *lse)
         return out, lse
 
     def accumulate(self, layer: int, queries, lse, frames=None, kinds=None, decay: float = 1.0, stream=None) -> None:
@@ -697,11 +724,12 @@ class HistoryAttention:
             self._on_device(t, "lse[%d]", s)
             lp[s] = t.data_ptr()
         prm_ref = C.byref(prm)
-        ws = self._workspace(lib.ss_attend_accumulate_workspace_bytes(self._handles, S, n_q, prm_ref))
+        with _memory_of(stream):
+            ws = self._workspace(lib.ss_attend_accumulate_workspace_bytes(self._handles, S, n_q, prm_ref))
         L.check(lib.ss_attend_accumulate(self._handles, S, qp, n_q, lp, prm_ref, decay, ws.data_ptr(), ws.numel(),
                                          _stream_handle(stream)))
         if stream is not None:
-            _indices_used_on(stream, self.indices, ws, *queries, *lse, self.slopes, frames, kinds)
+            _indices_used_on(stream, self.indices, *queries, *lse, self.slopes, frames, kinds)
 
 
 def set_profile_events(start, stop) -> None:

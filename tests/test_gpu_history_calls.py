@@ -143,3 +143,52 @@ def test_arenas_are_kept_for_a_callers_stream(monkeypatch):
         call()
         assert arenas <= used, name
     torch.cuda.synchronize()
+
+
+def test_buffers_come_from_the_callers_stream(monkeypatch):
+    """What a call on a given stream fills is memory of that stream: memory of the current
+    one may still be read by work whose owner has let go of it."""
+    import paper_2609_02780_amd as P
+    rng = np.random.default_rng(82)
+    heads = (8, 2, 64)
+    st = Stream(rng, heads, [(6, 8)])
+    cl = P.LongClusters(st.ix, 8, 4, 0.5)
+    cl.absorb(1, 1)
+    q = dev(bf(rng, 8, 70, 64))
+    att = P.HistoryAttention([st.ix])
+    two = P.HistoryAttention([st.ix, st.ix])
+    listed = torch.tensor([[1, 3]], device="cuda")
+    lse = att(0, [q])[1]
+    cl.retrieve([q], 2)                                  # its kept workspace
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    empty, record, made, read = torch.empty, torch.Tensor.record_stream, [], set()
+    here = torch.cuda.current_stream()
+
+    def note_empty(*a, **kw):
+        made.append(torch.cuda.current_stream() == side)
+        return empty(*a, **kw)
+
+    def note_read(t, stream):
+        if stream == here:
+            read.add(t.data_ptr())
+        return record(t, stream)
+
+    monkeypatch.setattr(torch, "empty", note_empty)
+    monkeypatch.setattr(torch.Tensor, "record_stream", note_read)
+    cases = {
+        "attention": lambda: (lambda r: [*r[0], *r[1]])(att(0, [q], frames=listed, stream=side)),
+        "two streams": lambda: (lambda r: [*r[0], *r[1]])(two(0, [q, q], stream=side)),
+        "weights": lambda: att.accumulate(0, [q], lse, frames=listed, stream=side) or [],
+        "scores": lambda: [st.ix.debug_scores([q], 0, 0, stream=side)],
+        "clusters": lambda: cl.retrieve([q], 2, stream=side),
+        "evidence": lambda: P.assemble_evidence([st.ix], listed, 1, stream=side),
+    }
+    for name, call in cases.items():
+        log("call", name)
+        made.clear()
+        read.clear()
+        out = call()
+        assert made and all(made), name
+        assert {t.data_ptr() for t in out} <= read, name
+    torch.cuda.synchronize()
