@@ -94,6 +94,12 @@ def _query_pointers(indices, queries):
     return L.ptr_array(ptrs), (C.c_int32 * S)(*n_q)
 
 
+def _on_current(device, what: str) -> None:
+    """Kernels are launched on the current device."""
+    if torch.cuda.current_device() != device.index:
+        raise ValueError(f"{what} on {device}, which is not the current device")
+
+
 class ShallowIndex:
     """One stream's shallow-layer key index in a device arena owned by this object."""
 
@@ -203,6 +209,11 @@ class ShallowIndex:
             raise ValueError(f"expected {self.n_layers} key and {self.n_layers} value tensors")
         kp = [_check_bf16(t, shape, "layer_keys[%d]", l) for l, t in enumerate(layer_keys)]
         vp = [_check_bf16(t, shape, "layer_values[%d]", l) for l, t in enumerate(layer_values)]
+        _on_current(self.arena.device, "the index lives")
+        for what, ts in (("keys", layer_keys), ("values", layer_values)):
+            for l, t in enumerate(ts):
+                if t.device != self.arena.device:
+                    raise ValueError(f"layer_{what}[{l}] lives on {t.device}, the index on {self.arena.device}")
         first = C.c_int64()
         L.check(L.lib().ss_index_append_kv(self.handle, L.ptr_array(kp), L.ptr_array(vp), n_frames, n_tokens,
                                            _stream_handle(stream), C.byref(first)))
@@ -244,6 +255,7 @@ class ShallowIndex:
         come whole."""
         if dst.arena.device != self.arena.device:
             raise ValueError(f"dst lives on {dst.arena.device}, this index on {self.arena.device}")
+        _on_current(self.arena.device, "the index lives")
         L.check(L.lib().ss_index_evict(self.handle, dst.handle, frame_hi, keep_rows, _stream_handle(stream)))
         self._used_on(stream)
         dst._used_on(stream)
@@ -600,8 +612,7 @@ class HistoryAttention:
             raise ValueError(f"{what % at} lives on {t.device}, the indices on {self._device}")
 
     def _params(self, layer: int, frames, kinds):
-        if torch.cuda.current_device() != self._device.index:
-            raise ValueError(f"the indices live on {self._device}, which is not the current device")
+        _on_current(self._device, "the indices live")
         p = L.AttendParams(layer, self.softcap, self.slopes.data_ptr() if self.slopes is not None else None,
                            None, None, 0)
         if frames is None:

@@ -192,3 +192,30 @@ def test_buffers_come_from_the_callers_stream(monkeypatch):
         assert made and all(made), name
         assert {t.data_ptr() for t in out} <= read, name
     torch.cuda.synchronize()
+
+
+def test_another_current_device(monkeypatch):
+    """Every entry point of the value cache refuses an index of another device than the current
+    one, where its kernels would run, and tensors of another device than the index."""
+    import paper_2609_02780_amd as P
+    rng = np.random.default_rng(83)
+    src, dst = (Stream(rng, (8, 2, 64), [(6, 8)], extra=8).ix for _ in range(2))
+    q, k = dev(bf(rng, 8, 5, 64)), dev(bf(rng, 2, 8, 64))
+    att = P.HistoryAttention([src])
+    lse = att(0, [q])[1]
+    before = src.weights.clone()
+
+    class Elsewhere(torch.Tensor):
+        device = torch.device("cuda", 1)
+
+    away = k.as_subclass(Elsewhere)
+    for ks, vs in (([away], [k]), ([k], [away])):
+        with pytest.raises(ValueError, match="lives on cuda:1"):
+            src.append_kv(ks, vs, 1, 8)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    for call in (lambda: att(0, [q]), lambda: att.accumulate(0, [q], lse), lambda: src.evict_into(dst, 6, 3),
+                 lambda: src.append_kv([k], [k], 1, 8)):
+        with pytest.raises(ValueError, match="not the current device"):
+            call()
+    monkeypatch.undo()
+    assert src.info() == dst.info() == (6, 48) and torch.equal(src.weights, before)
