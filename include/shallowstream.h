@@ -347,7 +347,7 @@ ss_status ss_clusters_destroy(ss_clusters* cl);
 /* Frames [first, frame_hi) of `idx` leave its detailed window, in order, and
  * are folded into `cl`; `first` is where the previous call stopped (0 at the
  * start).  frame_hi must not reach into the recent window (the newest n_recent
- * frames), and every absorbed frame must store rows_per_unit rows.  ws: device
+ * frames; first itself is always taken), and every absorbed frame must store rows_per_unit rows.  ws: device
  * workspace of ss_clusters_absorb_workspace_bytes(frame_hi - first) bytes. */
 size_t ss_clusters_absorb_workspace_bytes(int64_t n_frames);
 ss_status ss_clusters_absorb(ss_clusters* cl, ss_index* idx, int64_t frame_hi, void* ws, size_t ws_bytes,

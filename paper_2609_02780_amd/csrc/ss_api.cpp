@@ -1004,7 +1004,8 @@ ss_status ss_clusters_absorb(ss_clusters* cl, ss_index* idx, int64_t frame_hi, v
     if (c.n_layers != d.n_layers || c.n_kv_heads != d.n_kv_heads || c.head_dim != d.head_dim)
       return fail(SS_ERR_INVALID_ARGUMENT, "cluster set and index shapes differ");
     const int64_t f_lo = idx->first_detail;
-    const int64_t f_end = std::max<int64_t>(0, idx->n_frames - d.n_recent);
+    // (an eviction may have left an index whose recent window reaches before f_lo)
+    const int64_t f_end = std::max(f_lo, idx->n_frames - (int64_t)d.n_recent);
     if (frame_hi < f_lo || frame_hi > f_end)
       return fail(SS_ERR_INVALID_ARGUMENT, "frame_hi %lld outside %lld..%lld (frames leave in order, never from the recent window)",
                   (long long)frame_hi, (long long)f_lo, (long long)f_end);

@@ -6,7 +6,7 @@ import numpy as np
 import pytest
 
 import history_ref as R
-from test_gpu_history_attention import Stream, bf, dev, log
+from test_gpu_history_attention import Stream, bf, check, dev, log, want
 
 pytestmark = pytest.mark.gpu
 
@@ -219,3 +219,32 @@ def test_another_current_device(monkeypatch):
             call()
     monkeypatch.undo()
     assert src.info() == dst.info() == (6, 48) and torch.equal(src.weights, before)
+
+
+def test_evicted_into_a_larger_recent_window():
+    """An eviction leaves an index whose recent window reaches before its first detailed frame:
+    where the budget puts the border, absorption takes it, and frames leave once there are enough."""
+    import paper_2609_02780_amd as P
+    rng = np.random.default_rng(84)
+    heads = (8, 2, 64)
+    st = Stream(rng, heads, [(12, 8)])
+    P.LongClusters(st.ix, 8, 12, 0.5).absorb(8, 8)
+    dst = P.ShallowIndex(1, *heads, 20, 160, n_recent=6)
+    dst.attach_values()
+    st.ix.evict_into(dst, 8, 8)
+    assert dst.window() == (8, 8) and dst.info() == (12, 32)
+    cl = P.LongClusters(dst, 8, 12, 0.5)
+    assert dst.budget_split(0) == 8
+    cl.absorb(8, 0)
+    for f in (7, 9):
+        with pytest.raises(P.SSError, match="outside 8..8"):
+            cl.absorb(f, 1)
+    q = bf(rng, 8, 5, 64)
+    assert int(P.Retriever([dst], 8, 2)([[dev(q)]])[3][0]) == 0
+    out, lse = P.HistoryAttention([dst])(0, [dev(q)])
+    check((out[0], lse[0]), want(st, 0, q, first=8))
+    k, v = bf(rng, 2, 32, 64), bf(rng, 2, 32, 64)
+    assert dst.append_kv([dev(k)], [dev(v)], 4, 8) == 12
+    assert dst.budget_split(0) == 10
+    cl.absorb(10, 2)
+    assert dst.window() == (8, 10)
