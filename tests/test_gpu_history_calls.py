@@ -248,3 +248,101 @@ def test_evicted_into_a_larger_recent_window():
     assert dst.budget_split(0) == 10
     cl.absorb(10, 2)
     assert dst.window() == (8, 10)
+
+
+@pytest.mark.parametrize("heads,nq,rows", [((16, 16, 64), 600, 300), ((16, 8, 128), 300, 800), ((32, 8, 128), 100, 900),
+                                           ((16, 16, 64), 300, 1100)], ids=str)
+def test_weights_of_many_query_rows_in_one_share(heads, nq, rows):
+    """More than the 256 query rows of a KV head that are staged at a time: the next ones add to what
+    the first left.  16 streams fill the card, so that the query rows are not shared out (then the
+    call has no partial sums and asks for the least workspace)."""
+    import paper_2609_02780_amd as P
+    rng = np.random.default_rng([heads[0], nq, rows])
+    G = heads[0] // heads[1]
+    assert G * nq > 256
+    runs = [(rows // 50, 50)]
+    sts = [Stream(rng, heads, runs) for _ in range(16)]
+    qs = [bf(rng, heads[0], nq, heads[2], scale=1.5) for _ in range(16)]
+    qd = [dev(q) for q in qs]
+    slopes = np.linspace(-0.02, 0.3, heads[0]).astype(np.float32)
+    some = list(range(len(sts[0].rows) - 1))
+    for softcap, sl, frames, decay in ((0.0, None, None, 0.0), (0.0, None, None, 1.0), (20.0, slopes, None, 0.5),
+                                       (20.0, slopes, some, 0.25)):
+        log("case", heads, nq, rows, softcap, sl is not None, frames is not None, decay)
+        att = P.HistoryAttention([x.ix for x in sts], softcap, None if sl is None else torch.from_numpy(sl).cuda())
+        fr = None if frames is None else torch.tensor([frames] * 16, device="cuda")
+        prm = att._params(0, fr, None)
+        if frames is None:
+            assert P.lib().ss_attend_accumulate_workspace_bytes(att._handles, 16, (C.c_int32 * 16)(*[nq] * 16),
+                                                                C.byref(prm)) == 256
+        _, lse = att(0, qd, frames=fr)
+        before = []
+        for x in sts:
+            x.ix.weights.copy_(torch.rand(x.ix.weights.shape, device="cuda"))
+            before.append(x.ix.weights[0].double().cpu().numpy())
+        att.accumulate(0, qd, lse, frames=fr, decay=decay)
+        for s in (0, 7, 15):
+            k, _, keep, age = sts[s].seen(0, frames)
+            w, b = R.weights(R.f64(qs[s]), k, lse[s].cpu().numpy(), G, softcap,
+                             None if sl is None else sl.astype(np.float64), age)
+            ref, tol = decay * before[s], 2 * R.U * before[s]
+            ref[:, keep] += w
+            tol[:, keep] += b + 2 * R.U * (w + before[s][:, keep])
+            got = sts[s].ix.weights[0].double().cpu().numpy()
+            assert (np.abs(got - ref) <= tol).all(), (s, float(np.abs(got - ref).max()))
+
+
+@pytest.mark.parametrize("heads", [(8, 2, 64), (4, 1, 128)], ids=str)
+def test_rows_beyond_the_caches(heads):
+    """More than 256 MB of keys that one block reads (and of keys and values), which are loaded past
+    the caches: attention of few to 120 query rows a KV head, with and without a list, and weights.
+
+    Tolerances are those of history_ref with fewer additions in a row: a lane adds at most the p of
+    its 32 keys of a tile, then one sum a tile of at least 64 keys and one a share, so a chain has
+    at most n / 64 + 64 additions however the n rows are shared out."""
+    import paper_2609_02780_amd as P
+    rng = np.random.default_rng(heads[2])
+    Hq, Hk, d = heads
+    G, F, per = Hq // Hk, 3534, 300
+    n = F * per
+    assert n * Hk * d * 2 > 256 << 20
+
+    def rows():          # magnitudes of 1/8 to 2
+        x = rng.integers(0, 1 << 16, (Hk, n, d), dtype=np.uint16)
+        return (x & 0x807F) | (((x >> 7) & 3) + 124 << 7)
+
+    k, v = rows(), rows()
+    ix = P.ShallowIndex(1, *heads, F, n)
+    ix.attach_values()
+    ix.append_kv([dev(k)], [dev(v)], F, per)
+    every = torch.arange(F, device="cuda").flip(0)[None].contiguous()
+    chain = (n / 64 + 64) * R.U
+    kh, vh = R.f64(k), R.f64(v)
+    att = P.HistoryAttention([ix])
+    for nq in (1, 40 // G, 60 // G, 120 // G):
+        q = bf(rng, Hq, nq, d, scale=5.0)            # scores of some 4, so that few rows take most of the weight
+        log("case", heads, nq)
+        runs = [att(0, [dev(q)]), att(0, [dev(q)], frames=every)]
+        qh, w, bw = R.f64(q), np.zeros((Hk, n)), np.zeros((Hk, n))
+        for h in range(Hq) if nq == 1 else (0, Hq - 1):
+            s, err = R.scores(qh[h], kh[h // G], 0.0, None, None)
+            m = s.max(1, keepdims=True)
+            e = err.max(1) + 8 * R.U * np.abs(m[:, 0]) + 4 * R.U
+            p = np.exp(s - m)
+            z = p.sum(1)
+            lse, rel = m[:, 0] + np.log(z), 2 * e + chain
+            p /= z[:, None]
+            out, mag = p @ vh[h // G], p @ np.abs(vh[h // G])
+            for o, y in runs:
+                g, gl = o[0][h].double().cpu().numpy(), y[0][h].double().cpu().numpy()
+                assert (np.abs(g - out) <= (R.H + 2 * rel)[:, None] * mag + R.H * np.abs(out) * (1 + R.H)).all(), h
+                assert (np.abs(gl - lse) <= rel + 8 * R.U * (np.abs(lse) + 1)).all(), h
+            if nq == 1:
+                zz = runs[0][1][0][h].double().cpu().numpy()[:, None]
+                x = np.exp(s - zz)
+                w[h // G] += x[0]
+                bw[h // G] += (x * (2 * (err + 8 * R.U * (np.abs(s) + np.abs(zz))) + (G + 8) * R.U))[0] + 2.0 ** -126
+        if nq == 1:
+            for fr in (None, every):
+                att.accumulate(0, [dev(q)], runs[0][1], frames=fr, decay=0.0)
+                assert (np.abs(ix.weights[0].double().cpu().numpy() - w) <= bw).all()
