@@ -15,7 +15,7 @@
 // operand is read from the row-major tile by the transposing LDS read, four keys
 // of one dimension at a time, which is that same order.
 // P is rounded to bf16 for the second product (its sum is taken before): a
-// rounding of at most 2^-9 of each term, like the rounding of the values
+// rounding of at most 2^-8 of each term, like the rounding of the values
 // themselves; maxima, sums and the output stay fp32 until the one rounding at
 // the end.
 #include "ss_internal.h"
@@ -95,7 +95,7 @@ __device__ __forceinline__ void wait_loads() {
 }
 
 // tanh through exp; below 1 by the continued fraction x / (1 + x^2 / (3 + x^2 / (5 +
-// ...))) cut after 13 (off by less than 2^-30 there), which keeps small scores' relative
+// ...))) cut after 11 (off by less than 2^-31 there), which keeps small scores' relative
 // precision.
 __device__ __forceinline__ float tanh_any(float x) {
   const float y = x * x;
@@ -107,7 +107,7 @@ __device__ __forceinline__ float tanh_any(float x) {
 }
 // v[i] <- cap tanh(v[i] x) in units of log 2, x = scale / cap: by polynomials of least
 // maximum error in z^2, z = v x, for tanh(z) / z: of degree 3 where all of a wave's |z|
-// are below 0.35 (off by 2^-24.9 at most), of degree 5 below 0.6 (2^-28.6).  Scores far
+// are below 0.35 (off by 2^-24.7 at most), of degree 5 below 0.6 (2^-28.3).  Scores far
 // below their cap are the usual case.
 template <int N>
 __device__ __forceinline__ float top_of(const float (&v)[N]) {
