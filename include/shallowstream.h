@@ -485,7 +485,8 @@ typedef struct {
  *                 [H_kv][capacity][d] (16-byte aligned); tokens n_own .. capacity
  *                 are not read.  An entry is not read when its n_own is 0;
  *   n_own         host array: 0 (the history alone) or n_q .. 2^20;
- *   capacity      host array: tokens from one KV head to the next, >= n_own;
+ *   capacity      host array: tokens from one KV head to the next, n_own .. 2^20 (not read
+ *                 when n_own is 0);
  *   parents       NULL, or a host array of device pointers to int32 [n_q], each of
  *                 which may be NULL.  NULL: query i sees the own tokens up to
  *                 itself.  Else the queries are a tree of drafted tokens (at most
