@@ -314,9 +314,10 @@ __device__ __forceinline__ int value_swizzle(int r) {
 // What bounds it.  Few columns: reading keys and values (one token over 705,600 rows of 4
 // KV heads, d 128: 219 to 240 us, 6.0 to 6.6 TB/s; WQ = 1: each wave loads what it reads, no
 // barriers).
-// Many columns: the matrix unit and the power it may draw (1,024 tokens of 28 heads over
-// 117,600 rows: 1.44 to 1.53 ms, 1.1 to 1.2 PFLOP/s by card; a block's tile of 64 keys x 256 columns takes
-// 3,200 clocks, 2,048 of them matrix work, at the 1.5 to 1.8 GHz the card then holds).
+// Many columns: the matrix unit and the power that the card may draw under it (1,024 tokens of 28 heads over
+// 117,600 rows: 1.44 to 1.54 ms, 1.1 to 1.2 PFLOP/s by card; a block's tile of 64 keys x 256 columns takes
+// 3,200 clocks, 2,048 of them matrix work: it is busy for 62% of the clocks, a large library product for 70%, both
+// at 1.6 to 1.75 GHz).
 // Between, blocks of four waves, two a CU: one's softmax runs beside the other's products and
 // loads (56 columns over 705,600 rows, 4 KV heads, d 128: 251 us with one block of eight, 224; 112
 // columns 303 -> 284; at d 64 one block of eight waves and tiles of 128 keys keep up to 64 columns: 125 us, 140).
@@ -885,7 +886,8 @@ __global__ __launch_bounds__(256) void k_join(AttendArgs a) {
 // to the workspace and k_add adds them in order.
 // One token: bound by reading the keys, which a block without a map takes through LDS in
 // whole lines (705,600 rows of 4 KV heads, d 128: 116 to 119 us, 6.1 TB/s).  More: by cap,
-// bias and exp on the vector unit (32 tokens of 28 heads, 117,600 rows, 105 M scores: 56 us).
+// bias and exp on the vector unit for 59% of the time (32 tokens of 28 heads, 117,600 rows, 105 M scores: 56
+// us); the rest are products and LDS reads that a wave does not overlap with them.
 template <int D, int PM, int NW, bool MAP>
 __global__ __launch_bounds__(64 * NW) void k_accumulate(AttendArgs a, float decay) {
   constexpr int RB = D * 2, CH = D / 8, KST = D / 16;
