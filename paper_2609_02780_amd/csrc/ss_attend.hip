@@ -587,17 +587,18 @@ __global__ __launch_bounds__(64 * WQ * WK, 2) void k_attend(AttendArgs a) {
       }
       cs = 1.0f;
     } else if (!MAP && WQ < 8 && a.slopes) {      // (the widest tiling takes the map: its loop is 1.3% shorter for it)
-      // frames of rpf rows: a group of 32 keys starts at row `rem` of its frame
-      const float inv = 1.0f / (float)rpf;
+      // frames of rpf rows: a group of 32 keys starts at row `rem` of its frame.  Each score meets its own
+      // frame's bias (that of the group's first frame and a step back would round at the larger one)
+      const float inv = 1.0f / (float)rpf, slope = hist ? slope2 : 0.0f;
 #pragma unroll
       for (int u = 0; u < SUB; ++u) {
         const int jb = j0 + (wk + u * WK) * 32, f0 = jb / rpf, rem = jb - f0 * rpf + 4 * half;
-        const float b0 = hist ? -slope2 * (float)(age0 - f0) : 0.0f, step = hist ? slope2 : 0.0f;
+        const float age = (float)(age0 - f0), b0 = -slope * age, b1 = -slope * (age - 1.0f);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int x = rem + 8 * (i >> 2) + (i & 3);          // below rpf + 32
-          const float on = rpf >= 32 ? (x >= rpf ? step : 0.0f) : step * floorf(((float)x + 0.5f) * inv);
-          sv[u * 16 + i] = fmaf(sv[u * 16 + i], cs, b0) + on;
+          const float b = rpf >= 32 ? (x >= rpf ? b1 : b0) : -slope * (age - floorf(((float)x + 0.5f) * inv));
+          sv[u * 16 + i] = fmaf(sv[u * 16 + i], cs, b);
         }
       }
       cs = 1.0f;

@@ -346,3 +346,34 @@ def test_rows_beyond_the_caches(heads):
             for fr in (None, every):
                 att.accumulate(0, [dev(q)], runs[0][1], frames=fr, decay=0.0)
                 assert (np.abs(ix.weights[0].double().cpu().numpy() - w) <= bw).all()
+
+
+@pytest.mark.parametrize("rows", [1, 2, 7, 16, 31, 32, 40])
+@pytest.mark.parametrize("heads", [(4, 2, 64), (28, 4, 128)], ids=str)
+def test_steep_bias(heads, rows):
+    """Under a steep bias the newest frame takes all weight, and its score is as precise as a product
+    of its own age: not rounded at the bias of the older frames that share its group of 32 keys.
+
+    To first order an error e_j of q.k moves the log of the sum by sum_j p_j e_j, which is doubled
+    here; its sum adds n + 64 roundings.  At the magnitude of the bias there are at most 7: of log2 e,
+    of the slope in units of log 2, of the bias, of the biased score, of maximum + log2 of the sum, of
+    ln 2 and of the product with it."""
+    import paper_2609_02780_amd as P
+    rng = np.random.default_rng([heads[0], rows])
+    st = Stream(rng, heads, [(96, rows)])                # whole groups of 32 rows: their last row is the newest
+    q = bf(rng, heads[0], 3, heads[2])
+    k, v, _, age = st.seen(0)
+    for slope in (0.7, 30.0, 300.0):
+        slopes = np.full(heads[0], slope, np.float32)
+        log("case", heads, rows, slope)
+        out, lse = P.HistoryAttention([st.ix], slopes=torch.from_numpy(slopes).cuda())(0, [dev(q)])
+        for h in range(heads[0]):
+            s, err = R.scores(R.f64(q[h]), k[h // (heads[0] // heads[1])], 0.0, None, None)
+            s = s - float(slopes[h]) * age
+            m = s.max(1, keepdims=True)
+            p = np.exp(s - m)
+            z = p.sum(1)
+            ref = m[:, 0] + np.log(z)
+            tol = 2 * (p * err).sum(1) / z + (len(age) + 64) * R.U + 7 * R.U * (np.abs(ref) + 1)
+            got = lse[0][h].double().cpu().numpy()
+            assert (np.abs(got - ref) <= tol).all(), (slope, h, float((np.abs(got - ref) / tol).max()))
