@@ -377,3 +377,47 @@ def test_steep_bias(heads, rows):
             tol = 2 * (p * err).sum(1) / z + (len(age) + 64) * R.U + 7 * R.U * (np.abs(ref) + 1)
             got = lse[0][h].double().cpu().numpy()
             assert (np.abs(got - ref) <= tol).all(), (slope, h, float((np.abs(got - ref) / tol).max()))
+
+
+@pytest.mark.parametrize("heads,nq", [((4, 2, 64), 1), ((28, 4, 128), 17), ((16, 1, 64), 60), ((8, 8, 128), 200)], ids=str)
+def test_without_lse(heads, nq):
+    """A C caller may leave the logs out: the outputs are the same."""
+    import paper_2609_02780_amd as P
+    rng = np.random.default_rng([heads[0], nq])
+    st = Stream(rng, heads, [(21, 33)])
+    q = dev(bf(rng, heads[0], nq, heads[2], scale=1.5))
+    att = P.HistoryAttention([st.ix])
+    expected = att(0, [q])[0][0]
+    out, lib, nqs, prm = torch.full_like(expected, 5.0), P.lib(), (C.c_int32 * 1)(nq), att._params(0, None, None)
+    need = lib.ss_attend_workspace_bytes(att._handles, 1, nqs, None, C.byref(prm))
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    assert lib.ss_attend(att._handles, 1, (C.c_void_p * 1)(q.data_ptr()), nqs, None, C.byref(prm), ws.data_ptr(), need,
+                         torch.cuda.current_stream().cuda_stream, (C.c_void_p * 1)(out.data_ptr()), None) == 0
+    assert torch.equal(out, expected)
+
+
+@pytest.mark.parametrize("nq", [2, 90])
+def test_three_groups_of_streams_with_lists(nq):
+    """33 streams with frames of two sizes, lists, cap and bias: attention and decayed weights."""
+    import paper_2609_02780_amd as P
+    rng = np.random.default_rng(nq)
+    sts = [Stream(rng, (4, 2, 64), [(1 + s % 5, 1 + s), (2, 9)]) for s in range(33)]
+    qs = [bf(rng, 4, nq + s % 3, 64, scale=1.5) for s in range(33)]
+    qd, slopes = [dev(q) for q in qs], np.linspace(-0.05, 0.3, 4).astype(np.float32)
+    lists = rng.integers(-1, 9, (33, 5))
+    frames = torch.from_numpy(lists).cuda()
+    att = P.HistoryAttention([x.ix for x in sts], 12.0, torch.from_numpy(slopes).cuda())
+    out, lse = att(0, qd, frames=frames)
+    for x in sts:
+        x.ix.weights.fill_(2.0)
+    att.accumulate(0, qd, lse, frames=frames, decay=0.5)
+    for s, x in enumerate(sts):
+        seen, s64 = lists[s].tolist(), slopes.astype(np.float64)
+        check((out[s], lse[s]), want(x, 0, qs[s], None, None, seen, 0, 12.0, s64), s)
+        k, _, keep, age = x.seen(0, seen)
+        w, b = R.weights(R.f64(qs[s]), k, lse[s].cpu().numpy(), 2, 12.0, s64, age)
+        ref = np.ones((2, len(keep)))
+        tol = np.full_like(ref, 4 * R.U)
+        ref[:, keep] += w
+        tol[:, keep] += b + 2 * R.U * (w + 1)
+        assert (np.abs(x.ix.weights[0].double().cpu().numpy() - ref) <= tol).all(), s
