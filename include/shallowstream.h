@@ -559,6 +559,132 @@ ss_status ss_attend_accumulate(ss_index* const* idx, int32_t n_streams, const vo
  * SS_ERR_DEVICE dst must be discarded. */
 ss_status ss_index_evict(const ss_index* src, ss_index* dst, int64_t frame_hi, int32_t keep_rows, void* stream);
 
+/* Rotary positions.  The first `dims` elements of a row are dims/2 pairs (a, b), which
+ * at position t become
+ *   a' = gain (a cos x - b sin x),   b' = gain (b cos x + a sin x),   x = 2 pi t freqs[i];
+ * the others are copied.  Pairs are (i, i + dims/2), or with `interleaved` (2i, 2i + 1).
+ *   freqs  device double [dims/2], turns a position (ss_rotary_freqs makes them);
+ *   dims   even, 2 .. d.
+ * ss_rotary_freqs writes, on the host, freqs[i] = f_i / 2 pi with f_i = base^(-2i/dims),
+ * and *gain = 1.  Scaled for contexts `factor` times (1..2^20) as long: f_i / factor; or,
+ * when `original` (the length that the model was trained at) is above 0, by parts
+ * (Peng et al. 2023): with r = original f_i / 2 pi turns over that length and
+ * c = (r - slow) / (fast - slow) held in 0..1, f_i (c + (1 - c) / factor), and
+ * *gain = 1 + 0.1 ln(factor).  0 <= slow < fast (32 and 1 there); base > 1. */
+typedef struct {
+  const double* freqs;
+  int32_t dims;
+  int32_t interleaved;
+  float gain;
+} ss_rotary;
+ss_status ss_rotary_freqs(int32_t dims, double base, double factor, double original, double fast, double slow,
+                          double* freqs, float* gain);
+
+/* Rows of several heads, bf16 [heads][tokens][d] with d side by side: `data` is a
+ * device pointer (16-byte aligned), the strides count elements, are multiples of 8
+ * (16 bytes) and not negative. */
+typedef struct {
+  void* data;
+  int64_t head_stride;
+  int64_t token_stride;
+} ss_rows;
+
+/* Rotate n_tokens (1..65536) rows of n_heads (1..4096) heads.  positions: device int64
+ * [n_tokens], below 2^31 in magnitude.  With `transposed` the transposed rotation (-sin), which is the
+ * gradient of the other one, and undoes it when gain is 1.  `out` may be x, rows
+ * and strides alike; else they may not overlap. */
+ss_status ss_rotate(const ss_rotary* rotary, int32_t n_heads, int32_t n_tokens, int32_t head_dim, const ss_rows* x,
+                    const int64_t* positions, int32_t transposed, const ss_rows* out, void* stream);
+
+/* A paged cache of keys and values in 8 bits, for any number of layers and streams.
+ * Tokens are kept in blocks of 32.  A full block is a page: e4m3 codes with one fp32
+ * scale for each KV head's keys and one for its values; value = code * scale,
+ *   a = max(largest magnitude, 2^-100), scale = a / 448, code = e4m3(x * (448 / a)).
+ * The tokens behind a stream's last full block stay in bf16, in the stream's slot.
+ *   n_layers 1..1024; heads and head_dim as in ss_index_desc; n_pages 1..2^31-1 (a page
+ *   holds a block at every layer); n_slots 1..2^20, the streams open at one time.
+ * Layout of the arena (each part 256-byte aligned): key codes [L][n_pages][H_kv][32 d],
+ * value codes, key scales fp32 [L][n_pages][H_kv], value scales, open keys bf16
+ * [L][n_slots][2][H_kv][32 d], open values.  Inside a page (and an open block):
+ *   keys    [d/16][32 tokens][16];
+ *   values  [d/32][2][32][16]: place (c, h, m, 8 x + 4 y + e), x, y in 0..1, e in 0..3, is
+ *           dimension 32 c + m of token 16 y + 8 x + 4 h + e.
+ * A caller may read and write the arena between calls; the library writes it in
+ * ss_cache_append alone, and creation leaves it as it is. */
+typedef struct ss_cache ss_cache; /* opaque, host-side handle */
+typedef struct {
+  int32_t n_layers;
+  int32_t n_q_heads;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+  int64_t n_pages;
+  int32_t n_slots;
+} ss_cache_desc;
+size_t ss_cache_required_bytes(const ss_cache_desc* desc); /* 0 if `desc` is invalid */
+ss_status ss_cache_create(const ss_cache_desc* desc, void* dev_arena, size_t arena_bytes, ss_cache** out);
+ss_status ss_cache_destroy(ss_cache* cache);
+
+/* The streams of a call, all in device memory, so that a captured call follows them:
+ *   tables   int32 [n_streams][width]: block b of stream s is page tables[s][b].  Streams
+ *            may share pages that both only read;
+ *   lengths  int32 [n_streams]: the stream's tokens, those of this call among them.  At
+ *            most 32 width + 31 count (the last 31 need no page); below 0 counts as 0;
+ *   slots    int32 [n_streams]: where the stream's open block lies, different ones for the
+ *            streams of an append;
+ *   n_streams 1..512, width 1..2^26-1.
+ * A page outside 0 .. n_pages-1 is not written, and its tokens are not seen; nor are
+ * those of an open block in a slot outside 0 .. n_slots-1. */
+typedef struct {
+  const int32_t* tables;
+  const int32_t* lengths;
+  const int32_t* slots;
+  int32_t n_streams;
+  int32_t width;
+} ss_cache_streams;
+
+/* Append tokens to every stream at one layer: stream s gets the next n_new[s] (host
+ * array, 0 and more; NULL: n_tokens / n_streams each) of the n_tokens (1..65536) rows,
+ * as its last lengths[s] - n_new[s] .. lengths[s] - 1.  (A stream with fewer tokens than
+ * n_new[s] gets its last ones; the rows of the others are passed over.)
+ *   keys, values  n_kv_heads heads;
+ *   rotary        NULL: keys are stored as they come;
+ *   positions     device int64 [n_tokens], or NULL: a token's place in its stream;
+ *   queries       NULL, or n_q_heads heads, which are rotated alike into queries_out (may
+ *                 be queries, rows and strides alike); rows that are passed over are not written.
+ * A key is rotated in fp32 and rounded to bf16 once; a block that becomes full is formed
+ * from the bf16 rows, so the cache does not depend on how its tokens were cut into calls.
+ * Open rows of block b lie in half b & 1 of the slot.  The rows of the block that a call
+ * begins in stay there too, unless the call ends an even number of blocks (2, 4, ...)
+ * later: a call of at most 32 tokens a stream can be taken back, wholly or in
+ * part, by lowering lengths, and repeated.  Rows must be finite. */
+ss_status ss_cache_append(ss_cache* cache, const ss_cache_streams* streams, int32_t layer, int32_t n_tokens,
+                          const int32_t* n_new, const ss_rows* keys, const ss_rows* values, const ss_rotary* rotary,
+                          const int64_t* positions, const ss_rows* queries, const ss_rows* queries_out, void* stream);
+
+/* Attention over a layer of the cache.  The n_q[s] queries (NULL: n_tokens / n_streams each)
+ * of stream s are its last tokens: query i sees the tokens up to lengths[s] - n_q[s] + i, of
+ * those the newest `window` (1..2^30; 0: all).  With s_j = q.k_j / sqrt(d)
+ *   out = sum_j p_j v_j,  p = softmax of s,  lse = ln sum_j exp(s_j).
+ *   queries, out  n_q_heads heads; query head h reads KV head h / G;
+ *   lse           NULL, or device fp32 [n_q_heads][n_tokens];
+ *   prior_out, prior_lse  both or neither: out and lse of the same queries over other
+ *                 rows (of ss_attend, say), with which the result is joined:
+ *                 out = (e^lse out + e^prior_lse prior_out) / (e^lse + e^prior_lse); a prior_out
+ *                 whose prior_lse is -inf is not read;
+ *   ws            device workspace of ss_cache_attend_workspace_bytes() bytes (256-byte
+ *                 aligned), which the call leaves dirty: calls that may overlap need one each,
+ *                 unless the size is 256, the least: those calls write nothing to it.
+ * out and lse may overlap nothing that is read.  A query that sees nothing gives out = 0 and
+ * lse = -inf.  Maxima, sums and outputs are fp32 until the one rounding at the end; p is
+ * rounded to bf16 before it meets the values.  Seen rows must be finite; rows behind a
+ * stream's end may hold anything.  A result is the same bit for bit each time. */
+size_t ss_cache_attend_workspace_bytes(const ss_cache* cache, const ss_cache_streams* streams, int32_t n_tokens,
+                                       const int32_t* n_q, int32_t window);
+ss_status ss_cache_attend(const ss_cache* cache, const ss_cache_streams* streams, int32_t layer, int32_t n_tokens,
+                          const int32_t* n_q, const ss_rows* queries, int32_t window, const ss_rows* prior_out,
+                          const float* prior_lse, void* ws, size_t ws_bytes, void* stream, const ss_rows* out,
+                          float* lse);
+
 /* Every score of one list over rows [row0, row0+n_rows) of one index, with the
  * same arithmetic as ss_retrieve (parity only).  queries: host array of L_s
  * device pointers as in ss_retrieve.  out: device fp32 [n_rows].  With

@@ -7,6 +7,7 @@ The work runs in ``libshallowstream.so`` (HIP kernels behind the C ABI of
 from ._lib import SSError, lib  # noqa: F401
 from .index import (HistoryAttention, LongClusters, PooledRanker, Retriever, ShallowIndex,  # noqa: F401
                     assemble_evidence, sample_plan, set_profile_events)
+from .paged import PagedBatch, PagedCache, Rotary  # noqa: F401
 
-__all__ = ["ShallowIndex", "Retriever", "PooledRanker", "LongClusters", "HistoryAttention", "assemble_evidence",
-           "SSError", "sample_plan", "set_profile_events", "lib"]
+__all__ = ["ShallowIndex", "Retriever", "PooledRanker", "LongClusters", "HistoryAttention", "Rotary", "PagedCache",
+           "PagedBatch", "assemble_evidence", "SSError", "sample_plan", "set_profile_events", "lib"]

@@ -71,7 +71,26 @@ class OwnTokens(C.Structure):
                 ("parents", C.c_void_p)]
 
 
+class Rotary(C.Structure):
+    _fields_ = [("freqs", C.c_void_p), ("dims", C.c_int32), ("interleaved", C.c_int32), ("gain", C.c_float)]
+
+
+class Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("head_stride", C.c_int64), ("token_stride", C.c_int64)]
+
+
+class CacheDesc(C.Structure):
+    _fields_ = [("n_layers", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("n_pages", C.c_int64), ("n_slots", C.c_int32)]
+
+
+class CacheStreams(C.Structure):
+    _fields_ = [("tables", C.c_void_p), ("lengths", C.c_void_p), ("slots", C.c_void_p), ("n_streams", C.c_int32),
+                ("width", C.c_int32)]
+
+
 _P = C.c_void_p
+_ROWS = C.POINTER(Rows)
 _SIGS = {
     "ss_index_required_bytes": (C.c_size_t, [C.POINTER(IndexDesc)]),
     "ss_index_create": (C.c_int32, [C.POINTER(IndexDesc), _P, C.c_size_t, C.POINTER(_P)]),
@@ -123,6 +142,18 @@ _SIGS = {
     "ss_attend_accumulate": (C.c_int32, [C.POINTER(_P), C.c_int32, C.POINTER(_P), C.POINTER(C.c_int32),
                                          C.POINTER(_P), C.POINTER(AttendParams), C.c_float, _P, C.c_size_t, _P]),
     "ss_index_evict": (C.c_int32, [_P, _P, C.c_int64, C.c_int32, _P]),
+    "ss_rotary_freqs": (C.c_int32, [C.c_int32, C.c_double, C.c_double, C.c_double, C.c_double, C.c_double, _P,
+                                    C.POINTER(C.c_float)]),
+    "ss_rotate": (C.c_int32, [C.POINTER(Rotary), C.c_int32, C.c_int32, C.c_int32, _ROWS, _P, C.c_int32, _ROWS, _P]),
+    "ss_cache_required_bytes": (C.c_size_t, [C.POINTER(CacheDesc)]),
+    "ss_cache_create": (C.c_int32, [C.POINTER(CacheDesc), _P, C.c_size_t, C.POINTER(_P)]),
+    "ss_cache_destroy": (C.c_int32, [_P]),
+    "ss_cache_append": (C.c_int32, [_P, C.POINTER(CacheStreams), C.c_int32, C.c_int32, C.POINTER(C.c_int32), _ROWS,
+                                    _ROWS, C.POINTER(Rotary), _P, _ROWS, _ROWS, _P]),
+    "ss_cache_attend_workspace_bytes": (C.c_size_t, [_P, C.POINTER(CacheStreams), C.c_int32, C.POINTER(C.c_int32),
+                                                     C.c_int32]),
+    "ss_cache_attend": (C.c_int32, [_P, C.POINTER(CacheStreams), C.c_int32, C.c_int32, C.POINTER(C.c_int32), _ROWS,
+                                    C.c_int32, _ROWS, _P, _P, C.c_size_t, _P, _ROWS, _P]),
     "ss_debug_sample_plan": (C.c_int32, [C.c_int64, C.c_int32, C.POINTER(C.c_int32)]),
     "ss_set_profile_events": (C.c_int32, [_P, _P]),
     "ss_status_string": (C.c_char_p, [C.c_int32]),

@@ -3,6 +3,7 @@
 // any HIP call, so invalid calls leave the index and the device untouched.
 #include "../../include/shallowstream.h"
 #include "ss_internal.h"
+#include "ss_paged.h"
 
 #include <hip/hip_runtime.h>
 
@@ -950,6 +951,11 @@ struct ss_clusters {
   ss_cluster_desc desc;
   ss::ClusterDev dev;
 };
+
+int32_t ss_fail_text(int32_t st, const char* text) {
+  std::snprintf(g_err, sizeof g_err, "%s", text);
+  return st;
+}
 
 extern "C" {
 

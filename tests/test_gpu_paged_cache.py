@@ -1,0 +1,372 @@
+"""Rotary positions, appending to a paged 8-bit cache and attention over it, against the
+64-bit forms of ``paged_ref``."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paged_ref as R
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+HEADS = [(4, 2, 64), (28, 4, 128), (16, 1, 128), (3, 1, 64), (8, 8, 128)]
+
+
+def normal(seed, *shape, scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(*shape, generator=g) * scale).to(torch.bfloat16)
+
+
+# --------------------------------------------------------------------------
+# rotation
+# --------------------------------------------------------------------------
+
+def check_turn(got, x, want):
+    """fp32 products of cos and sin that are off by less than 2^-20 (angle and functions), one rounding to bf16."""
+    size = x.abs().amax(-1, keepdim=True) * 2.0 ** -19 * 2
+    assert torch.isfinite(got).all()
+    bad = (got.double().cpu() - want).abs() - (2.0 ** -8 * want.abs() + size + 1e-37)
+    assert bad.max() <= 0, float(bad.max())
+
+
+@pytest.mark.parametrize("d,dims", [(64, 64), (128, 128), (128, 64), (128, 96), (64, 2), (128, 20), (64, 62), (128, 126)])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rotation_of_part_of_the_head(d, dims, interleaved):
+    import paper_2609_02780_amd as P
+    for n, heads, transposed in ((1, 3, False), (33, 5, True)):
+        x = normal(n, heads, n, d)
+        pos = torch.arange(n) * 977 + 12345
+        rot = P.Rotary(dims, interleaved=interleaved)
+        got = rot(x.to(DEV), pos.to(DEV), transposed=transposed)
+        f, gain = R.frequencies(dims)
+        check_turn(got, x.double(), R.rotate(x.double(), pos, f, gain, interleaved, transposed))
+        assert torch.equal(got[..., dims:].cpu(), x[..., dims:])
+
+
+@pytest.mark.parametrize("factor,original", [(4.0, 0), (4.0, 4096), (2.5, 32768)])
+def test_scaled_far_and_negative_positions(factor, original):
+    import paper_2609_02780_amd as P
+    x = normal(7, 4, 6, 128)
+    pos = torch.tensor([0, 1, -5, 2 ** 31 - 1, -2 ** 31 + 1, 700_001])
+    rot = P.Rotary(128, base=500000.0, factor=factor, original=original)
+    f, gain = R.frequencies(128, 500000.0, factor, original)
+    assert rot.gain == pytest.approx(gain, rel=1e-6)
+    got = rot(x.to(DEV), pos.to(DEV))
+    check_turn(got, x.double() * gain, R.rotate(x.double(), pos, f, gain))
+
+
+def test_rotation_strides_in_place_and_back():
+    import paper_2609_02780_amd as P
+    x = normal(3, 70, 6, 64)                      # token by token
+    pos = torch.arange(70, device=DEV)
+    rot = P.Rotary(64)
+    f, gain = R.frequencies(64)
+    t = x.to(DEV).transpose(0, 1)
+    want = R.rotate(x.transpose(0, 1).double(), range(70), f)
+    got = rot(t, pos)
+    assert got.stride() == t.stride()
+    check_turn(got, x.transpose(0, 1).double(), want)
+    # a slice of a wider projection, into a row of a larger tensor
+    wide = torch.zeros(70, 10, 64, dtype=torch.bfloat16, device=DEV)
+    wide[:, 2:8] = t.transpose(0, 1)
+    out = torch.full((6, 75, 64), 7.0, dtype=torch.bfloat16, device=DEV)
+    assert rot(wide[:, 2:8].transpose(0, 1), pos, out=out[:, :70]).data_ptr() == out.data_ptr()
+    assert torch.equal(out[:, :70], got) and (out[:, 70:] == 7.0).all()
+    same = t.clone()
+    assert rot(same, pos, out=same) is same
+    assert torch.equal(same, got)
+    back = rot(same, pos, transposed=True)
+    # two roundings of bf16 of the row's pairs
+    err = (back.double() - t.double()).abs().amax()
+    assert err <= 2 * 2.0 ** -8 * math.sqrt(2) * t.double().abs().amax()
+    # the gradient of sum(w * rot(x)) is the transposed rotation of w
+    w = normal(9, 6, 70, 64)
+    a = (w.double() * R.rotate(x.transpose(0, 1).double(), range(70), f)).sum()
+    b = (R.rotate(w.double(), range(70), f, transposed=True) * x.transpose(0, 1).double()).sum()
+    assert abs(a - b) <= 1e-9 * abs(a) + 1e-9
+
+
+# --------------------------------------------------------------------------
+# a cache and what stands beside it
+# --------------------------------------------------------------------------
+
+class Rig:
+    """A cache with streams whose pages and slots are in a mixed order, and the rows they should hold."""
+
+    def __init__(self, heads, streams, width, layers=2, layer=1, seed=1, spare=3):
+        import paper_2609_02780_amd as P
+        self.Hq, self.Hk, self.d = heads
+        self.S, self.width, self.layer = streams, width, layer
+        rng = np.random.default_rng(seed)
+        n = streams * width
+        self.cache = P.PagedCache(layers, *heads, n + spare, streams + 2)
+        self.cache.arena.fill_(0xFF)                # NaN wherever nothing was written
+        self.pages = rng.permutation(n + spare)[:n].reshape(streams, width).astype(np.int32)
+        self.slot = rng.permutation(streams + 2)[:streams].astype(np.int32)
+        self.tables = torch.from_numpy(self.pages.copy()).to(DEV)
+        self.lengths = torch.zeros(streams, dtype=torch.int32, device=DEV)
+        self.slots = torch.from_numpy(self.slot.copy()).to(DEV)
+        self.batch = P.PagedBatch(self.cache, self.tables, self.lengths, self.slots)
+        self.ref = [R.Stream(self.Hk, self.d) for _ in range(streams)]
+        self.seed = seed
+
+    def rows(self, n):
+        """Rows of n new tokens, head by head or token by token."""
+        self.seed += 1
+        k, v = normal(self.seed, self.Hk, n, self.d, scale=1.5), normal(self.seed + 1000, self.Hk, n, self.d)
+        k[..., 5] *= 8.0
+        return k, v
+
+    def add(self, counts, **kw):
+        """Append counts[s] tokens to each stream."""
+        n = sum(counts)
+        k, v = self.rows(n)
+        self.lengths += torch.tensor(counts, dtype=torch.int32, device=DEV)
+        q = self.batch.append(self.layer, k.to(DEV), v.to(DEV), n_new=counts, **kw)
+        at = 0
+        for s, c in enumerate(counts):
+            self.ref[s].add(k[:, at:at + c].double(), v[:, at:at + c].double())
+            at += c
+        return q
+
+    def stored(self):
+        """Per stream the cache's rows as values, keys and values [H][length][d]."""
+        c, out = self.cache, []
+        kp = c.keys[self.layer].cpu().float().reshape(-1, self.Hk, 32, self.d)
+        vp = c.values[self.layer].cpu().float().reshape(-1, self.Hk, 32, self.d)
+        ks, vs = c.key_scales[self.layer].cpu(), c.value_scales[self.layer].cpu()
+        ko = c.open_keys[self.layer].cpu().reshape(-1, 2, self.Hk, 32, self.d)
+        vo = c.open_values[self.layer].cpu().reshape(-1, 2, self.Hk, 32, self.d)
+        for s, L in enumerate(self.lengths.cpu().tolist()):
+            full, tail = divmod(L, 32)
+            got = []
+            for pages, scale, open_ in ((kp, ks, ko), (vp, vs, vo)):
+                ids = self.pages[s, :full]
+                x = (pages[ids] * scale[ids][..., None, None]).transpose(0, 1).reshape(self.Hk, full * 32, self.d)
+                got.append(torch.cat([x, open_[self.slot[s], full & 1, :, :tail].float()], 1).double())
+            out.append(got)
+        return out
+
+    def check_stored(self):
+        for s, (got, ref) in enumerate(zip(self.stored(), self.ref)):
+            for name, x, y in zip("kv", got, ref.held()):
+                assert x.shape == y.shape, (s, name)
+                assert torch.equal(x.float(), y.float()), (s, name, float((x - y).abs().max()))
+
+
+def check_attend(rig, counts, window=0, prior=None, seen=None, q=None, uniform=False, major=False):
+    n = sum(counts)
+    if q is None:
+        q = normal(rig.seed + 77, rig.Hq, n, rig.d, scale=1.5)
+    dev = q.to(DEV)
+    if major:
+        dev = dev.transpose(0, 1).contiguous().transpose(0, 1)
+    pr = None if prior is None else (prior[0].to(DEV), prior[1].to(DEV))
+    out, lse = rig.batch.attend(rig.layer, dev, n_q=None if uniform else counts, window=window, prior=pr)
+    again, lse2 = rig.batch.attend(rig.layer, dev, n_q=None if uniform else counts, window=window, prior=pr)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+    assert out.stride() == dev.stride()
+    at = 0
+    for s, c in enumerate(counts):
+        k, v = rig.ref[s].held()
+        sl = slice(at, at + c)
+        at += c
+        if c == 0:
+            continue
+        p64 = None if prior is None else (prior[0][:, sl].double(), prior[1][:, sl].double())
+        want, wlse, size, top = R.attend(q[:, sl].double(), k, v, k.shape[1], window,
+                                         None if seen is None else seen[s], p64)
+        tol, ltol = R.bounds(want, wlse, size, top, rig.d)
+        got, glse = out[:, sl].cpu().double(), lse[:, sl].cpu().double()
+        assert torch.isfinite(got).all(), s
+        assert ((got - want).abs() <= tol).all(), (s, float(((got - want).abs() / tol).max()))
+        none = torch.isinf(wlse)
+        assert torch.equal(torch.isinf(glse) & (glse < 0), none), s
+        assert (got[none] == 0).all()
+        off = (glse - wlse).abs()[~none] - ltol[~none]
+        assert none.all() or off.max() <= 0, (s, float(off.max()))
+    return out, lse
+
+
+# --------------------------------------------------------------------------
+# append
+# --------------------------------------------------------------------------
+
+@pytest.mark.parametrize("heads", HEADS)
+def test_append_holds_what_the_definition_says(heads):
+    rig = Rig(heads, 4, 4)
+    for counts in ([1, 0, 31, 32], [1, 33, 1, 1], [30, 31, 64, 0], [5, 1, 0, 70], [1, 1, 1, 1]):
+        rig.add(counts)
+        rig.check_stored()
+
+
+def test_append_does_not_depend_on_the_cuts_and_writes_nothing_else():
+    heads, total = (16, 4, 64), 131
+    got = []
+    for cuts in ([131], [1] * 131, [31, 1, 1, 63, 35], [64, 67], [20, 70, 41]):
+        rig = Rig(heads, 2, 5, seed=5)
+        k, v = normal(1, 4, 2 * total, 64), normal(2, 4, 2 * total, 64)
+        k, v = k.reshape(4, 2, total, 64).to(DEV), v.reshape(4, 2, total, 64).to(DEV)
+        at = 0
+        import paper_2609_02780_amd as P
+        rot = P.Rotary(48, interleaved=True)
+        for n in cuts:
+            rig.lengths += n
+            rig.batch.append(rig.layer, k[:, :, at:at + n].reshape(4, 2 * n, 64), v[:, :, at:at + n].reshape(4, 2 * n, 64),
+                             rotary=rot)
+            at += n
+        got.append(rig.stored())
+        # the other layer, the pages behind the last full block and the spare ones are as they were
+        c = rig.cache
+        other = c.keys[0].reshape(c.n_pages, -1).view(torch.uint8)
+        assert (other == 0xFF).all()
+        used = {int(p) for s in range(2) for p in rig.pages[s, :total // 32]}
+        rest = [p for p in range(c.n_pages) if p not in used]
+        for t in (c.keys, c.values):
+            assert (t[rig.layer].reshape(c.n_pages, -1)[rest].view(torch.uint8) == 0xFF).all()
+        for t in (c.open_keys, c.open_values):
+            o = t[rig.layer].reshape(c.n_slots, 2, 4, 32, 64).view(torch.int16)
+            free = [s for s in range(c.n_slots) if s not in rig.slot]
+            assert (o[free] == -1).all()
+            assert (o[rig.slot.tolist(), 0][:, :, total % 32:] == -1).all() or len(cuts) > 1
+    for other in got[1:]:
+        for a, b in zip(got[0], other):
+            assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("heads", [(4, 2, 64), (28, 4, 128)])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_append_rotates_keys_and_queries(heads, interleaved):
+    import paper_2609_02780_amd as P
+    Hq, Hk, d = heads
+    rig = Rig(heads, 3, 4)
+    dims = d // 2
+    rot = P.Rotary(dims, interleaved=interleaved, factor=4.0, original=64)
+    f, gain = R.frequencies(dims, factor=4.0, original=64)
+    for counts, far in (([40, 1, 7], False), ([3, 31, 90], False), ([1, 1, 1], True)):
+        old = rig.lengths.cpu().tolist()
+        n = sum(counts)
+        q = normal(n, n, Hq, d).to(DEV).transpose(0, 1)
+        pos = np.concatenate([np.arange(o, o + c) for o, c in zip(old, counts)])
+        if far:
+            pos = pos + 650_000
+        before = [r.k.shape[1] for r in rig.ref]
+        got = rig.add(counts, rotary=rot, queries=q, positions=torch.from_numpy(pos).to(DEV) if far else None)
+        assert got.stride() == q.stride()
+        check_turn(got, q.cpu().double() * gain, R.rotate(q.cpu().double(), pos, f, gain, interleaved))
+        # the stored rows: rotated in 64 bits, off by the rotation's error and a rounding to bf16, then to e4m3 (2^-4
+        # of the value, half a step of 2^-9 near 0)
+        at = 0
+        for s, c in enumerate(counts):
+            k = rig.ref[s].k[:, before[s]:]
+            rig.ref[s].k[:, before[s]:] = R.rotate(k, pos[at:at + c], f, gain, interleaved)
+            at += c
+        for (gk, gv), ref in zip(rig.stored(), rig.ref):
+            want = ref.k
+            full = want.shape[1] // 32 * 32
+            size = want.abs().amax(-1, keepdim=True) * 2.0 ** -18
+            assert ((gk - want).abs()[:, full:] <= (2.0 ** -8 * want.abs() + size)[:, full:]).all()
+            for b in range(0, full, 32):
+                w = want[:, b:b + 32]
+                scale = w.abs().amax((1, 2), keepdim=True) / 448.0
+                tol = (2.0 ** -4 + 2.0 ** -7) * w.abs() + scale * 2.0 ** -9 + size[:, b:b + 32]
+                assert ((gk[:, b:b + 32] - w).abs() <= tol).all()
+            assert torch.equal(gv.float(), ref.held()[1].float())
+
+
+def test_tokens_can_be_taken_back_and_calls_repeated():
+    """The open rows of the block that a call began in stay."""
+    rig = Rig((4, 2, 64), 2, 6, seed=9)
+    rig.add([61, 30])
+    before = [(r.k.clone(), r.v.clone()) for r in rig.ref]
+    for drafts in (2, 5, 32):
+        rig.add([drafts, drafts])
+        rig.check_stored()
+        after = [(r.k, r.v) for r in rig.ref]
+        for back in (drafts, drafts - 1):
+            rig.lengths.copy_(torch.tensor([61 + drafts - back, 30 + drafts - back], dtype=torch.int32))
+            for r, (k, v) in zip(rig.ref, after):
+                n = k.shape[1] - back
+                r.k, r.v = k[:, :n], v[:, :n]
+            check_attend(rig, [1, 1])
+        rig.lengths.copy_(torch.tensor([61, 30], dtype=torch.int32))
+        for r, (k, v) in zip(rig.ref, before):
+            r.k, r.v = k, v
+    rig.add([40, 41])
+    rig.check_stored()
+
+
+def test_bad_pages_slots_and_lengths_are_passed_over():
+    """Pages and slots outside the cache are neither written nor seen; a stream that is shorter than its new
+    tokens gets the last of them; lengths below 0 are 0, beyond the table what it holds."""
+    rig = Rig((4, 2, 64), 4, 3, seed=11)
+    rig.tables[0, 1] = -1
+    rig.tables[1, 0] = rig.cache.n_pages
+    rig.slots[2] = rig.cache.n_slots
+    whole = rig.cache.arena.clone()
+    rig.add([70, 70, 70, 70])
+    seen = [torch.ones(70, dtype=torch.bool) for _ in range(4)]
+    seen[0][32:64] = False
+    seen[1][:32] = False
+    seen[2][64:] = False
+    check_attend(rig, [3, 70, 9, 1], seen=seen)
+    check_attend(rig, [1, 1, 1, 1], seen=seen, uniform=True)
+    bad = rig.cache.keys[1].reshape(rig.cache.n_pages, -1).view(torch.uint8)[rig.pages[0, 1]]
+    assert (bad == 0xFF).all()
+    assert not torch.equal(whole, rig.cache.arena)
+    # a length below the new tokens, and one below 0
+    rig = Rig((4, 2, 64), 2, 3, seed=12)
+    k, v = rig.rows(80)
+    rig.lengths.copy_(torch.tensor([35, -4], dtype=torch.int32))
+    rig.batch.append(1, k.to(DEV), v.to(DEV), n_new=[40, 40])
+    rig.ref[0].add(k[:, 5:40].double(), v[:, 5:40].double())
+    rig.lengths.clamp_min_(0)
+    rig.check_stored()
+    rig.lengths[1] = -7
+    check_attend(rig, [40, 2])
+    # more tokens than the table holds: the first 32 * 3 + 31 count
+    rig = Rig((4, 2, 64), 1, 3, seed=13)
+    rig.add([127])
+    rig.check_stored()
+    rig.lengths.fill_(2 ** 31 - 1)
+    check_attend(rig, [2])
+
+
+# --------------------------------------------------------------------------
+# attention
+# --------------------------------------------------------------------------
+
+@pytest.mark.parametrize("heads", HEADS)
+@pytest.mark.parametrize("window", [0, 1, 33, 100])
+def test_attention_of_short_streams(heads, window):
+    rig = Rig(heads, 7, 8)
+    rig.add([1, 31, 32, 33, 64, 95, 200])
+    check_attend(rig, [1] * 7, window=window, uniform=True)
+    check_attend(rig, [1, 2, 0, 33, 3, 70, 130], window=window, major=True)
+
+
+@pytest.mark.parametrize("heads", HEADS)
+@pytest.mark.parametrize("window", [0, 1500])
+def test_attention_in_shares(heads, window):
+    """Long tables are cut into shares, whatever the streams' lengths: units of one share, of many, none."""
+    rig = Rig(heads, 5, 80)
+    rig.add([2500, 0, 37, 1111, 1])
+    check_attend(rig, [1] * 5, window=window, uniform=True)
+    check_attend(rig, [2, 1, 2, 1, 1], window=window)
+    check_attend(rig, [130, 3, 37, 0, 1], window=window, major=True)
+
+
+@pytest.mark.parametrize("heads", [(28, 4, 128), (3, 1, 64)])
+def test_attention_joined_with_a_prior(heads):
+    Hq = heads[0]
+    rig = Rig(heads, 3, 50)
+    rig.add([1500, 0, 40])
+    for counts in ([1, 1, 1], [50, 3, 40]):
+        n = sum(counts)
+        po, pl = normal(4, Hq, n, heads[2]), torch.randn(Hq, n) * 2 + 5
+        pl[:, 0], po[:, 0] = -math.inf, math.nan
+        pl[0, counts[0]] = -math.inf                     # nothing seen on either side
+        pl[-1, -1] = 80.0                                 # all of it the prior's
+        check_attend(rig, counts, prior=(po, pl))
