@@ -74,7 +74,7 @@ struct PagedAttendArgs {
   Spans spans;
 };
 struct PagedAttendPlan {
-  int shape;                          // 0: up to 32 columns, 1: blocks of 128
+  int bm, round;                      // columns of a unit, blocks that its work is counted in
   int units, per, cols, n_wg, min_share;
   size_t o_bytes, ml_bytes, plan_bytes;
 };

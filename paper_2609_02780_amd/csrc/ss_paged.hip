@@ -15,6 +15,7 @@
 #include "ss_paged.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace ss {
 namespace {
@@ -48,12 +49,29 @@ __device__ __forceinline__ float other_half(float v) {
   return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
 }
 
-// Eight e4m3 as bf16 (exact).
-__device__ __forceinline__ u32x4 widen(uint32_t lo, uint32_t hi) {
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false);
-  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
-  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false);
-  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+__device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0,
+                                                 0, 0);
+}
+
+// A page's 16-byte pieces, read once (past the caches); of no page zeros, without a trip to memory.
+constexpr int kAuxNT = 2;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t page_bytes(const uint8_t* p, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), (short)0, bytes, 0x00020000);
+}
+__device__ __forceinline__ u32x4 load_shared(__amdgpu_buffer_rsrc_t r, int at) {     // other blocks read it too
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0));
+}
+__device__ __forceinline__ u32x4 load_piece(__amdgpu_buffer_rsrc_t r, int at) {
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, kAuxNT));
+}
+
+// Eight e4m3 times a power of two as bf16 (exact).
+__device__ __forceinline__ u32x4 widen(uint32_t lo, uint32_t hi, float scale) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
   return u32x4{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, c),
                __builtin_bit_cast(uint32_t, d)};
 }
@@ -461,167 +479,249 @@ __device__ __forceinline__ void finish(const PagedAttendArgs& a, int h, int at, 
   if (d == 0 && a.lse) a.lse[(int64_t)h * a.N + at] = l > 0.0f ? (m + log2_fast(l)) * kLn2 : neg_inf();
 }
 
-// Scores of 32 N keys by a lane's column -> p as the second product's operand.
-// v: sums of products; cs, lvs: for each block of 32 keys the score's and the value's
-// scale (the latter's log 2), rvs: 1 / value scale.  m moves only when it has to: as
-// long as a lane's p add up to at most 2^13, fp32 sums and bf16 p are as good against
-// an older, smaller m.  O is rescaled when m moves.
-template <int N, int DT>
-__device__ __forceinline__ void softmax_step(float (&v)[N * 16], const float (&lvs)[N], const float (&rvs)[N], float& m,
-                                             float& l, f32x16 (&O)[DT], u32x4 (&pb)[N * 2]) {
-  auto form = [&](float mu) -> float {
-    float all = 0.0f;
-#pragma unroll
-    for (int u = 0; u < N; ++u) {
-      const float off = lvs[u] - mu;
-      float p[16], sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        p[i] = exp2_fast(v[u * 16 + i] + off);
-        sum[i & 3] += p[i];
-      }
-#pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        bf16x8 x;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          x[e] = (__bf16)p[4 * w + e];
-          x[4 + e] = (__bf16)p[4 * w + 8 + e];
-        }
-        pb[u * 2 + w] = __builtin_bit_cast(u32x4, x);
-      }
-      all = fmaf((sum[0] + sum[1]) + (sum[2] + sum[3]), rvs[u], all);
-    }
-    return all;
-  };
+// exp2 of scores against m, as the second product's operand takes them.  v: scores in units of log 2; lvs: log 2
+// of the block's value scale, which p takes on (so values need no scaling), rvs: 1 / that scale.
+// m moves only when it has to: as long as a lane's p add up to at most 2^13, fp32 sums and bf16 p are
+// as good against an older, smaller m.  O is rescaled when m moves.  form(mu) forms all p against mu and
+// returns their sum without the value scale; top(): the largest score of the column.
+template <class Form, class Top, class Scale>
+__device__ __forceinline__ void running_softmax(float& m, float& l, Form&& form, Top&& top, Scale&& rescale) {
   float sum = form(m == neg_inf() ? 0.0f : m);
   if (__any(!(sum <= 8192.0f) || m == neg_inf())) {
-    float top = v[0];
-#pragma unroll
-    for (int i = 1; i < N * 16; ++i) top = fmaxf(top, v[i]);
-    top = fmaxf(top, other_half(top));
-    const float mn = fmaxf(m, top);
+    const float mn = fmaxf(m, top());
     const float al = m == neg_inf() ? 0.0f : exp2_fast(m - mn);
     m = mn;
     l *= al;
-#pragma unroll
-    for (int i = 0; i < DT; ++i) O[i] *= al;
+    rescale(al);
     sum = form(m == neg_inf() ? 0.0f : m);
   }
   l += sum;
 }
 
-// A lane's 16 keys of block b that its column (token `last`, the first seen `lowest`) does not see.
-__device__ __forceinline__ void hide(float* v, int b, int half, int last, int lowest) {
-  const int j0 = b * B + 4 * half;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int j = j0 + 8 * (i >> 2) + (i & 3);
-    if (j > last || j < lowest) v[i] = neg_inf();
-  }
+// A value scale is cut in two: p takes what lies in 2^-60 .. 2^60, the conversion of the
+// codes the rest, a power of two (blocks of zeros have the least scale, and their p must still count).
+struct ValueScale {
+  float log2, inverse, codes;
+};
+__device__ __forceinline__ ValueScale cut_scale(float vs) {
+  const int e = (int)(__float_as_uint(vs) >> 23) - 127;
+  const int k = e < -60 ? e + 60 : e > 60 ? e - 60 : 0;
+  const float in_p = vs * __uint_as_float((uint32_t)(127 - k) << 23);
+  return {log2_fast(in_p), 1.0f / in_p, __uint_as_float((uint32_t)(127 + k) << 23)};
 }
 
 // A lane's pieces of an open block: rows from cnt on are zero.
-template <int D>
-__device__ __forceinline__ u32x4 open_key(const uint16_t* base, int i, int lane, int cnt) {
-  const u32x4 x = *reinterpret_cast<const u32x4*>(base + (((i >> 1) * 2 + (lane >> 5)) * B + (lane & 31)) * 16 + 8 * (i & 1));
-  return (lane & 31) < cnt ? x : u32x4{0, 0, 0, 0};
+__device__ __forceinline__ u32x4 open_key(const uint16_t* base, int piece, int token, int x, int cnt) {
+  const u32x4 v = *reinterpret_cast<const u32x4*>(base + (piece * B + token) * 16 + 8 * x);
+  return token < cnt ? v : u32x4{0, 0, 0, 0};
 }
-template <int D>
-__device__ __forceinline__ u32x4 open_value(const uint16_t* base, int c, int t, int lane, int cnt) {
-  u32x4 x = *reinterpret_cast<const u32x4*>(base + (c * 64 + lane) * 16 + 8 * t);
+// 8 tokens of one dimension: words 2 y and 2 y + 1 of [c][h][m].
+__device__ __forceinline__ u32x4 open_value(const uint16_t* base, int c, int h, int m, int y, int cnt) {
+  u32x4 v = *reinterpret_cast<const u32x4*>(base + ((c * 2 + h) * 32 + m) * 16 + 8 * y);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    // words 0, 1: tokens 8 t + 4 half + 0..3; words 2, 3: 16 on
-    const int tok = 8 * t + 16 * (i >> 1) + 4 * (lane >> 5) + 2 * (i & 1);
-    x[i] &= (tok < cnt ? 0xFFFFu : 0u) | (tok + 1 < cnt ? 0xFFFF0000u : 0u);
+    const int tok = 8 * y + 16 * (i >> 1) + 4 * h + 2 * (i & 1);
+    v[i] &= (tok < cnt ? 0xFFFFu : 0u) | (tok + 1 < cnt ? 0xFFFF0000u : 0u);
   }
-  return x;
+  return v;
 }
 
-// k_paged_few: units of up to 32 columns (decoded tokens, a few drafts).  The four waves of a
+__device__ __forceinline__ float of_lane(float x, int lane) {
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), lane));
+}
+
+// k_paged_few: units of up to C columns (decoded tokens, a few drafts).  The four waves of a
 // block take its 32-token blocks in turn, each straight from memory to registers, and join
-// at the end of a unit.
-template <int D>
+// at the end of a unit.  Bound by reading the pages, so p is kept in two bf16 parts (16 bits
+// of it): the second product twice costs nothing.
+// C = 16: 16x16x32 products.  Lane l = 16 g + r of S^T holds tokens 16 t + 4 g + e of column r;
+// a load of 16 bytes a lane brings piece 4 j + g of token 16 t + r, or the values of dimension
+// 32 c + 16 (g / 2) + r for half g & 1, of which the lanes 32 apart swap a half.
+template <int D, int C>
 __global__ __launch_bounds__(256, 2) void k_paged_few(PagedAttendArgs a) {
-  constexpr int KST = D / 16, NC = D / 32, OS = D + 4, W = 4;
-  __shared__ __align__(16) float mo[W][32][OS];
-  __shared__ float ml[W][2][32];
+  constexpr bool WIDE = C == 32;
+  constexpr int NL = D / 32;                     // 16-byte loads of a block's keys (values)
+  constexpr int KST = WIDE ? D / 16 : D / 32;    // steps of the first product
+  constexpr int NO = D / C, NV = C / 2, OS = D + 4, W = 4, AHEAD = 1;
+  using acc_t = std::conditional_t<WIDE, f32x16, f32x4>;
+  __shared__ __align__(16) float mo[W][C][OS];
+  __shared__ float ml[W][2][C];
   __shared__ int pre[kPagedUnits + 1];
-  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, c32 = lane & 31, wave = uniform(tid >> 6);
-  for_share<256>(a, 32, 1, pre, [&](int hk, const Unit& un, int first, int cnt, int slot) {
-    const int M = un.M, cc = min(c32, M - 1), tok = cc / a.G, head = hk * a.G + cc - tok * a.G;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane / C, r = lane % C, wave = uniform(tid >> 6);
+  // token of score i in its block
+  auto token_of = [&](int i) { return (WIDE ? 8 : 16) * (i >> 2) + 4 * g + (i & 3); };
+  auto mma = [](u32x4 x, u32x4 y, acc_t z) -> acc_t {
+    if constexpr (WIDE) return mfma32(x, y, z);
+    else return mfma16(x, y, z);
+  };
+  // byte offsets of this lane's pieces in a page
+  auto key_at = [&](int i) { return WIDE ? i * 1024 + lane * 16 : (4 * (i % (D / 64)) + g) * 512 + (16 * (i / (D / 64)) + r) * 16; };
+  const int value_lane = WIDE ? lane * 16 : ((g & 1) * 32 + 16 * (g >> 1) + r) * 16;
+  for_share<256>(a, C, 1, pre, [&](int hk, const Unit& un, int first, int cnt, int slot) {
+    const int M = un.M, cc = min(r, M - 1), tok = cc / a.G, head = hk * a.G + cc - tok * a.G;
     const int last = un.L - un.n + tok, lowest = a.window > 0 ? last - a.window + 1 : 0;
     const int full = uniform(un.L / B), b_at = uniform(un.b_lo + first);
     const int n = (cnt - wave + W - 1) / W;                 // this wave's blocks: b_at + wave + W i
+    // tokens that every column sees: w_lo .. p_lo
     const int p_lo = uniform(un.L - un.n), w_lo = uniform(a.window > 0 ? max(0, un.L - a.window) : 0);
     u32x4 qf[KST];
     {
       const uint16_t* q = a.q.p + head * a.q.hs + (int64_t)(un.start + tok) * a.q.ts;
 #pragma unroll
-      for (int i = 0; i < KST; ++i) qf[i] = *reinterpret_cast<const u32x4*>(q + ((i >> 1) * 2 + half) * 16 + 8 * (i & 1));
+      for (int i = 0; i < KST; ++i)
+        qf[i] = *reinterpret_cast<const u32x4*>(q + ((i >> 1) * (64 / C) + g) * 16 + 8 * (i & 1));
     }
-    f32x16 O[NC];
+    acc_t O[NO];
 #pragma unroll
-    for (int i = 0; i < NC; ++i) O[i] = f32x16{};
+    for (int i = 0; i < NO; ++i) O[i] = acc_t{};
     float m = neg_inf(), l = 0.0f;
 
-    auto step = [&](const u32x4 (&kf)[KST], const u32x4 (&vf)[NC][2], float cs, float lvs, float rvs, int b) {
-      f32x16 S = f32x16{};
+    // kf(i): keys WIDE [step], else [t][step]; vf(i): values [NO][1 or 2 steps]; more() once the keys are used
+    constexpr int NK = WIDE ? KST : 2 * KST, NVF = WIDE ? 2 * NO : NO;
+    auto step = [&](auto&& kf, auto&& vf, auto&& more, float cs, float lvs, float rvs, int b) {
+      float v[NV];
+      if constexpr (WIDE) {
+        acc_t S = acc_t{};
 #pragma unroll
-      for (int i = 0; i < KST; ++i) S = mfma32(kf[i], qf[i], S);
-      float v[16];
+        for (int i = 0; i < KST; ++i) S = mma(kf(i), qf[i], S);
+        more();
 #pragma unroll
-      for (int i = 0; i < 16; ++i) v[i] = S[i] * cs;
-      // (w_lo: the first token that the last column sees; what lies before it, another may see)
-      if (b * B + B - 1 > p_lo || b * B < w_lo) hide(v, b, half, last, lowest);
-      const float lv[1] = {lvs}, rv[1] = {rvs};
-      u32x4 pb[2];
-      softmax_step<1, NC>(v, lv, rv, m, l, O, pb);
+        for (int i = 0; i < NV; ++i) v[i] = S[i];
+      } else {
+        acc_t S[2] = {acc_t{}, acc_t{}};
 #pragma unroll
-      for (int c = 0; c < NC; ++c)
+        for (int i = 0; i < KST; ++i)
 #pragma unroll
-        for (int t = 0; t < 2; ++t) O[c] = mfma32(vf[c][t], pb[t], O[c]);
+          for (int t = 0; t < 2; ++t) S[t] = mma(kf(t * KST + i), qf[i], S[t]);
+        more();
+#pragma unroll
+        for (int i = 0; i < NV; ++i) v[i] = S[i >> 2][i & 3];
+      }
+      if (b * B + B - 1 > p_lo || b * B < w_lo) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          const int j = b * B + token_of(i);
+          if (j > last || j < lowest) v[i] = neg_inf();
+        }
+      }
+      // words of p: groups of four tokens 0, 2 (and 1, 3) of WIDE, 0, 1 of the others
+      u32x4 hi[NV / 8], lo[NV / 8];
+      running_softmax(
+          m, l,
+          [&](float mu) {
+            const float off = lvs - mu;
+            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int w = 0; w < NV / 8; ++w) {
+              bf16x8 x, y;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const int i = WIDE ? 4 * w + (e & 3) + 8 * (e >> 2) : e;
+                const float p = exp2_fast(fmaf(v[i], cs, off));
+                sum[e & 3] += p;
+                x[e] = (__bf16)p;
+                y[e] = (__bf16)(p - (float)x[e]);
+              }
+              hi[w] = __builtin_bit_cast(u32x4, x);
+              lo[w] = __builtin_bit_cast(u32x4, y);
+            }
+            return ((sum[0] + sum[1]) + (sum[2] + sum[3])) * rvs;
+          },
+          [&]() {
+            float top = v[0];
+#pragma unroll
+            for (int i = 1; i < NV; ++i) top = fmaxf(top, v[i]);
+            top *= cs;
+            if constexpr (!WIDE) top = fmaxf(top, __shfl_xor(top, 16));
+            return fmaxf(top, other_half(top));
+          },
+          [&](float al) {
+#pragma unroll
+            for (int i = 0; i < NO; ++i) O[i] *= al;
+          });
+#pragma unroll
+      for (int i = 0; i < NO; ++i)
+#pragma unroll
+        for (int w = 0; w < NV / 8; ++w) {
+          const u32x4 x = vf(i * (NV / 8) + w);
+          O[i] = mma(x, hi[w], O[i]);
+          O[i] = mma(x, lo[w], O[i]);
+        }
     };
 
     for (int i0 = 0; i0 < n; i0 += 64) {
       // pages and scales of the next 64 blocks, one a lane
       int id = -1;
-      float ksv = 0.0f, vsv = 1.0f;
+      float ksv = 0.0f;
+      ValueScale vsv = {0.0f, 1.0f, 1.0f};
       {
         const int b = b_at + wave + W * (i0 + lane);
         if (i0 + lane < n && b < full) id = a.c.tables[(int64_t)un.s * a.c.width + b];
         if ((unsigned)id >= (unsigned)a.c.n_pages) id = -1;
-        if (id >= 0) {
-          ksv = a.c.ks[(int64_t)id * a.c.Hk + hk] * a.c1;
-          vsv = a.c.vs[(int64_t)id * a.c.Hk + hk];
-        }
       }
-      const float lvv = log2_fast(vsv), rvv = 1.0f / vsv;
       const int k1 = min(64, n - i0);
-      u32x4 kq[NC], vq[NC];
-      auto load = [&](int k) {
-        const int pid = max(0, __builtin_amdgcn_readlane(id, k));
-        const int64_t at = ((int64_t)pid * a.c.Hk + hk) * (B * D);
-#pragma unroll
-        for (int c = 0; c < NC; ++c) kq[c] = *(reinterpret_cast<const u32x4*>(a.c.k8 + at) + c * 64 + lane);
-#pragma unroll
-        for (int c = 0; c < NC; ++c) vq[c] = *(reinterpret_cast<const u32x4*>(a.c.v8 + at) + c * 64 + lane);
+      // AHEAD blocks ahead; behind the last one nothing is read, without a branch, so that waits are counted
+      u32x4 kq[AHEAD][NL], vq[AHEAD][NL];
+      auto page = [&](int k, int64_t& at) -> int {
+        const int pid = k < k1 ? __builtin_amdgcn_readlane(id, k & 63) : -1;
+        at = ((int64_t)max(0, pid) * a.c.Hk + hk) * (B * D);
+        return pid < 0 ? 0 : B * D;
       };
-      load(0);
-      for (int k = 0; k < k1; ++k) {
-        u32x4 kf[KST], vf[NC][2];
+      auto load_keys = [&](int64_t at, int bytes, u32x4 (&kr)[NL]) {
+        const auto p = page_bytes(a.c.k8 + at, bytes);
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          kf[2 * c] = widen(kq[c][0], kq[c][1]);
-          kf[2 * c + 1] = widen(kq[c][2], kq[c][3]);
-          vf[c][0] = widen(vq[c][0], vq[c][1]);
-          vf[c][1] = widen(vq[c][2], vq[c][3]);
+        for (int i = 0; i < NL; ++i) kr[i] = load_piece(p, key_at(i));
+      };
+      auto load_values = [&](int64_t at, int bytes, u32x4 (&vr)[NL]) {
+        const auto p = page_bytes(a.c.v8 + at, bytes);
+#pragma unroll
+        for (int i = 0; i < NL; ++i) vr[i] = load_piece(p, i * 1024 + value_lane);
+      };
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) {
+        int64_t at;
+        const int bytes = page(k, at);
+        load_keys(at, bytes, kq[k]);
+        load_values(at, bytes, vq[k]);
+      }
+      if (id >= 0) {
+        ksv = a.c.ks[(int64_t)id * a.c.Hk + hk] * a.c1;
+        vsv = cut_scale(a.c.vs[(int64_t)id * a.c.Hk + hk]);
+      }
+      auto one = [&](int k, u32x4 (&kr)[NL], u32x4 (&vr)[NL]) {
+        const float codes = of_lane(vsv.codes, k);
+        int64_t at;
+        const int bytes = page(k + AHEAD, at);
+        if (__builtin_amdgcn_readlane(id, k) >= 0) {
+          u32x4 half[2];
+          step([&](int i) { return widen(kr[i >> 1][2 * (i & 1)], kr[i >> 1][2 * (i & 1) + 1], 1.0f); },
+               [&](int i) {
+                 const u32x4& x = vr[i >> 1];
+                 if constexpr (WIDE) {
+                   return widen(x[2 * (i & 1)], x[2 * (i & 1) + 1], codes);
+                 } else {
+                   if ((i & 1) == 0) {
+                     const auto y = __builtin_amdgcn_permlane32_swap(x[0], x[2], false, false);
+                     const auto z = __builtin_amdgcn_permlane32_swap(x[1], x[3], false, false);
+                     half[0] = widen(y[0], z[0], codes);
+                     half[1] = widen(y[1], z[1], codes);
+                   }
+                   return half[i & 1];
+                 }
+               },
+               [&]() { load_keys(at, bytes, kr); }, of_lane(ksv, k), of_lane(vsv.log2, k), of_lane(vsv.inverse, k),
+               b_at + wave + W * (i0 + k));
+        } else {
+          load_keys(at, bytes, kr);
         }
-        if (k + 1 < k1) load(k + 1);
-        if (__builtin_amdgcn_readlane(id, k) < 0) continue;
-        auto at = [&](float x) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), k)); };
-        step(kf, vf, at(ksv), at(lvv), at(rvv), b_at + wave + W * (i0 + k));
+        load_values(at, bytes, vr);
+      };
+      for (int k = 0; k < k1; k += AHEAD) {
+#pragma unroll
+        for (int x = 0; x < AHEAD; ++x) {
+          if (k + x >= k1) break;
+          one(k + x, kq[x], vq[x]);
+        }
       }
     }
     const int open_rows = un.L - full * B;
@@ -629,30 +729,33 @@ __global__ __launch_bounds__(256, 2) void k_paged_few(PagedAttendArgs a) {
       const int sl = uniform(a.c.slots[un.s]);
       if ((unsigned)sl < (unsigned)a.c.n_slots) {
         const int64_t at = (((int64_t)sl * 2 + (full & 1)) * a.c.Hk + hk) * (B * D);
-        u32x4 kf[KST], vf[NC][2];
-#pragma unroll
-        for (int i = 0; i < KST; ++i) kf[i] = open_key<D>(a.c.ok + at, i, lane, open_rows);
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-          for (int t = 0; t < 2; ++t) vf[c][t] = open_value<D>(a.c.ov + at, c, t, lane, open_rows);
-        step(kf, vf, a.c1, 0.0f, 1.0f, full);
+        step(
+            [&](int i) {
+              const int t = WIDE ? 0 : i / KST, st = WIDE ? i : i % KST;
+              return open_key(a.c.ok + at, (st >> 1) * (64 / C) + g, 16 * t + r, st & 1, open_rows);
+            },
+            [&](int i) {
+              return WIDE ? open_value(a.c.ov + at, i >> 1, g, r, i & 1, open_rows)
+                          : open_value(a.c.ov + at, i >> 1, g & 1, 16 * (i & 1) + r, g >> 1, open_rows);
+            },
+            []() {}, a.c1, 0.0f, 1.0f, full);
       }
     }
+    if constexpr (!WIDE) l += __shfl_xor(l, 16);
     l += other_half(l);
 
     __syncthreads();                  // the unit before is read
-    if (c32 < M) {
-      float* o = &mo[wave][c32][4 * half];
+    if (r < M) {
+      float* o = &mo[wave][r][4 * g];
 #pragma unroll
-      for (int c = 0; c < NC; ++c)
+      for (int i = 0; i < NO; ++i)
 #pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4)
-          *reinterpret_cast<f32x4*>(o + 32 * c + 8 * q4) =
-              f32x4{O[c][q4 * 4], O[c][q4 * 4 + 1], O[c][q4 * 4 + 2], O[c][q4 * 4 + 3]};
-      if (half == 0) {
-        ml[wave][0][c32] = m;
-        ml[wave][1][c32] = l;
+        for (int q4 = 0; q4 < (WIDE ? 4 : 1); ++q4)
+          *reinterpret_cast<f32x4*>(o + C * i + 8 * q4) =
+              f32x4{O[i][q4 * 4], O[i][q4 * 4 + 1], O[i][q4 * 4 + 2], O[i][q4 * 4 + 3]};
+      if (g == 0) {
+        ml[wave][0][r] = m;
+        ml[wave][1][r] = l;
       }
     }
     __syncthreads();
@@ -685,16 +788,33 @@ __global__ __launch_bounds__(256, 2) void k_paged_few(PagedAttendArgs a) {
   });
 }
 
+// A lane's 16 keys of block b that its column (token `last`, the first seen `lowest`) does not see.
+__device__ __forceinline__ void hide(float* v, int b, int half, int last, int lowest) {
+  const int j0 = b * B + 4 * half;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int j = j0 + 8 * (i >> 2) + (i & 3);
+    if (j > last || j < lowest) v[i] = neg_inf();
+  }
+}
+
+// All waves of the block have come this far, and their LDS traffic is done (loads from memory may be under way).
+__device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 // k_paged_many: units of 32 WQ columns, 32 a wave.  The waves stage tiles of two blocks (64
 // tokens) together: 8-bit pieces from memory to registers a tile ahead, widened once into
 // LDS, where a fragment is a run of 1 KB.
+// WQ = 8: the two waves of a SIMD (w and w + 4) take turns: while one forms its softmax on the
+// vector unit, the other keeps the matrix unit busy, half an iteration behind.  WQ = 4 (33 to 128
+// columns): two blocks a CU, whose phases fall beside each other by themselves.
 template <int D, int WQ>
 __global__ __launch_bounds__(64 * WQ, 2) void k_paged_many(PagedAttendArgs a) {
-  constexpr int KST = D / 16, NC = D / 32, BM = 32 * WQ, SUBS = WQ / 4, NCH = NC / SUBS;
+  constexpr bool TURNS = WQ == 8;
+  constexpr int KST = D / 16, NC = D / 32, BM = 32 * WQ, SUBS = WQ / 4, NCH = NC / SUBS, NS = TURNS ? 4 : 2;
   constexpr int KB = 2 * KST * 64, TB = 2 * KB;        // 16-byte pieces of a tile's keys, of a tile
   static_assert(NCH >= 1);
-  __shared__ __align__(16) u32x4 ring[2][TB];
-  __shared__ float4 meta[2][2];                         // score scale, log 2 and inverse of the value scale, valid
+  __shared__ __align__(16) u32x4 ring[NS][TB];
+  __shared__ float4 meta[NS][2];                        // score scale, log 2 and inverse of the value scale, valid
   __shared__ int pre[kPagedUnits + 1];
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, c32 = lane & 31, wave = uniform(tid >> 6);
   const int su = (wave >> 1) & 1, sub = wave >> 2;      // staging: block su of a tile, its keys or its values
@@ -721,94 +841,213 @@ __global__ __launch_bounds__(64 * WQ, 2) void k_paged_many(PagedAttendArgs a) {
     float m = neg_inf(), l = 0.0f;
 
     u32x4 raw[NCH];
-    float rk = 0.0f, rv = 1.0f;
-    int rid = -1;
-    // this wave's pieces of tile t, to registers
+    int ids = -1, rid = -1;            // a lane the page of one of 64 tiles, and its scales
+    float rk = 0.0f, kss = 0.0f;
+    ValueScale vss = {0.0f, 1.0f, 1.0f}, rv = vss;
+    // this wave's pieces of tile t, to registers; of no page, or behind the last tile, none are read
     auto fetch = [&](int t) {
-      const int b = b_at + 2 * t + su;
-      rid = b < full ? uniform(table[b]) : -1;
-      if ((unsigned)rid >= (unsigned)a.c.n_pages) rid = -1;
-      if (rid < 0) return;
-      const int64_t at = (int64_t)rid * a.c.Hk + hk;
-      const u32x4* src = reinterpret_cast<const u32x4*>((values ? a.c.v8 : a.c.k8) + at * (B * D)) + sub * NCH * 64 + lane;
+      if ((t & 63) == 0) {
+        const int b = b_at + 2 * (t + lane) + su;
+        ids = t + lane < cnt && b < full ? table[b] : -1;
+        if ((unsigned)ids >= (unsigned)a.c.n_pages) ids = -1;
+        if (ids >= 0) {
+          kss = a.c.ks[(int64_t)ids * a.c.Hk + hk] * a.c1;
+          vss = cut_scale(a.c.vs[(int64_t)ids * a.c.Hk + hk]);
+        }
+      }
+      rid = __builtin_amdgcn_readlane(ids, t & 63);
+      const int64_t at = (int64_t)max(0, rid) * a.c.Hk + hk;
+      const auto p = page_bytes((values ? a.c.v8 : a.c.k8) + at * (B * D), rid < 0 ? 0 : B * D);
 #pragma unroll
-      for (int i = 0; i < NCH; ++i) raw[i] = src[i * 64];
-      rk = a.c.ks[at];
-      rv = a.c.vs[at];
+      for (int i = 0; i < NCH; ++i) raw[i] = load_shared(p, (sub * NCH + i) * 1024 + lane * 16);
+      rk = of_lane(kss, t & 63);
+      rv = {of_lane(vss.log2, t & 63), of_lane(vss.inverse, t & 63), of_lane(vss.codes, t & 63)};
     };
     // and widened to LDS
     auto stage = [&](int t) {
+      if (t >= cnt) return;
       const int b = b_at + 2 * t + su;
-      u32x4* buf = ring[t & 1];
+      u32x4* buf = ring[t % NS];
       const bool open = b == full && open_rows > 0 && has_slot;
-      const int64_t at = (((int64_t)(has_slot ? sl : 0) * 2 + (full & 1)) * a.c.Hk + hk) * (B * D);
+      const float codes = values ? rv.codes : 1.0f;
+      u32x4* to = buf + (values ? KB : 0) + (su * KST + 2 * sub * NCH) * 64 + lane;
+      if (!open) {                     // of no page zeros
 #pragma unroll
-      for (int i = 0; i < NCH; ++i) {
-        const int ch = sub * NCH + i;
-        u32x4 x = {0, 0, 0, 0}, y = {0, 0, 0, 0};
-        if (rid >= 0) {
-          x = widen(raw[i][0], raw[i][1]);
-          y = widen(raw[i][2], raw[i][3]);
-        } else if (open) {
-          if (values) {
-            x = open_value<D>(a.c.ov + at, ch, 0, lane, open_rows);
-            y = open_value<D>(a.c.ov + at, ch, 1, lane, open_rows);
-          } else {
-            x = open_key<D>(a.c.ok + at, 2 * ch, lane, open_rows);
-            y = open_key<D>(a.c.ok + at, 2 * ch + 1, lane, open_rows);
-          }
+        for (int i = 0; i < NCH; ++i) {
+          to[128 * i] = widen(raw[i][0], raw[i][1], codes);
+          to[128 * i + 64] = widen(raw[i][2], raw[i][3], codes);
         }
-        u32x4* to = buf + (values ? KB : 0) + (su * KST + 2 * ch) * 64 + lane;
-        to[0] = x;
-        to[64] = y;
+      } else {
+        const int64_t at = (((int64_t)sl * 2 + (full & 1)) * a.c.Hk + hk) * (B * D);
+#pragma unroll
+        for (int i = 0; i < NCH; ++i)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const int ch = sub * NCH + i;
+            to[128 * i + 64 * x] = values ? open_value(a.c.ov + at, ch, half, c32, x, open_rows)
+                                          : open_key(a.c.ok + at, 2 * ch + half, c32, x, open_rows);
+          }
       }
       if (!values && sub == 0 && lane == 0)
-        meta[t & 1][su] = rid >= 0 ? make_float4(rk * a.c1, log2_fast(rv), 1.0f / rv, 1.0f)
-                                   : make_float4(a.c1, 0.0f, 1.0f, open ? 1.0f : 0.0f);
+        meta[t % NS][su] = rid >= 0 ? make_float4(rk, rv.log2, rv.inverse, 1.0f)
+                                    : make_float4(a.c1, 0.0f, 1.0f, open ? 1.0f : 0.0f);
     };
 
-    __syncthreads();                  // the unit before is read
-    fetch(0);
-    stage(0);
-    if (cnt > 1) fetch(1);
-    __syncthreads();
-    for (int t = 0; t < cnt; ++t) {
-      const u32x4* buf = ring[t & 1] + lane;
-      f32x16 S[2];
+    u32x4 pb[4];            // p as the second product's operand
+    f32x16 S[2];
+    // Both products run in steps of four fragments, the next step's read from LDS while this one's
+    // are multiplied; without that order the compiler waits for each read.
+    constexpr int KF = 4, KS = 2 * KST / KF, VF = NC, VS = 4, FR = KF > VF ? KF : VF;
+    u32x4 fr[2][FR];
+    auto read_keys = [&](int t, int step, u32x4 (&f)[FR]) {
+      const u32x4* buf = ring[t % NS] + lane;
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        S[u] = f32x16{};
-#pragma unroll
-        for (int i = 0; i < KST; ++i) S[u] = mfma32(buf[(u * KST + i) * 64], qf[i], S[u]);
+      for (int x = 0; x < KF; ++x) {
+        const int n = step * KF + x, i = n >> 1, u = n & 1;
+        f[x] = buf[(u * KST + i) * 64];
       }
-      float v[32], lv[2], rs[2];
+    };
+    auto multiply_keys = [&](int step, const u32x4 (&f)[FR]) {
+#pragma unroll
+      for (int x = 0; x < KF; ++x) {
+        const int n = step * KF + x, i = n >> 1, u = n & 1;
+        S[u] = mfma32(f[x], qf[i], i == 0 ? f32x16{} : S[u]);
+      }
+    };
+    auto read_values = [&](int t, int step, u32x4 (&f)[FR]) {
+      const u32x4* buf = ring[t % NS] + KB + lane;
+#pragma unroll
+      for (int i = 0; i < NC; ++i) f[i] = buf[((step >> 1) * KST + 2 * i + (step & 1)) * 64];
+    };
+    // S^T of tile t, whose first step is in fr[at]
+    auto scores = [&](int t, int at) {
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        if (k + 1 < KS) read_keys(t, k + 1, fr[(at + k + 1) & 1]);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply_keys(k, fr[(at + k) & 1]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    // O^T += V^T P^T of tile t, whose first step is in fr[0]; more() goes with the last step
+    auto add_values = [&](int t, auto&& more) {
+#pragma unroll
+      for (int k = 0; k < VS; ++k) {
+        if (k + 1 < VS) read_values(t, k + 1, fr[(k + 1) & 1]);
+        else more();
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < NC; ++i) O[i] = mfma32(fr[k & 1][i], pb[k], O[i]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    auto softmax = [&](int t) {
+      float cs[2], lv[2], rs[2], v[32];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const float4 x = meta[t & 1][u];
+        const float4 x = meta[t % NS][u];
+        cs[u] = x.x;
         lv[u] = x.y;
         rs[u] = x.z;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[u * 16 + i] = S[u][i] * x.x;
+        for (int i = 0; i < 16; ++i) v[u * 16 + i] = S[u][i];
         const int b = b_at + 2 * t + u;
         if (b * B + B - 1 > p_lo || b * B < w_lo) hide(v + u * 16, b, half, last, lowest);
-        if (x.w == 0.0f) {
+        if (__any(x.w == 0.0f)) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) v[u * 16 + i] = neg_inf();
         }
       }
-      u32x4 pb[4];
-      softmax_step<2, NC>(v, lv, rs, m, l, O, pb);
+      running_softmax(
+          m, l,
+          [&](float mu) {
+            float all = 0.0f;
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < 2; ++u) {
+              const float off = lv[u] - mu;
+              float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int w = 0; w < 2; ++w)
+              for (int w = 0; w < 2; ++w) {
+                bf16x8 x;
 #pragma unroll
-          for (int i = 0; i < NC; ++i) O[i] = mfma32(buf[KB + (u * KST + 2 * i + w) * 64], pb[u * 2 + w], O[i]);
-      if (t + 1 < cnt) {
-        stage(t + 1);
-        if (t + 2 < cnt) fetch(t + 2);
+                for (int e = 0; e < 8; ++e) {
+                  const float p = exp2_fast(fmaf(v[u * 16 + 4 * w + (e & 3) + 8 * (e >> 2)], cs[u], off));
+                  sum[e & 3] += p;
+                  x[e] = (__bf16)p;
+                }
+                pb[u * 2 + w] = __builtin_bit_cast(u32x4, x);
+              }
+              all = fmaf((sum[0] + sum[1]) + (sum[2] + sum[3]), rs[u], all);
+            }
+            return all;
+          },
+          [&]() {
+            float top[2] = {v[0], v[16]};
+#pragma unroll
+            for (int i = 1; i < 16; ++i) {
+              top[0] = fmaxf(top[0], v[i]);
+              top[1] = fmaxf(top[1], v[16 + i]);
+            }
+            const float x = fmaxf(top[0] * cs[0], top[1] * cs[1]);
+            return fmaxf(x, other_half(x));
+          },
+          [&](float al) {
+#pragma unroll
+            for (int i = 0; i < NC; ++i) O[i] *= al;
+          });
+      if constexpr (TURNS) {       // formed here, not behind the barrier
+#pragma unroll
+        for (int w = 0; w < 4; ++w) asm volatile("" : "+v"(pb[w]));
+        asm volatile("" : "+v"(l));
       }
-      __syncthreads();
+    };
+
+    meet();                           // the unit before is read
+    if constexpr (TURNS) {
+      // Halves of an iteration: half 2t is the first group's softmax of tile t beside the second group's
+      // products of tile t - 1, half 2t + 1 the other way round.  Tile T's part of the first group is
+      // written in half 2T - 4, the second's in 2T - 5; its buffer's last tile, T - 4, is read until
+      // half 2T - 6, and T itself from half 2T - 1 on.
+      const bool second = wave >= 4;
+      const int ahead = second ? 3 : 2;
+      for (int t = 0; t < ahead; ++t) {
+        fetch(t);
+        stage(t);
+      }
+      fetch(ahead);
+      meet();
+      read_keys(0, 0, fr[0]);
+      scores(0, 0);
+      if (second) meet();
+      for (int t = 0; t < cnt; ++t) {
+        stage(t + ahead);
+        fetch(t + ahead + 1);
+        softmax(t);
+        read_values(t, 0, fr[0]);
+        meet();
+        // (behind the last tile the scores are those of an old buffer, and not used)
+        __builtin_amdgcn_s_setprio(1);
+        add_values(t, [&]() { read_keys(t + 1, 0, fr[VS & 1]); });
+        scores(t + 1, VS & 1);
+        __builtin_amdgcn_s_setprio(0);
+        meet();
+      }
+      if (!second) meet();
+    } else {
+      fetch(0);
+      stage(0);
+      fetch(1);
+      meet();
+      for (int t = 0; t < cnt; ++t) {
+        stage(t + 1);                 // its buffer's last reader passed the barrier at the end of tile t - 1
+        fetch(t + 2);
+        read_keys(t, 0, fr[0]);
+        scores(t, 0);
+        softmax(t);
+        read_values(t, 0, fr[0]);
+        add_values(t, []() {});
+        meet();
+      }
     }
     l += other_half(l);
     if (c >= un.M) return;
@@ -832,23 +1071,95 @@ __global__ __launch_bounds__(64 * WQ, 2) void k_paged_many(PagedAttendArgs a) {
   });
 }
 
-// k_paged_join: the parts of a unit's columns, brought to one maximum and added in order.
+// k_paged_join: the parts of a unit's columns, brought to one maximum and added in a fixed order.  Eight
+// groups of d / 4 lanes share a column's parts.
 template <int D>
-__global__ __launch_bounds__(256) void k_paged_join(PagedAttendArgs a, int bm, int round) {
+__global__ __launch_bounds__(2 * D) void k_paged_join(PagedAttendArgs a, int bm, int round) {
+  constexpr int L4 = D / 4, NG = 8;
+  const int hk = blockIdx.x / a.units, u = blockIdx.x % a.units, c = blockIdx.y;
+  const int64_t share = a.plan[0], one = a.plan[1 + a.units];
+  const int64_t x0 = hk * one + a.plan[1 + u], x1 = hk * one + a.plan[2 + u];
+  if (x0 == x1) return;
+  const int g0 = (int)(x0 / share), g1 = (int)((x1 - 1) / share);
+  if (g0 == g1) return;
+  const Unit un = unit_of(a, u, bm, round);
+  if (c >= min(bm, un.M - un.c0)) return;
+  __shared__ __align__(16) f32x4 so[NG][L4];
+  __shared__ float sm[NG], sl[NG];
+  const int grp = threadIdx.x / L4, d4 = threadIdx.x % L4;
+  // a block's part of this unit lies in its first slot when its share begins in the unit
+  auto part = [&](int g) { return (2 * (int64_t)g + ((int64_t)g * share >= x0 ? 0 : 1)) * a.cols + c; };
+  // a group's parts AT at a time: all loads under way before the first is used
+  constexpr int AT = 8;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  float l = 0.0f, m = neg_inf();
+  for (int g = g0 + grp; g <= g1; g += NG * AT) {
+    f32x4 po[AT];
+    float pm[AT], pl[AT], top = m;
+#pragma unroll
+    for (int i = 0; i < AT; ++i) {
+      const int64_t at = part(min(g + NG * i, g1));
+      pm[i] = a.part_ml[2 * at];
+      pl[i] = a.part_ml[2 * at + 1];
+      po[i] = *reinterpret_cast<const f32x4*>(a.part_o + at * D + 4 * d4);
+    }
+#pragma unroll
+    for (int i = 0; i < AT; ++i) {
+      if (g + NG * i > g1) pm[i] = neg_inf();
+      top = fmaxf(top, pm[i]);
+    }
+    const float mu = top == neg_inf() ? 0.0f : top, w0 = exp2_fast(m - mu);
+    o *= w0;
+    l *= w0;
+    m = top;
+#pragma unroll
+    for (int i = 0; i < AT; ++i) {
+      const float w = exp2_fast(pm[i] - mu);
+      l = fmaf(pl[i], w, l);
+      o += po[i] * w;
+    }
+  }
+  if (d4 == 0) sm[grp] = m;
+  __syncthreads();
+  float top = sm[0];
+#pragma unroll
+  for (int x = 1; x < NG; ++x) top = fmaxf(top, sm[x]);
+  {
+    const float w = exp2_fast(m - (top == neg_inf() ? 0.0f : top));
+    o *= w;
+    l *= w;
+  }
+  so[grp][d4] = o;
+  if (d4 == 0) sl[grp] = l;
+  __syncthreads();
+  if (grp > 0) return;
+#pragma unroll
+  for (int x = 1; x < NG; ++x) {
+    o += so[x][d4];
+    l += sl[x];
+  }
+  const int col = un.c0 + c;
+  finish(a, hk * a.G + col % a.G, un.start + col / a.G, 4 * d4, o, top, l);
+}
+
+// The same where units have many columns and few parts: a group of d / 4 lanes a column.
+template <int D>
+__global__ __launch_bounds__(256) void k_paged_join_many(PagedAttendArgs a, int bm, int round) {
   constexpr int L4 = D / 4, ROWS = 256 / L4;
   const int hk = blockIdx.x / a.units, u = blockIdx.x % a.units;
   const int64_t share = a.plan[0], one = a.plan[1 + a.units];
   const int64_t x0 = hk * one + a.plan[1 + u], x1 = hk * one + a.plan[2 + u];
   if (x0 == x1) return;
-  const int64_t g0 = x0 / share, g1 = (x1 - 1) / share;
+  const int g0 = (int)(x0 / share), g1 = (int)((x1 - 1) / share);
   if (g0 == g1) return;
   const Unit un = unit_of(a, u, bm, round);
   const int c = blockIdx.y * ROWS + threadIdx.x / L4, d = threadIdx.x % L4 * 4;
   if (c >= min(bm, un.M - un.c0)) return;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   float m = neg_inf(), l = 0.0f;
-  for (int64_t g = g0; g <= g1; ++g) {
-    const int64_t at = (2 * g + (g * share >= x0 ? 0 : 1)) * a.cols + c;
+#pragma unroll 2
+  for (int g = g0; g <= g1; ++g) {
+    const int64_t at = (2 * (int64_t)g + (g * share >= x0 ? 0 : 1)) * a.cols + c;
     const float pm = a.part_ml[2 * at], pl = a.part_ml[2 * at + 1];
     const f32x4 x = *reinterpret_cast<const f32x4*>(a.part_o + at * D + d);
     const float top = fmaxf(m, pm), mu = top == neg_inf() ? 0.0f : top;
@@ -864,12 +1175,19 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedAttendArgs a, int bm, i
 template <int D>
 hipError_t attend_impl(const PagedAttendArgs& a, const PagedAttendPlan& p, hipStream_t st) {
   const dim3 grid((unsigned)(a.n_wg ? a.n_wg : a.units * a.c.Hk));
-  if (p.shape == 0) hipLaunchKernelGGL((k_paged_few<D>), grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((k_paged_many<D, 4>), grid, dim3(256), 0, st, a);
+  if (p.bm == 16) hipLaunchKernelGGL((k_paged_few<D, 16>), grid, dim3(256), 0, st, a);
+  else if (p.bm == 32) hipLaunchKernelGGL((k_paged_few<D, 32>), grid, dim3(256), 0, st, a);
+  else if (p.bm == 128) hipLaunchKernelGGL((k_paged_many<D, 4>), grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((k_paged_many<D, 8>), grid, dim3(512), 0, st, a);
   if (a.n_wg) {
-    const int bm = p.shape == 0 ? 32 : 128, rows = 256 / (D / 4);
-    hipLaunchKernelGGL((k_paged_join<D>), dim3((unsigned)(a.units * a.c.Hk), (unsigned)((a.cols + rows - 1) / rows)),
-                       dim3(256), 0, st, a, bm, p.shape == 0 ? 1 : 2);
+    const unsigned rows = (unsigned)(a.units * a.c.Hk);
+    if (p.bm <= 32) {
+      hipLaunchKernelGGL((k_paged_join<D>), dim3(rows, (unsigned)a.cols), dim3(2 * D), 0, st, a, p.bm, p.round);
+    } else {
+      const int per = 256 / (D / 4);
+      hipLaunchKernelGGL((k_paged_join_many<D>), dim3(rows, (unsigned)((a.cols + per - 1) / per)), dim3(256), 0, st, a,
+                         p.bm, p.round);
+    }
   }
   return hipGetLastError();
 }

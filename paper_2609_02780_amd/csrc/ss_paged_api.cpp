@@ -211,8 +211,9 @@ ss_status plan_attend(const ss_cache* c, const ss_cache_streams* s, int32_t n_to
   } else {
     most = n_tokens / S;
   }
-  p.shape = G * most <= 32 ? 0 : 1;
-  const int bm = p.shape == 0 ? 32 : 128, round = p.shape == 0 ? 1 : 2;
+  const int bm = G * most <= 16 ? 16 : G * most <= 32 ? 32 : G * most <= 128 ? 128 : 256, round = bm <= 32 ? 1 : 2;
+  p.bm = bm;
+  p.round = round;
   p.per = n_q ? 0 : (int)cdiv((int64_t)G * most, bm);
   p.units = n_q ? (int)((int64_t)G * n_tokens / bm) + S : S * p.per;
   p.cols = std::min(bm, G * most);
@@ -223,9 +224,9 @@ ss_status plan_attend(const ss_cache* c, const ss_cache_streams* s, int32_t n_to
   if ((work + 1) * p.units > 0x7FFFFFFF)
     return fail(SS_ERR_UNSUPPORTED, "%d units of up to %lld blocks are more than 2^31", p.units, (long long)work);
   const int64_t all = work * p.units * Hk;
-  p.min_share = p.shape == 0 ? 32 : 8;
+  p.min_share = bm <= 32 ? 32 : 8;
   // a block a unit: where a unit is short, or where units alone fill the card several times
-  const int room = 512;
+  const int room = bm <= 128 ? 512 : 256;
   if (work <= p.min_share || p.units > ss::kPagedUnits || (int64_t)p.units * Hk >= 8 * room) {
     p.n_wg = 0;
     p.o_bytes = p.ml_bytes = p.plan_bytes = 0;
