@@ -12,7 +12,7 @@ namespace ss {
 constexpr int kBlockTokens = 32;      // tokens of a page
 constexpr int kPagedStreams = 512;    // streams of a call
 constexpr int kPagedTokens = 1 << 16; // new tokens (queries) of a call
-constexpr int kPagedUnits = 2048;      // units of a KV head that are cut into shares (more are not)
+constexpr int kPagedUnits = 1536;      // units of a KV head that are cut into shares (more are not)
 constexpr int kPagedWidth = (1 << 26) - 1;   // pages of a stream: its tokens are counted in 31 bits
 
 // Which tokens of a call are a stream's.

@@ -358,10 +358,21 @@ struct Unit {
   int s, n, start, L, c0, M;         // its columns c0 .. min(c0 + BM, M) - 1
   int b_lo, count;                   // first block, and how many (at least 1: someone writes the outputs); 0: no unit
 };
-__device__ __forceinline__ int unit_first(const PagedAttendArgs& a, int s, int bm) {
-  return a.per ? s * a.per : a.G * a.spans.start[s] / bm + s;
+// Where the streams' tokens begin, and their lengths, in LDS: one trip to memory for all.
+struct Streams {
+  int start[kPagedStreams + 1], length[kPagedStreams];
+};
+__device__ __forceinline__ void load_streams(const PagedAttendArgs& a, Streams& t) {
+  for (int i = threadIdx.x; i <= a.S; i += blockDim.x) {
+    t.start[i] = span_start(a.spans, i);
+    if (i < a.S) t.length[i] = stream_length(a.c, i);
+  }
+  __syncthreads();
 }
-__device__ __forceinline__ Unit unit_of(const PagedAttendArgs& a, int u, int bm, int round) {
+__device__ __forceinline__ int unit_first(const PagedAttendArgs& a, const Streams& t, int s, int bm) {
+  return a.per ? s * a.per : a.G * t.start[s] / bm + s;
+}
+__device__ __forceinline__ Unit unit_of(const PagedAttendArgs& a, const Streams& t, int u, int bm, int round) {
   Unit x;
   if (a.per) {
     x.s = u / a.per;
@@ -369,34 +380,34 @@ __device__ __forceinline__ Unit unit_of(const PagedAttendArgs& a, int u, int bm,
     int lo = 0, hi = a.S - 1;        // the last stream that begins at u or before
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
-      if (unit_first(a, mid, bm) <= u) lo = mid;
+      if (unit_first(a, t, mid, bm) <= u) lo = mid;
       else hi = mid - 1;
     }
     x.s = lo;
   }
-  x.start = span_start(a.spans, x.s);
-  x.n = span_start(a.spans, x.s + 1) - x.start;
+  x.start = t.start[x.s];
+  x.n = t.start[x.s + 1] - x.start;
   x.M = a.G * x.n;
-  x.c0 = (u - unit_first(a, x.s, bm)) * bm;
+  x.c0 = (u - unit_first(a, t, x.s, bm)) * bm;
   x.L = 0;
   x.b_lo = x.count = 0;
   if (x.c0 >= x.M) return x;
-  x.L = stream_length(a.c, x.s);
+  x.L = t.length[x.s];
   const int p_lo = x.L - x.n + x.c0 / a.G;                                   // the first and the last column's tokens
   const int p_hi = x.L - x.n + (min(x.M, x.c0 + bm) - 1) / a.G;
   const int lowest = a.window > 0 ? max(0, p_lo - a.window + 1) : 0;
-  x.b_lo = lowest / B / round * round;
-  x.count = p_hi < 0 ? 1 : max(1, (p_hi / B - x.b_lo + round) / round);
+  x.b_lo = round == 2 ? (lowest / B) & ~1 : lowest / B;
+  x.count = p_hi < 0 ? 1 : max(1, round == 2 ? (p_hi / B - x.b_lo + 2) >> 1 : p_hi / B - x.b_lo + 1);
   return x;
 }
 
 // pre[u]: the work before unit u (pre[units]: all of it).
 template <int T>
-__device__ __forceinline__ void plan_units(const PagedAttendArgs& a, int bm, int round, int* pre) {
+__device__ __forceinline__ void plan_units(const PagedAttendArgs& a, const Streams& t, int bm, int round, int* pre) {
   __shared__ int part[T / 64];
   const int tid = threadIdx.x, run = (a.units + T - 1) / T, u0 = min(a.units, tid * run), u1 = min(a.units, u0 + run);
   int sum = 0;
-  for (int u = u0; u < u1; ++u) sum += unit_of(a, u, bm, round).count;
+  for (int u = u0; u < u1; ++u) sum += unit_of(a, t, u, bm, round).count;
   int upto = sum;
 #pragma unroll
   for (int x = 1; x < 64; x <<= 1) {
@@ -411,7 +422,7 @@ __device__ __forceinline__ void plan_units(const PagedAttendArgs& a, int bm, int
     if (w < (tid >> 6)) at += part[w];
   for (int u = u0; u < u1; ++u) {
     pre[u] = at;
-    at += unit_of(a, u, bm, round).count;
+    at += unit_of(a, t, u, bm, round).count;
   }
   if (tid == T - 1) pre[a.units] = at;
   __syncthreads();
@@ -425,31 +436,49 @@ __device__ __forceinline__ int64_t share_of(const PagedAttendArgs& a, int64_t al
 // Calls work(kv head, unit, first of its blocks, how many, slot of the part or -1) for a block's share.
 template <int T, class F>
 __device__ __forceinline__ void for_share(const PagedAttendArgs& a, int bm, int round, int* pre, F&& work) {
-  const int wg = blockIdx.x;
-  if (a.n_wg == 0) {
-    const Unit x = unit_of(a, wg % a.units, bm, round);
-    if (x.count) work(wg / a.units, x, 0, x.count, -1);
-    return;
-  }
-  plan_units<T>(a, bm, round, pre);
-  const int64_t one = pre[a.units], all = one * a.c.Hk, share = share_of(a, all);
-  if (wg == 0) {
-    if (threadIdx.x == 0) a.plan[0] = (int)share;
-    for (int u = threadIdx.x; u <= a.units; u += T) a.plan[1 + u] = pre[u];
-  }
-  int64_t x = wg * share;
-  const int64_t end = min(all, x + share);
-  for (bool begin = true; x < end; begin = false) {
-    const int hk = (int)(x / one), y = (int)(x % one);
-    int lo = 0, hi = a.units - 1;                        // the last unit whose work begins at y or before
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (pre[mid] <= y) lo = mid;
-      else hi = mid - 1;
+  int wg = blockIdx.x;
+  // neighbouring shares, which read the same pages, on one XCD (blocks go round them)
+  if (a.n_wg != 0 && wg < a.n_wg / 8 * 8) wg = (wg & 7) * (a.n_wg / 8) + (wg >> 3);
+  int64_t one = 1, x = 0, end = 1;
+  __shared__ Streams streams;
+  load_streams(a, streams);
+  if (a.n_wg != 0) {
+    plan_units<T>(a, streams, bm, round, pre);
+    one = pre[a.units];
+    const int64_t all = one * a.c.Hk, share = share_of(a, all);
+    if (wg == 0) {
+      if (threadIdx.x == 0) a.plan[0] = (int)share;
+      for (int u = threadIdx.x; u <= a.units; u += T) a.plan[1 + u] = pre[u];
     }
-    const int u = uniform(lo), first = uniform(y - pre[u]), whole = uniform(pre[u + 1] - pre[u]);
-    const int cnt = uniform((int)min((int64_t)(whole - first), end - x));
-    work(uniform(hk), unit_of(a, u, bm, round), first, cnt, cnt == whole ? -1 : 2 * wg + (begin ? 0 : 1));
+    x = wg * share;
+    end = min(all, x + share);
+  }
+  for (int side = 0; x < end; side = 1) {                // (one call of work: it is inlined)
+    // (a block a unit: a head's on few XCDs, the last units, which may see the most, first)
+    int hk = wg % a.c.Hk, u = a.units - 1 - wg / a.c.Hk, first = 0;
+    if (a.n_wg != 0) {
+      hk = (int)(x / one);
+      const int y = (int)(x % one);
+      int lo = 0, hi = a.units - 1;                      // the last unit whose work begins at y or before
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (pre[mid] <= y) lo = mid;
+        else hi = mid - 1;
+      }
+      u = lo;
+      first = y - pre[u];
+    }
+    u = uniform(u);
+    first = uniform(first);
+    const Unit un = unit_of(a, streams, u, bm, round);
+    int cnt = un.count, slot = -1;
+    if (a.n_wg != 0) {
+      cnt = (int)min((int64_t)(un.count - first), end - x);
+      if (cnt != un.count) slot = 2 * wg + side;
+    }
+    cnt = uniform(cnt);
+    if (cnt == 0) return;
+    work(uniform(hk), un, first, cnt, uniform(slot));
     x += cnt;
   }
 }
@@ -814,7 +843,7 @@ __global__ __launch_bounds__(64 * WQ, 2) void k_paged_many(PagedAttendArgs a) {
   constexpr int KB = 2 * KST * 64, TB = 2 * KB;        // 16-byte pieces of a tile's keys, of a tile
   static_assert(NCH >= 1);
   __shared__ __align__(16) u32x4 ring[NS][TB];
-  __shared__ float4 meta[NS][2];                        // score scale, log 2 and inverse of the value scale, valid
+  __shared__ float4 meta[2][64][2];   // of a tile's blocks, 64 tiles at a time: score scale; value scale (0: not seen)
   __shared__ int pre[kPagedUnits + 1];
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, c32 = lane & 31, wave = uniform(tid >> 6);
   const int su = (wave >> 1) & 1, sub = wave >> 2;      // staging: block su of a tile, its keys or its values
@@ -840,57 +869,56 @@ __global__ __launch_bounds__(64 * WQ, 2) void k_paged_many(PagedAttendArgs a) {
     for (int i = 0; i < NC; ++i) O[i] = f32x16{};
     float m = neg_inf(), l = 0.0f;
 
-    u32x4 raw[NCH];
-    int ids = -1, rid = -1;            // a lane the page of one of 64 tiles, and its scales
-    float rk = 0.0f, kss = 0.0f;
-    ValueScale vss = {0.0f, 1.0f, 1.0f}, rv = vss;
-    // this wave's pieces of tile t, to registers; of no page, or behind the last tile, none are read
-    auto fetch = [&](int t) {
-      if ((t & 63) == 0) {
-        const int b = b_at + 2 * (t + lane) + su;
-        ids = t + lane < cnt && b < full ? table[b] : -1;
-        if ((unsigned)ids >= (unsigned)a.c.n_pages) ids = -1;
-        if (ids >= 0) {
-          kss = a.c.ks[(int64_t)ids * a.c.Hk + hk] * a.c1;
-          vss = cut_scale(a.c.vs[(int64_t)ids * a.c.Hk + hk]);
-        }
+    // (kept in registers: read again from the arguments in every tile they cost a trip each)
+    const uint8_t* pages = (values ? a.c.v8 : a.c.k8) + hk * (B * D);
+    int page_stride = a.c.Hk * (B * D);
+    asm volatile("" : "+s"(pages), "+s"(page_stride));
+    int ids = -1;                      // a lane the page of one of 64 tiles, and what its codes are scaled by
+    float codes = 1.0f;
+    // pages and scales of tiles t .. t + 63; they may be used behind the next barrier
+    auto look_up = [&](int t) {
+      const int b = b_at + 2 * (t + lane) + su;
+      ids = t + lane < cnt && b < full ? table[b] : -1;
+      if ((unsigned)ids >= (unsigned)a.c.n_pages) ids = -1;
+      float4 x = make_float4(a.c1, 0.0f, 1.0f, b == full && open_rows > 0 && has_slot ? 1.0f : 0.0f);
+      if (ids >= 0) {
+        const ValueScale vs = cut_scale(a.c.vs[(int64_t)ids * a.c.Hk + hk]);
+        x = make_float4(a.c.ks[(int64_t)ids * a.c.Hk + hk] * a.c1, vs.log2, vs.inverse, 1.0f);
+        if (values) codes = vs.codes;
       }
-      rid = __builtin_amdgcn_readlane(ids, t & 63);
-      const int64_t at = (int64_t)max(0, rid) * a.c.Hk + hk;
-      const auto p = page_bytes((values ? a.c.v8 : a.c.k8) + at * (B * D), rid < 0 ? 0 : B * D);
+      if (!values && sub == 0) meta[(t >> 6) & 1][lane][su] = x;
+    };
+    // this wave's pieces of tile t, to registers; of no page, or behind the last tile, none are read
+    auto fetch = [&](int t, u32x4 (&raw)[NCH]) {
+      if ((t & 63) == 0 && t > 0) look_up(t);
+      const int id = __builtin_amdgcn_readlane(ids, t & 63);
+      const auto p = page_bytes(pages + (int64_t)max(0, id) * page_stride, id < 0 ? 0 : B * D);
 #pragma unroll
       for (int i = 0; i < NCH; ++i) raw[i] = load_shared(p, (sub * NCH + i) * 1024 + lane * 16);
-      rk = of_lane(kss, t & 63);
-      rv = {of_lane(vss.log2, t & 63), of_lane(vss.inverse, t & 63), of_lane(vss.codes, t & 63)};
     };
-    // and widened to LDS
-    auto stage = [&](int t) {
-      if (t >= cnt) return;
-      const int b = b_at + 2 * t + su;
-      u32x4* buf = ring[t % NS];
-      const bool open = b == full && open_rows > 0 && has_slot;
-      const float codes = values ? rv.codes : 1.0f;
-      u32x4* to = buf + (values ? KB : 0) + (su * KST + 2 * sub * NCH) * 64 + lane;
-      if (!open) {                     // of no page zeros
+    // and widened to LDS, piece by piece (2 NCH)
+    auto put = [&](int t, const u32x4 (&raw)[NCH], int i, float x) {
+      u32x4* to = ring[t % NS] + (values ? KB : 0) + (su * KST + 2 * sub * NCH) * 64 + lane;
+      to[64 * i] = widen(raw[i >> 1][2 * (i & 1)], raw[i >> 1][2 * (i & 1) + 1], x);
+    };
+    // an open block comes from its slot instead
+    auto put_open = [&](int t) {
+      if (t >= cnt || b_at + 2 * t + su != full || open_rows == 0 || !has_slot) return;
+      u32x4* to = ring[t % NS] + (values ? KB : 0) + (su * KST + 2 * sub * NCH) * 64 + lane;
+      const int64_t at = (((int64_t)sl * 2 + (full & 1)) * a.c.Hk + hk) * (B * D);
 #pragma unroll
-        for (int i = 0; i < NCH; ++i) {
-          to[128 * i] = widen(raw[i][0], raw[i][1], codes);
-          to[128 * i + 64] = widen(raw[i][2], raw[i][3], codes);
+      for (int i = 0; i < NCH; ++i)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int ch = sub * NCH + i;
+          to[128 * i + 64 * x] = values ? open_value(a.c.ov + at, ch, half, c32, x, open_rows)
+                                        : open_key(a.c.ok + at, 2 * ch + half, c32, x, open_rows);
         }
-      } else {
-        const int64_t at = (((int64_t)sl * 2 + (full & 1)) * a.c.Hk + hk) * (B * D);
+    };
+    auto stage = [&](int t, const u32x4 (&raw)[NCH]) {
 #pragma unroll
-        for (int i = 0; i < NCH; ++i)
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            const int ch = sub * NCH + i;
-            to[128 * i + 64 * x] = values ? open_value(a.c.ov + at, ch, half, c32, x, open_rows)
-                                          : open_key(a.c.ok + at, 2 * ch + half, c32, x, open_rows);
-          }
-      }
-      if (!values && sub == 0 && lane == 0)
-        meta[t % NS][su] = rid >= 0 ? make_float4(rk, rv.log2, rv.inverse, 1.0f)
-                                    : make_float4(a.c1, 0.0f, 1.0f, open ? 1.0f : 0.0f);
+      for (int i = 0; i < 2 * NCH; ++i) put(t, raw, i, of_lane(codes, t & 63));
+      put_open(t);
     };
 
     u32x4 pb[4];            // p as the second product's operand
@@ -929,23 +957,34 @@ __global__ __launch_bounds__(64 * WQ, 2) void k_paged_many(PagedAttendArgs a) {
         __builtin_amdgcn_sched_barrier(0);
       }
     };
-    // O^T += V^T P^T of tile t, whose first step is in fr[0]; more() goes with the last step
-    auto add_values = [&](int t, auto&& more) {
+    // O^T += V^T P^T of tile t, whose first step is in fr[0]; more() goes with the last step.  The pieces of tile
+    // `next` are widened between the products, whose time on the matrix unit covers them (in the softmax's
+    // half of an iteration they cost their full 600 clocks).
+    auto add_values = [&](int t, int next, const u32x4 (&raw)[NCH], auto&& more) {
+      const float x = of_lane(codes, next & 63);
+      constexpr int GAP = VS * NC / (2 * NCH);
 #pragma unroll
       for (int k = 0; k < VS; ++k) {
         if (k + 1 < VS) read_values(t, k + 1, fr[(k + 1) & 1]);
         else more();
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < NC; ++i) O[i] = mfma32(fr[k & 1][i], pb[k], O[i]);
+        for (int i = 0; i < NC; ++i) {
+          O[i] = mfma32(fr[k & 1][i], pb[k], O[i]);
+          const int n = k * NC + i + 1;
+          if (n % GAP == 0) {
+            put(next, raw, n / GAP - 1, x);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
         __builtin_amdgcn_sched_barrier(0);
       }
     };
-    auto softmax = [&](int t) {
+    auto softmax = [&](int t, const float4 (&mt)[2]) {
       float cs[2], lv[2], rs[2], v[32];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const float4 x = meta[t % NS][u];
+        const float4 x = mt[u];
         cs[u] = x.x;
         lv[u] = x.y;
         rs[u] = x.z;
@@ -1003,49 +1042,56 @@ __global__ __launch_bounds__(64 * WQ, 2) void k_paged_many(PagedAttendArgs a) {
     };
 
     meet();                           // the unit before is read
+    look_up(0);
+    meet();
+    constexpr int AHEAD = TURNS ? 2 : 1;      // a tile is staged so many iterations before its softmax, fetched one more
+    u32x4 raw[NCH];
+    {
+      u32x4 first[AHEAD][NCH];
+#pragma unroll
+      for (int t = 0; t < AHEAD; ++t) fetch(t, first[t]);
+      fetch(AHEAD, raw);
+#pragma unroll
+      for (int t = 0; t < AHEAD; ++t) stage(t, first[t]);
+    }
+    meet();
     if constexpr (TURNS) {
       // Halves of an iteration: half 2t is the first group's softmax of tile t beside the second group's
-      // products of tile t - 1, half 2t + 1 the other way round.  Tile T's part of the first group is
-      // written in half 2T - 4, the second's in 2T - 5; its buffer's last tile, T - 4, is read until
-      // half 2T - 6, and T itself from half 2T - 1 on.
+      // products of tile t - 1, half 2t + 1 the other way round.  The first group writes its part of tile T
+      // in half 2T - 3, the second in 2T - 2; its buffer's last tile, T - 4, is read until half 2T - 6, and
+      // T itself from half 2T - 1 on.
       const bool second = wave >= 4;
-      const int ahead = second ? 3 : 2;
-      for (int t = 0; t < ahead; ++t) {
-        fetch(t);
-        stage(t);
-      }
-      fetch(ahead);
-      meet();
       read_keys(0, 0, fr[0]);
       scores(0, 0);
       if (second) meet();
       for (int t = 0; t < cnt; ++t) {
-        stage(t + ahead);
-        fetch(t + ahead + 1);
-        softmax(t);
+        const float4 mt[2] = {meta[(t >> 6) & 1][t & 63][0], meta[(t >> 6) & 1][t & 63][1]};
+        __builtin_amdgcn_sched_barrier(0);
+        softmax(t, mt);
         read_values(t, 0, fr[0]);
         meet();
         // (behind the last tile the scores are those of an old buffer, and not used)
         __builtin_amdgcn_s_setprio(1);
-        add_values(t, [&]() { read_keys(t + 1, 0, fr[VS & 1]); });
+        add_values(t, t + AHEAD, raw, [&]() { read_keys(t + 1, 0, fr[VS & 1]); });
+        put_open(t + AHEAD);
+        fetch(t + AHEAD + 1, raw);
         scores(t + 1, VS & 1);
         __builtin_amdgcn_s_setprio(0);
         meet();
       }
       if (!second) meet();
     } else {
-      fetch(0);
-      stage(0);
-      fetch(1);
-      meet();
       for (int t = 0; t < cnt; ++t) {
-        stage(t + 1);                 // its buffer's last reader passed the barrier at the end of tile t - 1
-        fetch(t + 2);
+        const float4 mt[2] = {meta[(t >> 6) & 1][t & 63][0], meta[(t >> 6) & 1][t & 63][1]};
         read_keys(t, 0, fr[0]);
+        __builtin_amdgcn_sched_barrier(0);
         scores(t, 0);
-        softmax(t);
+        softmax(t, mt);
         read_values(t, 0, fr[0]);
-        add_values(t, []() {});
+        // (the next buffer's last reader passed the barrier at the end of tile t - 1)
+        add_values(t, t + AHEAD, raw, []() {});
+        put_open(t + AHEAD);
+        fetch(t + AHEAD + 1, raw);
         meet();
       }
     }
@@ -1082,7 +1128,9 @@ __global__ __launch_bounds__(2 * D) void k_paged_join(PagedAttendArgs a, int bm,
   if (x0 == x1) return;
   const int g0 = (int)(x0 / share), g1 = (int)((x1 - 1) / share);
   if (g0 == g1) return;
-  const Unit un = unit_of(a, u, bm, round);
+  __shared__ Streams streams;
+  load_streams(a, streams);
+  const Unit un = unit_of(a, streams, u, bm, round);
   if (c >= min(bm, un.M - un.c0)) return;
   __shared__ __align__(16) f32x4 so[NG][L4];
   __shared__ float sm[NG], sl[NG];
@@ -1152,7 +1200,9 @@ __global__ __launch_bounds__(256) void k_paged_join_many(PagedAttendArgs a, int 
   if (x0 == x1) return;
   const int g0 = (int)(x0 / share), g1 = (int)((x1 - 1) / share);
   if (g0 == g1) return;
-  const Unit un = unit_of(a, u, bm, round);
+  __shared__ Streams streams;
+  load_streams(a, streams);
+  const Unit un = unit_of(a, streams, u, bm, round);
   const int c = blockIdx.y * ROWS + threadIdx.x / L4, d = threadIdx.x % L4 * 4;
   if (c >= min(bm, un.M - un.c0)) return;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};

@@ -43,6 +43,7 @@ inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 constexpr size_t kLeastWorkspace = 256;
 constexpr int kMaxGroup = 16;
+constexpr int kJoinWork = 32;
 
 ss_status check_desc(const ss_cache_desc* d) {
   if (!d) return fail(SS_ERR_INVALID_ARGUMENT, "desc is NULL");
@@ -225,9 +226,11 @@ ss_status plan_attend(const ss_cache* c, const ss_cache_streams* s, int32_t n_to
     return fail(SS_ERR_UNSUPPORTED, "%d units of up to %lld blocks are more than 2^31", p.units, (long long)work);
   const int64_t all = work * p.units * Hk;
   p.min_share = bm <= 32 ? 32 : 8;
-  // a block a unit: where a unit is short, or where units alone fill the card several times
-  const int room = bm <= 128 ? 512 : 256;
-  if (work <= p.min_share || p.units > ss::kPagedUnits || (int64_t)p.units * Hk >= 8 * room) {
+  // A block a unit leaves part of the last round of blocks idle; shares fill all rounds, but their parts are
+  // joined, which costs about as much as kJoinWork blocks (pairs) of work.
+  const int64_t room = bm <= 128 ? 512 : 256, blocks = (int64_t)p.units * Hk;
+  const int64_t idle = (cdiv(blocks, room) * room - blocks) * work / room;
+  if (idle <= kJoinWork || p.units > ss::kPagedUnits) {
     p.n_wg = 0;
     p.o_bytes = p.ml_bytes = p.plan_bytes = 0;
     return SS_OK;
