@@ -837,7 +837,7 @@ __device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts
 // vector unit, the other keeps the matrix unit busy, half an iteration behind.  WQ = 4 (33 to 128
 // columns): two blocks a CU, whose phases fall beside each other by themselves.
 template <int D, int WQ>
-__global__ __launch_bounds__(64 * WQ, 2) void k_paged_many(PagedAttendArgs a) {
+__global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_many(PagedAttendArgs a) {
   constexpr bool TURNS = WQ == 8;
   constexpr int KST = D / 16, NC = D / 32, BM = 32 * WQ, SUBS = WQ / 4, NCH = NC / SUBS, NS = TURNS ? 4 : 2;
   constexpr int KB = 2 * KST * 64, TB = 2 * KB;        // 16-byte pieces of a tile's keys, of a tile
@@ -1231,7 +1231,7 @@ hipError_t attend_impl(const PagedAttendArgs& a, const PagedAttendPlan& p, hipSt
   else hipLaunchKernelGGL((k_paged_many<D, 8>), grid, dim3(512), 0, st, a);
   if (a.n_wg) {
     const unsigned rows = (unsigned)(a.units * a.c.Hk);
-    if (p.bm <= 32) {
+    if (p.bm <= 32 || a.n_wg > 4 * (int64_t)rows) {     // many parts a unit
       hipLaunchKernelGGL((k_paged_join<D>), dim3(rows, (unsigned)a.cols), dim3(2 * D), 0, st, a, p.bm, p.round);
     } else {
       const int per = 256 / (D / 4);

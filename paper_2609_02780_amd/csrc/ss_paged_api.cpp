@@ -212,23 +212,29 @@ ss_status plan_attend(const ss_cache* c, const ss_cache_streams* s, int32_t n_to
   } else {
     most = n_tokens / S;
   }
-  const int bm = G * most <= 16 ? 16 : G * most <= 32 ? 32 : G * most <= 128 ? 128 : 256, round = bm <= 32 ? 1 : 2;
+  // blocks of 32 tokens that a unit of bm columns can see
+  auto seen = [&](int bm) {
+    const int64_t all = (int64_t)s->width + 1;
+    return window ? std::min(all, cdiv((int64_t)window + cdiv(bm, G) + 1, ss::kBlockTokens) + 1) : all;
+  };
+  // More than 128 columns: 256 a unit, but at d = 64 (bound by the vector unit) 128 where units are short: what
+  // starts and ends them weighs more there (2,000 tokens over a window of 1,000: 72 us with 256, 52; 4,096 tokens
+  // over 16,384: 350 us, 365).
+  const int bm = G * most <= 16 ? 16 : G * most <= 32 ? 32 : G * most <= 128 || (D == 64 && seen(256) <= 64) ? 128 : 256;
+  const int round = bm <= 32 ? 1 : 2;
   p.bm = bm;
   p.round = round;
   p.per = n_q ? 0 : (int)cdiv((int64_t)G * most, bm);
   p.units = n_q ? (int)((int64_t)G * n_tokens / bm) + S : S * p.per;
   p.cols = std::min(bm, G * most);
-  // blocks (pairs of blocks) that a unit can see
-  int64_t work = (int64_t)s->width + 1;
-  if (window) work = std::min(work, cdiv((int64_t)window + cdiv(bm, G) + 1, ss::kBlockTokens) + 1);
-  work = cdiv(work, round);
+  const int64_t work = cdiv(seen(bm), round);
   if ((work + 1) * p.units > 0x7FFFFFFF)
     return fail(SS_ERR_UNSUPPORTED, "%d units of up to %lld blocks are more than 2^31", p.units, (long long)work);
   const int64_t all = work * p.units * Hk;
   p.min_share = bm <= 32 ? 32 : 8;
   // A block a unit leaves part of the last round of blocks idle; shares fill all rounds, but their parts are
   // joined, which costs about as much as kJoinWork blocks (pairs) of work.
-  const int64_t room = bm <= 128 ? 512 : 256, blocks = (int64_t)p.units * Hk;
+  const int64_t room = bm == 256 ? 256 : bm == 128 && D == 64 ? 768 : 512, blocks = (int64_t)p.units * Hk;
   const int64_t idle = (cdiv(blocks, room) * room - blocks) * work / room;
   if (idle <= kJoinWork || p.units > ss::kPagedUnits) {
     p.n_wg = 0;
