@@ -15,9 +15,13 @@ constexpr int kPagedTokens = 1 << 16; // new tokens (queries) of a call
 constexpr int kPagedUnits = 1536;      // units of a KV head that are cut into shares (more are not)
 constexpr int kPagedWidth = (1 << 26) - 1;   // pages of a stream: its tokens are counted in 31 bits
 
-// Which tokens of a call are a stream's.
+// Which tokens of a call are a stream's.  Kernels of small calls take the one or the other: 2 KB more of
+// arguments cost a launch some 0.4 us.
+struct EvenSpans {
+  int uniform;                        // tokens of every stream
+};
 struct Spans {
-  int uniform;                        // tokens of every stream, or 0: by start
+  int uniform;                        // 0: by start
   int start[kPagedStreams + 1];
 };
 
@@ -55,9 +59,8 @@ struct PagedAppendArgs {
   RowsView k, v, q, q_out;            // q.p null: no queries
   Turn turn;
   int Hq, S, items;                   // items: blocks that the new tokens can touch, of all streams
-  Spans spans;
 };
-hipError_t launch_paged_append(const PagedAppendArgs& a, int D, hipStream_t st);
+hipError_t launch_paged_append(const PagedAppendArgs& a, const Spans& spans, int D, hipStream_t st);
 
 struct PagedAttendArgs {
   PagedDev c;
@@ -71,14 +74,14 @@ struct PagedAttendArgs {
   float c1;                           // log2(e) / sqrt(d)
   int units, per, cols;               // units of a KV head; of a stream (0: ragged); columns kept of a unit
   int n_wg, min_share;                // blocks; 0: a block a unit, nothing to join
-  Spans spans;
 };
 struct PagedAttendPlan {
   int bm, round;                      // columns of a unit, blocks that its work is counted in
   int units, per, cols, n_wg, min_share;
   size_t o_bytes, ml_bytes, plan_bytes;
 };
-hipError_t launch_paged_attend(const PagedAttendArgs& a, const PagedAttendPlan& p, int D, hipStream_t st);
+hipError_t launch_paged_attend(const PagedAttendArgs& a, const Spans& spans, const PagedAttendPlan& p, int D,
+                               hipStream_t st);
 
 }  // namespace ss
 

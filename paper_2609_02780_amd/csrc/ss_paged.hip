@@ -80,6 +80,7 @@ __device__ __forceinline__ float bf16_at(uint16_t x) { return __uint_as_float((u
 __device__ __forceinline__ uint16_t to_bf16(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
 
 __device__ __forceinline__ int span_start(const Spans& s, int i) { return s.uniform ? i * s.uniform : s.start[i]; }
+__device__ __forceinline__ int span_start(const EvenSpans& s, int i) { return i * s.uniform; }
 
 // A stream's tokens, by what its table can hold.
 __device__ __forceinline__ int stream_length(const PagedDev& c, int s) {
@@ -87,46 +88,71 @@ __device__ __forceinline__ int stream_length(const PagedDev& c, int s) {
 }
 
 // ---------------------------------------------------------------------------
-// Rotation.  cos and sin of up to 32 tokens are formed once for all heads of a block:
-// the angle in turns, position * (f / 2 pi), in 64 bits (a far position times a
-// frequency loses what matters in 32), its fraction in 32.
+// Rotation.  cos and sin of a block's tokens are formed once for all its heads: the angle
+// in turns, position * (f / 2 pi), in 64 bits (a far position times a frequency loses what
+// matters in 32), and of its fraction the hardware's sine and cosine, which take turns and are off by
+// at most 2^-22.9 over a turn (over all multiples of 2^-20).
+//
+// A thread takes 16 elements of a row as two groups of 8, so that what it loads is what it
+// writes: both elements of eight pairs (i, i + dims / 2) where the groups lie on 16 bytes; else
+// 16 side by side, where pairs of neighbours are.  (Other odd sizes read the other elements one by one.)
 // ---------------------------------------------------------------------------
 constexpr int kMaxPairs = 64;
+template <int ROWS>
 struct Angles {
-  float2 cs[B][kMaxPairs + 1];       // gain cos, gain sin
+  float2 cs[ROWS][kMaxPairs * 32 / ROWS + 1];       // gain cos, gain sin; 64 rows of d = 64, 32 of d = 128
 };
 
 // Rows [r0, r1) of the table; token r's position is positions[first + r] or pos0 + r.
-__device__ __forceinline__ void fill_angles(Angles& g, const Turn& t, int r0, int r1, int first, int64_t pos0) {
-  const int half = t.dims >> 1, n = (r1 - r0) * half;
-  for (int i = threadIdx.x; i < n; i += blockDim.x) {
-    const int r = r0 + i / half, j = i % half;
+template <int ROWS>
+__device__ __forceinline__ void fill_angles(Angles<ROWS>& g, const Turn& t, int r0, int r1, int first, int64_t pos0) {
+  constexpr int PAIRS = kMaxPairs * 32 / ROWS;
+  const int half = t.dims >> 1, j = threadIdx.x % PAIRS;
+  if (j >= half) return;
+  const double f = t.freqs[j];
+  for (int r = r0 + threadIdx.x / PAIRS; r < r1; r += blockDim.x / PAIRS) {
     const int64_t pos = t.positions ? t.positions[first + r] : pos0 + r;
-    const double turns = (double)pos * t.freqs[j];
-    float s, c;
-    sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
-    g.cs[r][j] = make_float2(t.gain * c, t.gain * t.sign * s);
+    const double turns = (double)pos * f;
+    const float x = (float)(turns - rint(turns));
+    g.cs[r][j] = make_float2(t.gain * __builtin_amdgcn_cosf(x), t.gain * t.sign * __builtin_amdgcn_sinf(x));
   }
 }
 
-// Elements 16 p .. 16 p + 15 of a row at x, rotated by the angles cs.
-__device__ __forceinline__ void turned(const uint16_t* x, int p, const float2* cs, const Turn& t, float (&y)[16]) {
-  const int i0 = 16 * p, half = t.dims >> 1;
-  const u32x4* v = reinterpret_cast<const u32x4*>(x + i0);
-  const u32x4 a = v[0], b = v[1];
+// The two groups of item p: elements e0 .. e0 + 7 and e1 .. e1 + 7.
+struct Groups {
+  int e0, e1;
+};
+__device__ __forceinline__ Groups groups_of(const Turn& t, int p) {
+  const int half = t.dims >> 1;
+  if (!t.interleaved && (half & 7) == 0 && 8 * p < half) return {8 * p, half + 8 * p};
+  return {16 * p, 16 * p + 8};
+}
+struct Raw {
+  u32x4 a, b;
+};
+__device__ __forceinline__ Raw load_groups(const uint16_t* x, Groups g) {
+  return {*reinterpret_cast<const u32x4*>(x + g.e0), *reinterpret_cast<const u32x4*>(x + g.e1)};
+}
+__device__ __forceinline__ void as_floats(const Raw& v, float (&y)[16]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    y[2 * i] = __uint_as_float(a[i] << 16);
-    y[2 * i + 1] = __uint_as_float(a[i] & 0xFFFF0000u);
-    y[8 + 2 * i] = __uint_as_float(b[i] << 16);
-    y[8 + 2 * i + 1] = __uint_as_float(b[i] & 0xFFFF0000u);
+    y[2 * i] = __uint_as_float(v.a[i] << 16);
+    y[2 * i + 1] = __uint_as_float(v.a[i] & 0xFFFF0000u);
+    y[8 + 2 * i] = __uint_as_float(v.b[i] << 16);
+    y[8 + 2 * i + 1] = __uint_as_float(v.b[i] & 0xFFFF0000u);
   }
-  if (i0 >= t.dims) return;
+}
+// x: the row (read again only where its pairs lie across 16 bytes).
+__device__ __forceinline__ void turn_groups(const uint16_t* x, const Raw& v, Groups g, const float2* cs, const Turn& t,
+                                            float (&y)[16]) {
+  as_floats(v, y);
+  const int half = t.dims >> 1;
+  if (g.e0 >= t.dims) return;
   if (t.interleaved) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      if (i0 + 2 * i < t.dims) {
-        const float2 w = cs[i0 / 2 + i];
+      if (g.e0 + 2 * i < t.dims) {
+        const float2 w = cs[g.e0 / 2 + i];
         const float e = y[2 * i], o = y[2 * i + 1];
         y[2 * i] = e * w.x - o * w.y;
         y[2 * i + 1] = o * w.x + e * w.y;
@@ -134,23 +160,16 @@ __device__ __forceinline__ void turned(const uint16_t* x, int p, const float2* c
     }
   } else if ((half & 7) == 0) {
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const int at = i0 + 8 * k;
-      if (at >= t.dims) break;
-      const bool low = at < half;
-      const u32x4 o = *reinterpret_cast<const u32x4*>(x + (low ? at + half : at - half));
-      const float2* w = cs + (low ? at : at - half);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float z = i & 1 ? __uint_as_float(o[i / 2] & 0xFFFF0000u) : __uint_as_float(o[i / 2] << 16);
-        const float sn = low ? -w[i].y : w[i].y;
-        y[8 * k + i] = y[8 * k + i] * w[i].x + z * sn;
-      }
+    for (int i = 0; i < 8; ++i) {
+      const float2 w = cs[g.e0 + i];
+      const float e = y[i], o = y[8 + i];
+      y[i] = e * w.x - o * w.y;
+      y[8 + i] = o * w.x + e * w.y;
     }
   } else {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const int at = i0 + i;
+      const int at = g.e0 + i;
       if (at < t.dims) {
         const bool low = at < half;
         const float2 w = cs[low ? at : at - half];
@@ -159,35 +178,50 @@ __device__ __forceinline__ void turned(const uint16_t* x, int p, const float2* c
     }
   }
 }
-
-__device__ __forceinline__ void store16(uint16_t* p, const float (&y)[16]) {
-  bf16x8 a, b;
+__device__ __forceinline__ bf16x8 eight(const float* y) {
+  bf16x8 v;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    a[i] = (__bf16)y[i];
-    b[i] = (__bf16)y[8 + i];
-  }
-  reinterpret_cast<bf16x8*>(p)[0] = a;
-  reinterpret_cast<bf16x8*>(p)[1] = b;
+  for (int i = 0; i < 8; ++i) v[i] = (__bf16)y[i];
+  return v;
+}
+__device__ __forceinline__ void store_groups(uint16_t* p, Groups g, const float (&y)[16]) {
+  *reinterpret_cast<bf16x8*>(p + g.e0) = eight(y);
+  *reinterpret_cast<bf16x8*>(p + g.e1) = eight(y + 8);
 }
 
-// k_rotate: a block takes 32 tokens and some of the heads; a thread 16 elements of a row.
-constexpr int kRotateHeads = 4;
-template <int D>
-__global__ __launch_bounds__(2 * D) void k_rotate(RotateArgs a) {
-  constexpr int P = D / 16;
-  __shared__ Angles g;
-  const int t0 = blockIdx.x * B, n = min(B, a.N - t0);
-  fill_angles(g, a.turn, 0, n, t0, t0);
-  __syncthreads();
-  const int r = threadIdx.x / P, p = threadIdx.x % P;
-  if (r >= n) return;
-  const int h1 = min(a.heads, (int)(blockIdx.y + 1) * kRotateHeads);
-  for (int h = blockIdx.y * kRotateHeads; h < h1; ++h) {
+// Rotates row `at` of heads h0 .. h1 - 1 (at most N): all loads first.
+// x and out may be one: a thread writes what it has read, and where another reads it too (pairs across 16 bytes),
+// `apart` orders the two.
+template <int N>
+__device__ __forceinline__ void turn_heads(const RowsView& x, const RowsView& out, int64_t at, int h0, int h1, int p,
+                                           bool live, const float2* cs, const Turn& t, bool apart) {
+  const Groups g = groups_of(t, p);
+  Raw v[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (live && h0 + i < h1) v[i] = load_groups(x.p + (h0 + i) * x.hs + at * x.ts, g);
+  __syncthreads();                                 // the angles are there
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int h = h0 + i;
     float y[16];
-    turned(a.x.p + h * a.x.hs + (int64_t)(t0 + r) * a.x.ts, p, g.cs[r], a.turn, y);
-    store16(const_cast<uint16_t*>(a.out.p) + h * a.out.hs + (int64_t)(t0 + r) * a.out.ts + 16 * p, y);
+    if (live && h < h1) turn_groups(x.p + h * x.hs + at * x.ts, v[i], g, cs, t, y);
+    if (apart) __syncthreads();
+    if (live && h < h1) store_groups(const_cast<uint16_t*>(out.p) + h * out.hs + at * out.ts, g, y);
   }
+}
+__device__ __forceinline__ bool pairs_across(const Turn& t) { return t.dims > 0 && !t.interleaved && ((t.dims >> 1) & 7) != 0; }
+
+// k_rotate: a block takes 32 tokens (64 at d = 64) and H heads.  Bound by reading and writing the
+// rows: 8,192 tokens of 28 heads of 128 (118 MB), 24 us, 5.0 TB/s, the rate of a large copy.
+template <int D, int H>
+__global__ __launch_bounds__(256) void k_rotate(RotateArgs a) {
+  constexpr int P = D / 16, ROWS = 256 / P;
+  __shared__ Angles<ROWS> g;
+  const int t0 = blockIdx.x * ROWS, n = min(ROWS, a.N - t0), r = threadIdx.x / P;
+  fill_angles(g, a.turn, 0, n, t0, t0);
+  turn_heads<H>(a.x, a.out, t0 + r, blockIdx.y * H, min(a.heads, (int)(blockIdx.y + 1) * H), threadIdx.x % P, r < n,
+                g.cs[r], a.turn, pairs_across(a.turn));
 }
 
 // ---------------------------------------------------------------------------
@@ -197,20 +231,6 @@ __global__ __launch_bounds__(2 * D) void k_rotate(RotateArgs a) {
 // ---------------------------------------------------------------------------
 constexpr float kLeastMax = 0x1p-100f;    // 448 / it stays finite
 
-template <int D>
-__device__ __forceinline__ float block_max(float v, float* part) {
-  constexpr int W = 2 * D / 64;
-#pragma unroll
-  for (int x = 32; x > 0; x >>= 1) v = fmaxf(v, __shfl_xor(v, x));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = part[0];
-#pragma unroll
-  for (int w = 1; w < W; ++w) v = fmaxf(v, part[w]);
-  return v;
-}
-
 __device__ __forceinline__ uint32_t pack8(float a, float b, float c, float d) {
   int r = 0;
   r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, r, false);
@@ -218,91 +238,93 @@ __device__ __forceinline__ uint32_t pack8(float a, float b, float c, float d) {
   return (uint32_t)r;
 }
 
-template <int D>
-__global__ __launch_bounds__(2 * D) void k_paged_append(PagedAppendArgs a) {
+// Where element e of token r lies in a block of values.
+__device__ __forceinline__ int value_place(int r, int e) {
+  const int w = ((r >> 4) & 1) | ((r >> 3) & 1) << 1;
+  return (((e >> 5) * 2 + ((r >> 2) & 1)) * 32 + (e & 31)) * 16 + w * 4 + (r & 3);
+}
+
+template <int D, int H, class SP>
+__global__ __launch_bounds__(2 * D) void k_paged_append(PagedAppendArgs a, SP spans) {
   constexpr int P = D / 16;
-  __shared__ Angles g;
+  __shared__ Angles<32> g;
   __shared__ __align__(16) uint16_t vt[B][D + 8];
   __shared__ float part[8];
-  const int tid = threadIdx.x, r = tid / P, p = tid % P;
+  const int tid = threadIdx.x, p = tid % P;
   // the stream and which of its touched blocks: (n + 62) / 32 at most, wherever the old tokens end
   int s, k;
-  if (a.spans.uniform) {
-    const int per = (a.spans.uniform + 2 * B - 2) / B;
+  if (std::is_same_v<SP, EvenSpans>) {
+    const int per = (spans.uniform + 2 * B - 2) / B;
     s = blockIdx.x / per;
     k = blockIdx.x % per;
   } else {
     s = 0;
     int first = 0;
     for (;; ++s) {
-      const int n = a.spans.start[s + 1] - a.spans.start[s];
+      const int n = span_start(spans, s + 1) - span_start(spans, s);
       const int per = n > 0 ? (n + 2 * B - 2) / B : 0;
       if ((int)blockIdx.x < first + per) break;
       first += per;
     }
     k = blockIdx.x - first;
   }
-  const int start = span_start(a.spans, s), n = span_start(a.spans, s + 1) - start;
+  const int start = span_start(spans, s), n = span_start(spans, s + 1) - start;
   const int L = stream_length(a.c, s), old = L - n, b0 = max(old, 0) / B, last = (L - 1) / B;
   int b = b0 + k;
   if (L == 0 || b > last) return;
   const int slot = a.c.slots[s];
   const bool has_slot = (unsigned)slot < (unsigned)a.c.n_slots;
+  const bool keys = (int)blockIdx.y < a.c.Hk;
+  if (!keys) {
+    const int t0 = max(max(old, 0), B * b), t1 = min(L, B * (b + 1)), i = tid / P;
+    if (a.turn.dims) fill_angles(g, a.turn, t0 - B * b, t1 - B * b, start + B * b - old, (int64_t)B * b);
+    const int h0 = (blockIdx.y - a.c.Hk) * H;
+    turn_heads<H>(a.q, a.q_out, start + (t0 - old) + i, h0, min(a.Hq, h0 + H), p, t0 + i < t1,
+                  g.cs[(t0 - B * b + i) & 31], a.turn, pairs_across(a.turn));
+    return;
+  }
   // A token's open rows lie in buffer block & 1.  Where the last block's buffer is the one that
   // the first block reads, the first block's own thread block writes it, after reading.
   const bool shared = last > b0 && ((last - b0) & 1) == 0;
-  const bool keys = (int)blockIdx.y < a.c.Hk;
+  const int h = blockIdx.y, r = tid / P;
+  const Groups e = groups_of(a.turn, p);
   for (int job = 0; job < 2; ++job) {
     if (job == 1) {
-      if (!(shared && b == b0 && keys)) return;
+      if (!(shared && b == b0)) return;
       b = last;
       __syncthreads();
     }
     const int t0 = max(max(old, 0), B * b), t1 = min(L, B * (b + 1));    // new tokens of this block
-    if (a.turn.dims) fill_angles(g, a.turn, t0 - B * b, t1 - B * b, start + B * b - old, (int64_t)B * b);
-    __syncthreads();
     const int t = B * b + r;
     const bool fresh = t >= t0 && t < t1;
     const int64_t row = start + t - old;                                   // of the call's tokens
-    if (!keys) {
-      const int h0 = (blockIdx.y - a.c.Hk) * kRotateHeads, h1 = min(a.Hq, h0 + kRotateHeads);
-      if (!fresh) return;
-      for (int h = h0; h < h1; ++h) {
-        float y[16];
-        turned(a.q.p + h * a.q.hs + row * a.q.ts, p, g.cs[r], a.turn, y);
-        store16(const_cast<uint16_t*>(a.q_out.p) + h * a.q_out.hs + row * a.q_out.ts + 16 * p, y);
-      }
-      return;
-    }
-    const int h = blockIdx.y;
+    const uint16_t *kp = a.k.p + h * a.k.hs + row * a.k.ts, *vp = a.v.p + h * a.v.hs + row * a.v.ts;
     const bool full = job == 0 && t1 == B * (b + 1);
     const bool stays = has_slot && (job == 1 || (b == last && !shared) || (b == last && b == b0) ||
                                     (b == b0 && ((last - b0) & 1) == 1));
     const int64_t open_at = (((int64_t)slot * 2 + (b & 1)) * a.c.Hk + h) * B * D;
+    Raw kr, vr;
+    if (fresh) {
+      kr = load_groups(kp, e);
+      vr = load_groups(vp, {16 * p, 16 * p + 8});
+    }
+    if (a.turn.dims) fill_angles(g, a.turn, t0 - B * b, t1 - B * b, start + B * b - old, (int64_t)B * b);
+    __syncthreads();
     float y[16], v[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) y[i] = v[i] = 0.0f;
+    // bytes of a page (elements of an open block) from one piece of keys, 16 elements, to the next: 32 tokens of 16
+    const int k0 = ((e.e0 >> 4) * B + r) * 16 + (e.e0 & 15), k1 = ((e.e1 >> 4) * B + r) * 16 + (e.e1 & 15);
     if (fresh) {
-      turned(a.k.p + h * a.k.hs + row * a.k.ts, p, g.cs[r], a.turn, y);
-      const u32x4* src = reinterpret_cast<const u32x4*>(a.v.p + h * a.v.hs + row * a.v.ts + 16 * p);
-      const u32x4 x0 = src[0], x1 = src[1];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(x0[i] << 16);
-        v[2 * i + 1] = __uint_as_float(x0[i] & 0xFFFF0000u);
-        v[8 + 2 * i] = __uint_as_float(x1[i] << 16);
-        v[8 + 2 * i + 1] = __uint_as_float(x1[i] & 0xFFFF0000u);
-      }
+      turn_groups(kp, kr, e, g.cs[r], a.turn, y);
+      as_floats(vr, v);
 #pragma unroll
       for (int i = 0; i < 16; ++i) y[i] = (float)(__bf16)y[i];
     } else if (full && t < t0 && has_slot) {
-      const uint16_t* ko = a.c.ok + open_at + (p * B + r) * 16;
+      kr = {*reinterpret_cast<const u32x4*>(a.c.ok + open_at + k0), *reinterpret_cast<const u32x4*>(a.c.ok + open_at + k1)};
+      as_floats(kr, y);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        y[i] = bf16_at(ko[i]);
-        const int d = 16 * p + i, gq = r >> 3, w = (gq >> 1) | ((gq & 1) << 1);
-        v[i] = bf16_at(a.c.ov[open_at + (((d >> 5) * 2 + ((r >> 2) & 1)) * 32 + (d & 31)) * 16 + w * 4 + (r & 3)]);
-      }
+      for (int i = 0; i < 16; ++i) v[i] = bf16_at(a.c.ov[open_at + value_place(r, 16 * p + i)]);
     }
     if (full) {
       float km = 0.0f, vm = 0.0f;
@@ -310,18 +332,36 @@ __global__ __launch_bounds__(2 * D) void k_paged_append(PagedAppendArgs a) {
       for (int i = 0; i < 16; ++i) {
         km = fmaxf(km, fabsf(y[i]));
         vm = fmaxf(vm, fabsf(v[i]));
-        vt[r][16 * p + i] = to_bf16(v[i]);
       }
-      km = fmaxf(block_max<D>(km, part), kLeastMax);
-      vm = fmaxf(block_max<D>(vm, part), kLeastMax);
+      *reinterpret_cast<bf16x8*>(&vt[r][16 * p]) = eight(v);
+      *reinterpret_cast<bf16x8*>(&vt[r][16 * p + 8]) = eight(v + 8);
+      // the block's maxima, both at once (the barriers also show vt)
+#pragma unroll
+      for (int x = 32; x > 0; x >>= 1) {
+        km = fmaxf(km, __shfl_xor(km, x));
+        vm = fmaxf(vm, __shfl_xor(vm, x));
+      }
+      if ((tid & 63) == 0) {
+        part[2 * (tid >> 6)] = km;
+        part[2 * (tid >> 6) + 1] = vm;
+      }
+      __syncthreads();
+      km = vm = kLeastMax;
+#pragma unroll
+      for (int w = 0; w < 2 * D / 64; ++w) {
+        km = fmaxf(km, part[2 * w]);
+        vm = fmaxf(vm, part[2 * w + 1]);
+      }
       const int page = a.c.tables[(int64_t)s * a.c.width + b];
       if ((unsigned)page < (unsigned)a.c.n_pages && (has_slot || t0 == B * b)) {
         const int64_t at = ((int64_t)page * a.c.Hk + h);
         const float ki = 448.0f / km, vi = 448.0f / vm;
-        u32x4 w;
+        uint32_t w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = pack8(y[4 * i] * ki, y[4 * i + 1] * ki, y[4 * i + 2] * ki, y[4 * i + 3] * ki);
-        *reinterpret_cast<u32x4*>(a.c.k8 + at * B * D + (p * B + r) * 16) = w;
+        uint8_t* kd = a.c.k8 + at * B * D;
+        *reinterpret_cast<u32x2*>(kd + k0) = u32x2{w[0], w[1]};
+        *reinterpret_cast<u32x2*>(kd + k1) = u32x2{w[2], w[3]};
         // values: a thread takes 16 tokens of one dimension
         const int m = tid & 31, half = (tid >> 5) & 1, d = (tid >> 6) * 32 + m;
 #pragma unroll
@@ -330,7 +370,7 @@ __global__ __launch_bounds__(2 * D) void k_paged_append(PagedAppendArgs a) {
           w[i] = pack8(bf16_at(vt[tok][d]) * vi, bf16_at(vt[tok + 1][d]) * vi, bf16_at(vt[tok + 2][d]) * vi,
                        bf16_at(vt[tok + 3][d]) * vi);
         }
-        *reinterpret_cast<u32x4*>(a.c.v8 + at * B * D + tid * 16) = w;
+        *reinterpret_cast<u32x4*>(a.c.v8 + at * B * D + tid * 16) = u32x4{w[0], w[1], w[2], w[3]};
         if (tid == 0) {
           a.c.ks[at] = km / 448.0f;
           a.c.vs[at] = vm / 448.0f;
@@ -338,12 +378,10 @@ __global__ __launch_bounds__(2 * D) void k_paged_append(PagedAppendArgs a) {
       }
     }
     if (stays && fresh) {
-      store16(a.c.ok + open_at + (p * B + r) * 16, y);
+      *reinterpret_cast<bf16x8*>(a.c.ok + open_at + k0) = eight(y);
+      *reinterpret_cast<bf16x8*>(a.c.ok + open_at + k1) = eight(y + 8);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int d = 16 * p + i, gq = r >> 3, w = (gq >> 1) | ((gq & 1) << 1);
-        a.c.ov[open_at + (((d >> 5) * 2 + ((r >> 2) & 1)) * 32 + (d & 31)) * 16 + w * 4 + (r & 3)] = to_bf16(v[i]);
-      }
+      for (int i = 0; i < 16; ++i) a.c.ov[open_at + value_place(r, 16 * p + i)] = to_bf16(v[i]);
     }
   }
 }
@@ -362,9 +400,10 @@ struct Unit {
 struct Streams {
   int start[kPagedStreams + 1], length[kPagedStreams];
 };
-__device__ __forceinline__ void load_streams(const PagedAttendArgs& a, Streams& t) {
+template <class SP>
+__device__ __forceinline__ void load_streams(const PagedAttendArgs& a, const SP& spans, Streams& t) {
   for (int i = threadIdx.x; i <= a.S; i += blockDim.x) {
-    t.start[i] = span_start(a.spans, i);
+    t.start[i] = span_start(spans, i);
     if (i < a.S) t.length[i] = stream_length(a.c, i);
   }
   __syncthreads();
@@ -434,14 +473,14 @@ __device__ __forceinline__ int64_t share_of(const PagedAttendArgs& a, int64_t al
 }
 
 // Calls work(kv head, unit, first of its blocks, how many, slot of the part or -1) for a block's share.
-template <int T, class F>
-__device__ __forceinline__ void for_share(const PagedAttendArgs& a, int bm, int round, int* pre, F&& work) {
+template <int T, class SP, class F>
+__device__ __forceinline__ void for_share(const PagedAttendArgs& a, const SP& spans, int bm, int round, int* pre, F&& work) {
   int wg = blockIdx.x;
   // neighbouring shares, which read the same pages, on one XCD (blocks go round them)
   if (a.n_wg != 0 && wg < a.n_wg / 8 * 8) wg = (wg & 7) * (a.n_wg / 8) + (wg >> 3);
   int64_t one = 1, x = 0, end = 1;
   __shared__ Streams streams;
-  load_streams(a, streams);
+  load_streams(a, spans, streams);
   if (a.n_wg != 0) {
     plan_units<T>(a, streams, bm, round, pre);
     one = pre[a.units];
@@ -559,19 +598,19 @@ __device__ __forceinline__ float of_lane(float x, int lane) {
   return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), lane));
 }
 
-// k_paged_few: units of up to C columns (decoded tokens, a few drafts).  The four waves of a
+// k_paged_few: units of up to C columns (decoded tokens, a few drafts).  The W waves of a
 // block take its 32-token blocks in turn, each straight from memory to registers, and join
 // at the end of a unit.  Bound by reading the pages, so p is kept in two bf16 parts (16 bits
 // of it): the second product twice costs nothing.
 // C = 16: 16x16x32 products.  Lane l = 16 g + r of S^T holds tokens 16 t + 4 g + e of column r;
 // a load of 16 bytes a lane brings piece 4 j + g of token 16 t + r, or the values of dimension
 // 32 c + 16 (g / 2) + r for half g & 1, of which the lanes 32 apart swap a half.
-template <int D, int C>
-__global__ __launch_bounds__(256, 2) void k_paged_few(PagedAttendArgs a) {
+template <int D, int C, int W, class SP>
+__global__ __launch_bounds__(64 * W, W == 4 ? 2 : 1) void k_paged_few(PagedAttendArgs a, SP spans) {
   constexpr bool WIDE = C == 32;
   constexpr int NL = D / 32;                     // 16-byte loads of a block's keys (values)
   constexpr int KST = WIDE ? D / 16 : D / 32;    // steps of the first product
-  constexpr int NO = D / C, NV = C / 2, OS = D + 4, W = 4, AHEAD = 1;
+  constexpr int NO = D / C, NV = C / 2, OS = D + 4, AHEAD = 1;
   using acc_t = std::conditional_t<WIDE, f32x16, f32x4>;
   __shared__ __align__(16) float mo[W][C][OS];
   __shared__ float ml[W][2][C];
@@ -586,7 +625,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_few(PagedAttendArgs a) {
   // byte offsets of this lane's pieces in a page
   auto key_at = [&](int i) { return WIDE ? i * 1024 + lane * 16 : (4 * (i % (D / 64)) + g) * 512 + (16 * (i / (D / 64)) + r) * 16; };
   const int value_lane = WIDE ? lane * 16 : ((g & 1) * 32 + 16 * (g >> 1) + r) * 16;
-  for_share<256>(a, C, 1, pre, [&](int hk, const Unit& un, int first, int cnt, int slot) {
+  for_share<64 * W>(a, spans, C, 1, pre, [&](int hk, const Unit& un, int first, int cnt, int slot) {
     const int M = un.M, cc = min(r, M - 1), tok = cc / a.G, head = hk * a.G + cc - tok * a.G;
     const int last = un.L - un.n + tok, lowest = a.window > 0 ? last - a.window + 1 : 0;
     const int full = uniform(un.L / B), b_at = uniform(un.b_lo + first);
@@ -788,7 +827,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_few(PagedAttendArgs a) {
       }
     }
     __syncthreads();
-    for (int i = tid; i < M * (D / 4); i += 256) {
+    for (int i = tid; i < M * (D / 4); i += 64 * W) {
       const int c = i / (D / 4), d = i % (D / 4) * 4;
       float top = ml[0][0][c];
 #pragma unroll
@@ -837,7 +876,7 @@ __device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts
 // vector unit, the other keeps the matrix unit busy, half an iteration behind.  WQ = 4 (33 to 128
 // columns): two blocks a CU, whose phases fall beside each other by themselves.
 template <int D, int WQ>
-__global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_many(PagedAttendArgs a) {
+__global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_many(PagedAttendArgs a, Spans spans) {
   constexpr bool TURNS = WQ == 8;
   constexpr int KST = D / 16, NC = D / 32, BM = 32 * WQ, SUBS = WQ / 4, NCH = NC / SUBS, NS = TURNS ? 4 : 2;
   constexpr int KB = 2 * KST * 64, TB = 2 * KB;        // 16-byte pieces of a tile's keys, of a tile
@@ -848,7 +887,7 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, c32 = lane & 31, wave = uniform(tid >> 6);
   const int su = (wave >> 1) & 1, sub = wave >> 2;      // staging: block su of a tile, its keys or its values
   const bool values = wave & 1;
-  for_share<64 * WQ>(a, BM, 2, pre, [&](int hk, const Unit& un, int first, int cnt, int slot) {
+  for_share<64 * WQ>(a, spans, BM, 2, pre, [&](int hk, const Unit& un, int first, int cnt, int slot) {
     const int c = un.c0 + wave * 32 + c32, cc = min(c, un.M - 1), tok = cc / a.G, head = hk * a.G + cc - tok * a.G;
     const int last = un.L - un.n + tok, lowest = a.window > 0 ? last - a.window + 1 : 0;
     const int full = uniform(un.L / B), open_rows = uniform(un.L % B), b_at = uniform(un.b_lo + 2 * first);
@@ -1119,8 +1158,8 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
 
 // k_paged_join: the parts of a unit's columns, brought to one maximum and added in a fixed order.  Eight
 // groups of d / 4 lanes share a column's parts.
-template <int D>
-__global__ __launch_bounds__(2 * D) void k_paged_join(PagedAttendArgs a, int bm, int round) {
+template <int D, class SP>
+__global__ __launch_bounds__(2 * D) void k_paged_join(PagedAttendArgs a, SP spans, int bm, int round) {
   constexpr int L4 = D / 4, NG = 8;
   const int hk = blockIdx.x / a.units, u = blockIdx.x % a.units, c = blockIdx.y;
   const int64_t share = a.plan[0], one = a.plan[1 + a.units];
@@ -1129,7 +1168,7 @@ __global__ __launch_bounds__(2 * D) void k_paged_join(PagedAttendArgs a, int bm,
   const int g0 = (int)(x0 / share), g1 = (int)((x1 - 1) / share);
   if (g0 == g1) return;
   __shared__ Streams streams;
-  load_streams(a, streams);
+  load_streams(a, spans, streams);
   const Unit un = unit_of(a, streams, u, bm, round);
   if (c >= min(bm, un.M - un.c0)) return;
   __shared__ __align__(16) f32x4 so[NG][L4];
@@ -1192,7 +1231,7 @@ __global__ __launch_bounds__(2 * D) void k_paged_join(PagedAttendArgs a, int bm,
 
 // The same where units have many columns and few parts: a group of d / 4 lanes a column.
 template <int D>
-__global__ __launch_bounds__(256) void k_paged_join_many(PagedAttendArgs a, int bm, int round) {
+__global__ __launch_bounds__(256) void k_paged_join_many(PagedAttendArgs a, Spans spans, int bm, int round) {
   constexpr int L4 = D / 4, ROWS = 256 / L4;
   const int hk = blockIdx.x / a.units, u = blockIdx.x % a.units;
   const int64_t share = a.plan[0], one = a.plan[1 + a.units];
@@ -1201,7 +1240,7 @@ __global__ __launch_bounds__(256) void k_paged_join_many(PagedAttendArgs a, int 
   const int g0 = (int)(x0 / share), g1 = (int)((x1 - 1) / share);
   if (g0 == g1) return;
   __shared__ Streams streams;
-  load_streams(a, streams);
+  load_streams(a, spans, streams);
   const Unit un = unit_of(a, streams, u, bm, round);
   const int c = blockIdx.y * ROWS + threadIdx.x / L4, d = threadIdx.x % L4 * 4;
   if (c >= min(bm, un.M - un.c0)) return;
@@ -1222,45 +1261,74 @@ __global__ __launch_bounds__(256) void k_paged_join_many(PagedAttendArgs a, int 
   finish(a, hk * a.G + col % a.G, un.start + col / a.G, d, o, m, l);
 }
 
-template <int D>
-hipError_t attend_impl(const PagedAttendArgs& a, const PagedAttendPlan& p, hipStream_t st) {
+// The kernels of few columns, with the spans that they take.
+template <int D, class SP>
+hipError_t few_impl(const PagedAttendArgs& a, const SP& spans, const PagedAttendPlan& p, hipStream_t st) {
   const dim3 grid((unsigned)(a.n_wg ? a.n_wg : a.units * a.c.Hk));
-  if (p.bm == 16) hipLaunchKernelGGL((k_paged_few<D, 16>), grid, dim3(256), 0, st, a);
-  else if (p.bm == 32) hipLaunchKernelGGL((k_paged_few<D, 32>), grid, dim3(256), 0, st, a);
-  else if (p.bm == 128) hipLaunchKernelGGL((k_paged_many<D, 4>), grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((k_paged_many<D, 8>), grid, dim3(512), 0, st, a);
-  if (a.n_wg) {
-    const unsigned rows = (unsigned)(a.units * a.c.Hk);
-    if (p.bm <= 32 || a.n_wg > 4 * (int64_t)rows) {     // many parts a unit
-      hipLaunchKernelGGL((k_paged_join<D>), dim3(rows, (unsigned)a.cols), dim3(2 * D), 0, st, a, p.bm, p.round);
-    } else {
-      const int per = 256 / (D / 4);
-      hipLaunchKernelGGL((k_paged_join_many<D>), dim3(rows, (unsigned)((a.cols + per - 1) / per)), dim3(256), 0, st, a,
-                         p.bm, p.round);
-    }
+  // where blocks are few, eight waves each share a unit's pages
+  const bool wide = a.n_wg == 0 && grid.x <= 256;
+  if (p.bm == 16 && wide) hipLaunchKernelGGL((k_paged_few<D, 16, 8, SP>), grid, dim3(512), 0, st, a, spans);
+  else if (p.bm == 16) hipLaunchKernelGGL((k_paged_few<D, 16, 4, SP>), grid, dim3(256), 0, st, a, spans);
+  else if (wide) hipLaunchKernelGGL((k_paged_few<D, 32, 8, SP>), grid, dim3(512), 0, st, a, spans);
+  else hipLaunchKernelGGL((k_paged_few<D, 32, 4, SP>), grid, dim3(256), 0, st, a, spans);
+  if (a.n_wg)
+    hipLaunchKernelGGL((k_paged_join<D, SP>), dim3((unsigned)(a.units * a.c.Hk), (unsigned)a.cols), dim3(2 * D), 0, st, a,
+                       spans, p.bm, p.round);
+  return hipGetLastError();
+}
+
+template <int D>
+hipError_t attend_impl(const PagedAttendArgs& a, const Spans& spans, const PagedAttendPlan& p, hipStream_t st) {
+  if (p.bm <= 32)
+    return spans.uniform ? few_impl<D>(a, EvenSpans{spans.uniform}, p, st) : few_impl<D>(a, spans, p, st);
+  const unsigned rows = (unsigned)(a.units * a.c.Hk);
+  const dim3 grid(a.n_wg ? (unsigned)a.n_wg : rows);
+  if (p.bm == 128) hipLaunchKernelGGL((k_paged_many<D, 4>), grid, dim3(256), 0, st, a, spans);
+  else hipLaunchKernelGGL((k_paged_many<D, 8>), grid, dim3(512), 0, st, a, spans);
+  if (a.n_wg > 4 * (int64_t)rows) {                 // many parts a unit
+    hipLaunchKernelGGL((k_paged_join<D, Spans>), dim3(rows, (unsigned)a.cols), dim3(2 * D), 0, st, a, spans, p.bm, p.round);
+  } else if (a.n_wg) {
+    const int per = 256 / (D / 4);
+    hipLaunchKernelGGL((k_paged_join_many<D>), dim3(rows, (unsigned)((a.cols + per - 1) / per)), dim3(256), 0, st, a,
+                       spans, p.bm, p.round);
   }
+  return hipGetLastError();
+}
+
+template <int D, class SP>
+hipError_t append_impl(const PagedAppendArgs& a, const SP& spans, int h, hipStream_t st) {
+  const dim3 grid((unsigned)a.items, (unsigned)(a.c.Hk + (a.q.p ? (a.Hq + h - 1) / h : 0)));
+  if (h == 4) hipLaunchKernelGGL((k_paged_append<D, 4, SP>), grid, dim3(2 * D), 0, st, a, spans);
+  else hipLaunchKernelGGL((k_paged_append<D, 1, SP>), grid, dim3(2 * D), 0, st, a, spans);
   return hipGetLastError();
 }
 
 }  // namespace
 
+// Heads that a block rotates: four share its angles and have their loads under way together, where such
+// blocks fill the card; else one (1,777 tokens of 16 heads: 7.6 us with four, 6.7).
+static int heads_a_block(int64_t token_blocks, int heads) { return token_blocks * ((heads + 3) / 4) >= 256 ? 4 : 1; }
+
 hipError_t launch_rotate(const RotateArgs& a, int D, hipStream_t st) {
-  const dim3 grid((unsigned)((a.N + B - 1) / B), (unsigned)((a.heads + kRotateHeads - 1) / kRotateHeads));
-  if (D == 128) hipLaunchKernelGGL((k_rotate<128>), grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((k_rotate<64>), grid, dim3(128), 0, st, a);
+  const int rows = 256 / (D / 16), blocks = (a.N + rows - 1) / rows, h = heads_a_block(blocks, a.heads);
+  const dim3 grid((unsigned)blocks, (unsigned)((a.heads + h - 1) / h));
+  if (D == 128 && h == 4) hipLaunchKernelGGL((k_rotate<128, 4>), grid, dim3(256), 0, st, a);
+  else if (D == 128) hipLaunchKernelGGL((k_rotate<128, 1>), grid, dim3(256), 0, st, a);
+  else if (h == 4) hipLaunchKernelGGL((k_rotate<64, 4>), grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((k_rotate<64, 1>), grid, dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
-hipError_t launch_paged_append(const PagedAppendArgs& a, int D, hipStream_t st) {
-  const int qg = a.q.p ? (a.Hq + kRotateHeads - 1) / kRotateHeads : 0;
-  const dim3 grid((unsigned)a.items, (unsigned)(a.c.Hk + qg));
-  if (D == 128) hipLaunchKernelGGL((k_paged_append<128>), grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((k_paged_append<64>), grid, dim3(128), 0, st, a);
-  return hipGetLastError();
+hipError_t launch_paged_append(const PagedAppendArgs& a, const Spans& spans, int D, hipStream_t st) {
+  const int h = heads_a_block(a.items, a.Hq);
+  const EvenSpans even = {spans.uniform};
+  if (spans.uniform) return D == 128 ? append_impl<128>(a, even, h, st) : append_impl<64>(a, even, h, st);
+  return D == 128 ? append_impl<128>(a, spans, h, st) : append_impl<64>(a, spans, h, st);
 }
 
-hipError_t launch_paged_attend(const PagedAttendArgs& a, const PagedAttendPlan& p, int D, hipStream_t st) {
-  return D == 128 ? attend_impl<128>(a, p, st) : attend_impl<64>(a, p, st);
+hipError_t launch_paged_attend(const PagedAttendArgs& a, const Spans& spans, const PagedAttendPlan& p, int D,
+                               hipStream_t st) {
+  return D == 128 ? attend_impl<128>(a, spans, p, st) : attend_impl<64>(a, spans, p, st);
 }
 
 }  // namespace ss

@@ -43,7 +43,6 @@ inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 constexpr size_t kLeastWorkspace = 256;
 constexpr int kMaxGroup = 16;
-constexpr int kJoinWork = 32;
 
 ss_status check_desc(const ss_cache_desc* d) {
   if (!d) return fail(SS_ERR_INVALID_ARGUMENT, "desc is NULL");
@@ -185,12 +184,11 @@ ss::Turn turn_of(const ss_rotary* r, const int64_t* positions, bool transposed) 
   return {r->freqs, positions, r->dims, r->interleaved ? 1 : 0, r->gain, transposed ? -1.0f : 1.0f};
 }
 
-ss::Spans spans_of(int32_t n_tokens, int n_streams, const int32_t* n) {
-  ss::Spans s;
+void fill_spans(ss::Spans& s, int32_t n_tokens, int n_streams, const int32_t* n) {
   s.uniform = 0;
   if (!n) {
     s.uniform = n_tokens / n_streams;
-    return s;
+    return;
   }
   int at = 0;
   for (int i = 0; i < n_streams; ++i) {
@@ -198,7 +196,6 @@ ss::Spans spans_of(int32_t n_tokens, int n_streams, const int32_t* n) {
     at += n[i];
   }
   s.start[n_streams] = at;
-  return s;
 }
 
 // How a call of attention is cut: see for_share in the kernels.  Sizes alone decide
@@ -231,12 +228,13 @@ ss_status plan_attend(const ss_cache* c, const ss_cache_streams* s, int32_t n_to
   if ((work + 1) * p.units > 0x7FFFFFFF)
     return fail(SS_ERR_UNSUPPORTED, "%d units of up to %lld blocks are more than 2^31", p.units, (long long)work);
   const int64_t all = work * p.units * Hk;
-  p.min_share = bm <= 32 ? 32 : 8;
+  p.min_share = 8;
   // A block a unit leaves part of the last round of blocks idle; shares fill all rounds, but their parts are
-  // joined, which costs about as much as kJoinWork blocks (pairs) of work.
+  // joined by another kernel, which costs about as much as so many blocks (pairs) of work.
+  const int64_t join_work = bm <= 32 ? 64 : 32;
   const int64_t room = bm == 256 ? 256 : bm == 128 && D == 64 ? 768 : 512, blocks = (int64_t)p.units * Hk;
   const int64_t idle = (cdiv(blocks, room) * room - blocks) * work / room;
-  if (idle <= kJoinWork || p.units > ss::kPagedUnits) {
+  if (idle <= join_work || p.units > ss::kPagedUnits) {
     p.n_wg = 0;
     p.o_bytes = p.ml_bytes = p.plan_bytes = 0;
     return SS_OK;
@@ -363,15 +361,16 @@ ss_status ss_cache_append(ss_cache* cache, const ss_cache_streams* streams, int3
     a.turn = turn_of(rotary, positions, false);
     a.Hq = cache->desc.n_q_heads;
     a.S = streams->n_streams;
-    a.spans = spans_of(n_tokens, a.S, n_new);
+    ss::Spans spans;
+    fill_spans(spans, n_tokens, a.S, n_new);
     constexpr int B = ss::kBlockTokens;
     a.items = 0;
     if (n_new) {
       for (int i = 0; i < a.S; ++i) a.items += n_new[i] > 0 ? (n_new[i] + 2 * B - 2) / B : 0;
     } else {
-      a.items = a.S * ((a.spans.uniform + 2 * B - 2) / B);
+      a.items = a.S * ((spans.uniform + 2 * B - 2) / B);
     }
-    const hipError_t e = ss::launch_paged_append(a, cache->desc.head_dim, static_cast<hipStream_t>(stream));
+    const hipError_t e = ss::launch_paged_append(a, spans, cache->desc.head_dim, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return fail(SS_ERR_DEVICE, "append launch failed: %s", hipGetErrorString(e));
     return SS_OK;
   });
@@ -433,8 +432,9 @@ ss_status ss_cache_attend(const ss_cache* cache, const ss_cache_streams* streams
     a.cols = p.cols;
     a.n_wg = p.n_wg;
     a.min_share = p.min_share;
-    a.spans = spans_of(n_tokens, a.S, n_q);
-    const hipError_t e = ss::launch_paged_attend(a, p, d.head_dim, static_cast<hipStream_t>(stream));
+    ss::Spans spans;
+    fill_spans(spans, n_tokens, a.S, n_q);
+    const hipError_t e = ss::launch_paged_attend(a, spans, p, d.head_dim, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return fail(SS_ERR_DEVICE, "attention launch failed: %s", hipGetErrorString(e));
     return SS_OK;
   });

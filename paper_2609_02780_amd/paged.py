@@ -12,24 +12,44 @@ import ctypes as C
 import torch
 
 from . import _lib as L
-from .index import _memory_of, _on_current, _returned_from, _stream_handle, _used_on
+from .index import _on_current, _raw_stream, _returned_from, _stream_handle, _used_on
 
 _BF16 = torch.bfloat16
 
 
-def _rows(t, heads: int, tokens: int, d: int, device, what: str) -> L.Rows:
-    """A tensor ``[heads][tokens][d]`` as the C ABI takes it (which checks alignment and strides)."""
-    if not isinstance(t, torch.Tensor) or t.dtype != _BF16:
+def _rows(t, shape: tuple, device, what: str) -> L.Rows:
+    """A tensor ``[heads][tokens][d]`` of this shape as the C ABI takes it (which checks alignment and strides)."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not _BF16:
         raise ValueError(f"{what} must be a bfloat16 tensor")
-    if t.shape != (heads, tokens, d):
-        raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {(heads, tokens, d)}")
+    if t.shape != shape:
+        raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {shape}")
     if t.device != device:
         raise ValueError(f"{what} lives on {t.device}, expected {device}")
+    return _strides(t, what)
+
+
+def _strides(t, what: str) -> L.Rows:
+    heads, tokens, _ = t.shape
     hs, ts, one = t.stride()
     if one != 1:
         raise ValueError(f"the elements of a row of {what} must lie side by side")
     # a dimension of one row has any stride
     return L.Rows(t.data_ptr(), hs if heads > 1 else 0, ts if tokens > 1 else 0)
+
+
+def _new(stream, f, *args, **kw):
+    """``f``'s new tensor, in memory of the stream that fills it."""
+    if stream is None:
+        return f(*args, **kw)
+    with torch.cuda.stream(stream):
+        return f(*args, **kw)
+
+
+def _launch_stream(stream, device) -> int:
+    """The handle of the stream that a call on the current device runs on."""
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(device.index)
+    return _stream_handle(stream)
 
 
 def _ints(t, shape, dtype, device, what: str) -> int:
@@ -59,7 +79,7 @@ class Rotary:
         self.dims, self.interleaved = dims, bool(interleaved)
         self.gain = float(g.value if gain is None else gain)
         self.freqs = freqs.to(dev)          # turns a position
-        self._device = self.freqs.device
+        self._device, self._lib = self.freqs.device, L.lib()
         self._c = L.Rotary(self.freqs.data_ptr(), dims, int(self.interleaved), self.gain)
         self._ref = C.byref(self._c)
 
@@ -71,17 +91,17 @@ class Rotary:
             raise ValueError("x must be [heads][tokens][d]")
         _on_current(self._device, "the frequencies live")
         H, N, d = x.shape
-        src = _rows(x, H, N, d, self._device, "x")
-        at = _ints(positions, (N,), torch.int64, self._device, "positions")
-        if out is None:
-            with _memory_of(stream):
-                out = torch.empty_like(x)
-            fresh = True
+        dev = self._device
+        src = _rows(x, (H, N, d), dev, "x")
+        at = _ints(positions, (N,), torch.int64, dev, "positions")
+        fresh = out is None
+        if fresh:
+            out = _new(stream, torch.empty_like, x)
+            dst = _strides(out, "out")
         else:
-            fresh = False
-        dst = _rows(out, H, N, d, self._device, "out")
-        L.check(L.lib().ss_rotate(self._ref, H, N, d, C.byref(src), at, int(transposed), C.byref(dst),
-                                  _stream_handle(stream)))
+            dst = _rows(out, (H, N, d), dev, "out")
+        L.check(self._lib.ss_rotate(self._ref, H, N, d, C.byref(src), at, transposed, C.byref(dst),
+                                    _launch_stream(stream, dev)))
         if stream is not None:
             _used_on(stream, x, positions, self.freqs)
             if fresh:
@@ -99,11 +119,11 @@ class PagedCache:
     (:class:`PagedBatch`).  A stream's tokens behind its last full block stay bfloat16 in one
     of ``n_slots`` slots.
 
-    The views below may be read and written.  ``keys`` is ``[L][n_pages][H_kv][32][d/16][16]``
-    and ``values`` ``[L][n_pages][H_kv][2][2][2][4][d/32][32]``, both ``[...][32][d]`` with tokens and
-    dimensions cut as memory has them (``reshape`` to that copies); ``key_scales`` and
-    ``value_scales`` fp32 ``[L][n_pages][H_kv]``; ``open_keys`` and ``open_values`` bfloat16
-    ``[L][n_slots][2][H_kv]`` and then as the pages, block ``b`` in half ``b & 1``.
+    The views below hold one tensor a layer, which may be read and written.  ``keys[l]`` is
+    ``[n_pages][H_kv][32][d/16][16]`` and ``values[l]`` ``[n_pages][H_kv][2][2][2][4][d/32][32]``, both
+    ``[...][32][d]`` with tokens and dimensions cut as memory has them (``reshape`` to that copies);
+    ``key_scales[l]`` and ``value_scales[l]`` fp32 ``[n_pages][H_kv]``; ``open_keys[l]`` and
+    ``open_values[l]`` bfloat16 ``[n_slots][2][H_kv]`` and then as the pages, block ``b`` in half ``b & 1``.
     """
 
     def __init__(self, n_layers: int, n_q_heads: int, n_kv_heads: int, head_dim: int, n_pages: int, n_slots: int,
@@ -139,10 +159,10 @@ class PagedCache:
             return (k.permute(*lead, n + 1, n, n + 2), v.permute(*lead, n + 4, n + 3, n + 1, n + 5, n, n + 2))
 
         k, v = part(torch.float8_e4m3fn, *pages, *key), part(torch.float8_e4m3fn, *pages, *value)
-        self.keys, self.values = by_token(k, v)
-        self.key_scales, self.value_scales = part(torch.float32, *pages), part(torch.float32, *pages)
+        self.keys, self.values = (t.unbind(0) for t in by_token(k, v))
+        self.key_scales, self.value_scales = part(torch.float32, *pages).unbind(0), part(torch.float32, *pages).unbind(0)
         k, v = part(_BF16, *slots, *key), part(_BF16, *slots, *value)
-        self.open_keys, self.open_values = by_token(k, v)
+        self.open_keys, self.open_values = (t.unbind(0) for t in by_token(k, v))
 
     @property
     def handle(self) -> C.c_void_p:
@@ -193,6 +213,7 @@ class PagedBatch:
         self._ref = C.byref(self._c)
         self._counts_type = C.c_int32 * max(S, 1)
         self._least = torch.empty(256, dtype=torch.uint8, device=dev)
+        self._needs = {}
 
     def _counts(self, n, what: str):
         if n is None:
@@ -212,8 +233,9 @@ class PagedBatch:
         if not isinstance(keys, torch.Tensor) or keys.dim() != 3:
             raise ValueError("keys must be [n_kv_heads][tokens][d]")
         N, d = keys.shape[1], c.head_dim
-        k = _rows(keys, c.n_kv_heads, N, d, dev, "keys")
-        v = _rows(values, c.n_kv_heads, N, d, dev, "values")
+        shape = (c.n_kv_heads, N, d)
+        k = _rows(keys, shape, dev, "keys")
+        v = _rows(values, shape, dev, "values")
         rot, at = None, None
         if rotary is not None:
             if rotary._device != dev:
@@ -224,15 +246,17 @@ class PagedBatch:
         q = qo = None
         out = queries_out
         if queries is not None:
-            q = C.byref(_rows(queries, c.n_q_heads, N, d, dev, "queries"))
+            shape = (c.n_q_heads, N, d)
+            q = C.byref(_rows(queries, shape, dev, "queries"))
             if out is None:
-                with _memory_of(stream):
-                    out = torch.empty_like(queries)
-            qo = C.byref(_rows(out, c.n_q_heads, N, d, dev, "queries_out"))
+                out = _new(stream, torch.empty_like, queries)
+                qo = C.byref(_strides(out, "queries_out"))
+            else:
+                qo = C.byref(_rows(out, shape, dev, "queries_out"))
         elif out is not None:
             raise ValueError("queries_out without queries")
         L.check(self._lib.ss_cache_append(c.handle, self._ref, layer, N, self._counts(n_new, "n_new"), C.byref(k),
-                                          C.byref(v), rot, at, q, qo, _stream_handle(stream)))
+                                          C.byref(v), rot, at, q, qo, _launch_stream(stream, dev)))
         if stream is not None:
             _used_on(stream, c.arena, self.tables, self.lengths, self.slots, keys, values, positions, queries,
                      queries_out, rotary.freqs if rotary is not None else None)
@@ -251,24 +275,29 @@ class PagedBatch:
         if not isinstance(queries, torch.Tensor) or queries.dim() != 3:
             raise ValueError("queries must be [n_q_heads][tokens][d]")
         N, d, Hq = queries.shape[1], c.head_dim, c.n_q_heads
-        q = _rows(queries, Hq, N, d, dev, "queries")
+        q = _rows(queries, (Hq, N, d), dev, "queries")
         po = pl = None
         if prior is not None:
             o, z = prior
-            po = C.byref(_rows(o, Hq, N, d, dev, "prior out"))
+            po = C.byref(_rows(o, (Hq, N, d), dev, "prior out"))
             pl = _ints(z, (Hq, N), torch.float32, dev, "prior lse")
         n = self._counts(n_q, "n_q")
-        need = lib.ss_cache_attend_workspace_bytes(c.handle, self._ref, N, n, window)
-        if need == 0:
-            raise L.SSError(L.SS_ERR_INVALID_ARGUMENT, lib.ss_last_error().decode())
-        with _memory_of(stream):
-            # a need of 256, the least, is of a call that writes no workspace: those share one
-            ws = self._least if need == 256 else torch.empty(need, dtype=torch.uint8, device=dev)
-            out = torch.empty_like(queries)
-            lse = torch.empty((Hq, N), dtype=torch.float32, device=dev)
-        dst = _rows(out, Hq, N, d, dev, "out")
+        # (of calls with the same number of queries for every stream the size, which is theirs alone, is asked for once)
+        need = self._needs.get((N, window)) if n is None else None
+        if need is None:
+            need = lib.ss_cache_attend_workspace_bytes(c.handle, self._ref, N, n, window)
+            if need == 0:
+                raise L.SSError(L.SS_ERR_INVALID_ARGUMENT, lib.ss_last_error().decode())
+            if n is None:
+                if len(self._needs) >= 256:
+                    self._needs.clear()
+                self._needs[N, window] = need
+        # a need of 256, the least, is of a call that writes no workspace: those share one
+        ws = self._least if need == 256 else _new(stream, torch.empty, need, dtype=torch.uint8, device=dev)
+        out = _new(stream, torch.empty_like, queries)
+        lse = _new(stream, torch.empty, (Hq, N), dtype=torch.float32, device=dev)
         L.check(lib.ss_cache_attend(c.handle, self._ref, layer, N, n, C.byref(q), window, po, pl, ws.data_ptr(),
-                                    ws.numel(), _stream_handle(stream), C.byref(dst), lse.data_ptr()))
+                                    need, _launch_stream(stream, dev), C.byref(_strides(out, "out")), lse.data_ptr()))
         if stream is not None:
             _used_on(stream, c.arena, self.tables, self.lengths, self.slots, queries, *(prior or ()))
             _returned_from(stream, out, lse)
