@@ -675,8 +675,9 @@ ss_status ss_cache_append(ss_cache* cache, const ss_cache_streams* streams, int3
  *                 aligned), which the call leaves dirty: calls that may overlap need one each,
  *                 unless the size is 256, the least: those calls write nothing to it.
  * out and lse may overlap nothing that is read.  A query that sees nothing gives out = 0 and
- * lse = -inf.  Maxima, sums and outputs are fp32 until the one rounding at the end; p is
- * rounded to bf16 before it meets the values.  Seen rows must be finite; rows behind a
+ * lse = -inf.  Maxima, sums and outputs are fp32 until the one rounding at the end; p keeps
+ * at least 11 bits when it meets the values.  Seen rows must be finite, a stream's largest values in any two pages
+ * within 2^112 of each other; rows behind a
  * stream's end may hold anything.  A result is the same bit for bit each time. */
 size_t ss_cache_attend_workspace_bytes(const ss_cache* cache, const ss_cache_streams* streams, int32_t n_tokens,
                                        const int32_t* n_q, int32_t window);

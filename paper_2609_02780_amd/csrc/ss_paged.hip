@@ -21,6 +21,8 @@ namespace ss {
 namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -66,6 +68,20 @@ __device__ __forceinline__ u32x4 load_piece(__amdgpu_buffer_rsrc_t r, int at) {
   return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, kAuxNT));
 }
 
+__device__ __forceinline__ f32x16 mfma_half(u32x4 a, u32x4 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+// Eight e4m3 as fp16 (exact).
+__device__ __forceinline__ u32x4 widen_half(uint32_t lo, uint32_t hi) {
+  const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false);
+  const f16x2 b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true);
+  const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false);
+  const f16x2 d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true);
+  return u32x4{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, c),
+               __builtin_bit_cast(uint32_t, d)};
+}
+
 // Eight e4m3 times a power of two as bf16 (exact).
 __device__ __forceinline__ u32x4 widen(uint32_t lo, uint32_t hi, float scale) {
   const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
@@ -90,8 +106,10 @@ __device__ __forceinline__ int stream_length(const PagedDev& c, int s) {
 // ---------------------------------------------------------------------------
 // Rotation.  cos and sin of a block's tokens are formed once for all its heads: the angle
 // in turns, position * (f / 2 pi), in 64 bits (a far position times a frequency loses what
-// matters in 32), and of its fraction the hardware's sine and cosine, which take turns and are off by
-// at most 2^-22.9 over a turn (over all multiples of 2^-20).
+// matters in 32), less the nearest quarter turn, still in 64, and of the rest the Taylor series of sine and
+// cosine in 32 bits, cut behind x^9 and x^10 (x up to pi / 4: off by less than 2^-28), so that a rotated
+// row is as near as fp32 products make it.  (The hardware's sine and cosine, off by 2^-22.9, take less of a
+// time that the rows' traffic covers.)
 //
 // A thread takes 16 elements of a row as two groups of 8, so that what it loads is what it
 // writes: both elements of eight pairs (i, i + dims / 2) where the groups lie on 16 bytes; else
@@ -112,9 +130,21 @@ __device__ __forceinline__ void fill_angles(Angles<ROWS>& g, const Turn& t, int 
   const double f = t.freqs[j];
   for (int r = r0 + threadIdx.x / PAIRS; r < r1; r += blockDim.x / PAIRS) {
     const int64_t pos = t.positions ? t.positions[first + r] : pos0 + r;
-    const double turns = (double)pos * f;
-    const float x = (float)(turns - rint(turns));
-    g.cs[r][j] = make_float2(t.gain * __builtin_amdgcn_cosf(x), t.gain * t.sign * __builtin_amdgcn_sinf(x));
+    const double quarters = (double)pos * f * 4.0, q = rint(quarters);
+    const float x = (float)(quarters - q) * 1.57079632679489662f, z = x * x;
+    float c = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -1.0f / 3628800.0f, 1.0f / 40320.0f), -1.0f / 720.0f), 1.0f / 24.0f), -0.5f), 1.0f);
+    float s = x * fmaf(z, fmaf(z, fmaf(z, fmaf(z, 1.0f / 362880.0f, -1.0f / 5040.0f), 1.0f / 120.0f), -1.0f / 6.0f), 1.0f);
+    const int k = (int)(q - 4.0 * floor(q * 0.25));               // quarter turns, 0 .. 3
+    if (k & 1) {
+      const float y = c;
+      c = -s;
+      s = y;
+    }
+    if (k & 2) {
+      c = -c;
+      s = -s;
+    }
+    g.cs[r][j] = make_float2(t.gain * c, t.gain * t.sign * s);
   }
 }
 
@@ -566,6 +596,22 @@ __device__ __forceinline__ void running_softmax(float& m, float& l, Form&& form,
   l += sum;
 }
 
+// The same for p in fp16: form(mu) returns the sum of p with the value scale, which has to stay in its range, and the
+// one without; top() is the largest of the scores with it.
+template <class Form, class Top, class Scale>
+__device__ __forceinline__ void running_softmax_half(float& m, float& l, Form&& form, Top&& top, Scale&& rescale) {
+  float2 sum = form(m == neg_inf() ? 0.0f : m);
+  if (__any(!(sum.x <= 32768.0f) || m == neg_inf())) {
+    const float mn = fmaxf(m, top() - 6.0f);
+    const float al = m == neg_inf() ? 0.0f : exp2_fast(m - mn);
+    m = mn;
+    l *= al;
+    rescale(al);
+    sum = form(m == neg_inf() ? 0.0f : m);
+  }
+  l += sum.y;
+}
+
 // A value scale is cut in two: p takes what lies in 2^-60 .. 2^60, the conversion of the
 // codes the rest, a power of two (blocks of zeros have the least scale, and their p must still count).
 struct ValueScale {
@@ -584,14 +630,34 @@ __device__ __forceinline__ u32x4 open_key(const uint16_t* base, int piece, int t
   return token < cnt ? v : u32x4{0, 0, 0, 0};
 }
 // 8 tokens of one dimension: words 2 y and 2 y + 1 of [c][h][m].
-__device__ __forceinline__ u32x4 open_value(const uint16_t* base, int c, int h, int m, int y, int cnt) {
-  u32x4 v = *reinterpret_cast<const u32x4*>(base + ((c * 2 + h) * 32 + m) * 16 + 8 * y);
+__device__ __forceinline__ u32x4 open_masked(u32x4 v, int h, int y, int cnt) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int tok = 8 * y + 16 * (i >> 1) + 4 * h + 2 * (i & 1);
     v[i] &= (tok < cnt ? 0xFFFFu : 0u) | (tok + 1 < cnt ? 0xFFFF0000u : 0u);
   }
   return v;
+}
+__device__ __forceinline__ u32x4 open_value(const uint16_t* base, int c, int h, int m, int y, int cnt) {
+  return open_masked(*reinterpret_cast<const u32x4*>(base + ((c * 2 + h) * 32 + m) * 16 + 8 * y), h, y, cnt);
+}
+// The largest magnitude of eight bf16, as bits, and the power of two that lifts it to 2^7.
+__device__ __forceinline__ uint32_t largest(u32x4 v) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) top = max(top, max(v[i] & 0x7FFFu, (v[i] >> 16) & 0x7FFFu));
+  return top;
+}
+__device__ __forceinline__ int exponent_of(uint32_t top) { return (int)max(top >> 7, 1u) - 127 - 7; }
+// Eight bf16 times 2^-e as fp16.
+__device__ __forceinline__ u32x4 halves(u32x4 v, int e) {
+  f16x8 x;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = (_Float16)ldexpf(__uint_as_float(v[i] << 16), -e);
+    x[2 * i + 1] = (_Float16)ldexpf(__uint_as_float(v[i] & 0xFFFF0000u), -e);
+  }
+  return __builtin_bit_cast(u32x4, x);
 }
 
 __device__ __forceinline__ float of_lane(float x, int lane) {
@@ -872,6 +938,11 @@ __device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts
 // k_paged_many: units of 32 WQ columns, 32 a wave.  The waves stage tiles of two blocks (64
 // tokens) together: 8-bit pieces from memory to registers a tile ahead, widened once into
 // LDS, where a fragment is a run of 1 KB.
+// The products are of fp16: e4m3 is exact in it, and its 11 bits of p are off by an eighth of what bf16's 8 are,
+// at the same cost.  What is bf16, queries and open rows, is brought into its range by a power of two that
+// lifts the largest of a column (a block) to 2^7: exact, but for elements 2^21 times smaller.  p's range is kept by
+// what m is: the largest score with its value scale (against that of the first block, a power of two that the output
+// takes at the end), less 6, so that p reaches up to 2^6 (2^15 before m moves) and is lost only below 2^-31 of it.
 // WQ = 8: the two waves of a SIMD (w and w + 4) take turns: while one forms its softmax on the
 // vector unit, the other keeps the matrix unit busy, half an iteration behind.  WQ = 4 (33 to 128
 // columns): two blocks a CU, whose phases fall beside each other by themselves.
@@ -882,7 +953,9 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
   constexpr int KB = 2 * KST * 64, TB = 2 * KB;        // 16-byte pieces of a tile's keys, of a tile
   static_assert(NCH >= 1);
   __shared__ __align__(16) u32x4 ring[NS][TB];
-  __shared__ float4 meta[2][64][2];   // of a tile's blocks, 64 tiles at a time: score scale; value scale (0: not seen)
+  __shared__ __align__(16) float2 meta[2][64][2];   // of a tile's blocks, 64 tiles at a time: key scale (0: not seen), log 2
+                                                    // of the value scale against the unit's
+  __shared__ int open_power[2];       // of the open block's keys, of its values
   __shared__ int pre[kPagedUnits + 1];
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, c32 = lane & 31, wave = uniform(tid >> 6);
   const int su = (wave >> 1) & 1, sub = wave >> 2;      // staging: block su of a tile, its keys or its values
@@ -903,29 +976,44 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
 #pragma unroll
       for (int i = 0; i < KST; ++i) qf[i] = *reinterpret_cast<const u32x4*>(q + ((i >> 1) * 2 + half) * 16 + 8 * (i & 1));
     }
+    float qs;                          // what the column's scores are multiplied by
+    {
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < KST; ++i) top = max(top, largest(qf[i]));
+      top = max(top, __float_as_uint(other_half(__uint_as_float(top))));
+      const int e = exponent_of(top);
+#pragma unroll
+      for (int i = 0; i < KST; ++i) qf[i] = halves(qf[i], e);
+      qs = ldexpf(a.c1, e);
+    }
     f32x16 O[NC];
 #pragma unroll
     for (int i = 0; i < NC; ++i) O[i] = f32x16{};
-    float m = neg_inf(), l = 0.0f;
+    float m = neg_inf(), l = 0.0f, unit_e = 0.0f;
 
     // (kept in registers: read again from the arguments in every tile they cost a trip each)
     const uint8_t* pages = (values ? a.c.v8 : a.c.k8) + hk * (B * D);
     int page_stride = a.c.Hk * (B * D);
     asm volatile("" : "+s"(pages), "+s"(page_stride));
-    int ids = -1;                      // a lane the page of one of 64 tiles, and what its codes are scaled by
-    float codes = 1.0f;
+    int ids = -1;                      // a lane the page of one of 64 tiles
+    auto open_piece = [&](int ch, int x) {
+      const int64_t at = (((int64_t)sl * 2 + (full & 1)) * a.c.Hk + hk) * (B * D);
+      return values ? open_value(a.c.ov + at, ch, half, c32, x, open_rows)
+                    : open_key(a.c.ok + at, 2 * ch + half, c32, x, open_rows);
+    };
+    // against the unit's value scale, as far as fp32 goes (blocks 2^112 apart)
+    auto against = [&](float e) { return fminf(fmaxf(e - unit_e, -112.0f), 112.0f); };
     // pages and scales of tiles t .. t + 63; they may be used behind the next barrier
     auto look_up = [&](int t) {
       const int b = b_at + 2 * (t + lane) + su;
       ids = t + lane < cnt && b < full ? table[b] : -1;
       if ((unsigned)ids >= (unsigned)a.c.n_pages) ids = -1;
-      float4 x = make_float4(a.c1, 0.0f, 1.0f, b == full && open_rows > 0 && has_slot ? 1.0f : 0.0f);
-      if (ids >= 0) {
-        const ValueScale vs = cut_scale(a.c.vs[(int64_t)ids * a.c.Hk + hk]);
-        x = make_float4(a.c.ks[(int64_t)ids * a.c.Hk + hk] * a.c1, vs.log2, vs.inverse, 1.0f);
-        if (values) codes = vs.codes;
-      }
-      if (!values && sub == 0) meta[(t >> 6) & 1][lane][su] = x;
+      if (values || sub != 0) return;
+      float2 x = {0.0f, 0.0f};                               // (an open block's: put_open)
+      if (ids >= 0)
+        x = make_float2(a.c.ks[(int64_t)ids * a.c.Hk + hk], against(log2_fast(a.c.vs[(int64_t)ids * a.c.Hk + hk])));
+      meta[(t >> 6) & 1][lane][su] = x;
     };
     // this wave's pieces of tile t, to registers; of no page, or behind the last tile, none are read
     auto fetch = [&](int t, u32x4 (&raw)[NCH]) {
@@ -936,27 +1024,26 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
       for (int i = 0; i < NCH; ++i) raw[i] = load_shared(p, (sub * NCH + i) * 1024 + lane * 16);
     };
     // and widened to LDS, piece by piece (2 NCH)
-    auto put = [&](int t, const u32x4 (&raw)[NCH], int i, float x) {
+    auto put = [&](int t, const u32x4 (&raw)[NCH], int i) {
       u32x4* to = ring[t % NS] + (values ? KB : 0) + (su * KST + 2 * sub * NCH) * 64 + lane;
-      to[64 * i] = widen(raw[i >> 1][2 * (i & 1)], raw[i >> 1][2 * (i & 1) + 1], x);
+      to[64 * i] = widen_half(raw[i >> 1][2 * (i & 1)], raw[i >> 1][2 * (i & 1) + 1]);
     };
     // an open block comes from its slot instead
     auto put_open = [&](int t) {
       if (t >= cnt || b_at + 2 * t + su != full || open_rows == 0 || !has_slot) return;
       u32x4* to = ring[t % NS] + (values ? KB : 0) + (su * KST + 2 * sub * NCH) * 64 + lane;
-      const int64_t at = (((int64_t)sl * 2 + (full & 1)) * a.c.Hk + hk) * (B * D);
+      const int e = open_power[values];
 #pragma unroll
-      for (int i = 0; i < NCH; ++i)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const int ch = sub * NCH + i;
-          to[128 * i + 64 * x] = values ? open_value(a.c.ov + at, ch, half, c32, x, open_rows)
-                                        : open_key(a.c.ok + at, 2 * ch + half, c32, x, open_rows);
-        }
+      for (int i = 0; i < 2 * NCH; ++i) to[64 * i] = halves(open_piece(sub * NCH + (i >> 1), i & 1), e);
+      if (sub == 0 && lane == 0) {
+        float2& x = meta[(t >> 6) & 1][t & 63][su];
+        if (values) x.y = against((float)e);
+        else x.x = ldexpf(1.0f, e);
+      }
     };
     auto stage = [&](int t, const u32x4 (&raw)[NCH]) {
 #pragma unroll
-      for (int i = 0; i < 2 * NCH; ++i) put(t, raw, i, of_lane(codes, t & 63));
+      for (int i = 0; i < 2 * NCH; ++i) put(t, raw, i);
       put_open(t);
     };
 
@@ -978,7 +1065,7 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
 #pragma unroll
       for (int x = 0; x < KF; ++x) {
         const int n = step * KF + x, i = n >> 1, u = n & 1;
-        S[u] = mfma32(f[x], qf[i], i == 0 ? f32x16{} : S[u]);
+        S[u] = mfma_half(f[x], qf[i], i == 0 ? f32x16{} : S[u]);
       }
     };
     auto read_values = [&](int t, int step, u32x4 (&f)[FR]) {
@@ -1000,7 +1087,6 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
     // `next` are widened between the products, whose time on the matrix unit covers them (in the softmax's
     // half of an iteration they cost their full 600 clocks).
     auto add_values = [&](int t, int next, const u32x4 (&raw)[NCH], auto&& more) {
-      const float x = of_lane(codes, next & 63);
       constexpr int GAP = VS * NC / (2 * NCH);
 #pragma unroll
       for (int k = 0; k < VS; ++k) {
@@ -1009,53 +1095,56 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
-          O[i] = mfma32(fr[k & 1][i], pb[k], O[i]);
+          O[i] = mfma_half(fr[k & 1][i], pb[k], O[i]);
           const int n = k * NC + i + 1;
           if (n % GAP == 0) {
-            put(next, raw, n / GAP - 1, x);
+            put(next, raw, n / GAP - 1);
             __builtin_amdgcn_sched_barrier(0);
           }
         }
         __builtin_amdgcn_sched_barrier(0);
       }
     };
-    auto softmax = [&](int t, const float4 (&mt)[2]) {
+    auto softmax = [&](int t, const float4& mt) {
       float cs[2], lv[2], rs[2], v[32];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const float4 x = mt[u];
-        cs[u] = x.x;
+        const float2 x = u ? make_float2(mt.z, mt.w) : make_float2(mt.x, mt.y);
+        cs[u] = x.x * qs;
         lv[u] = x.y;
-        rs[u] = x.z;
+        rs[u] = exp2_fast(-x.y);
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[u * 16 + i] = S[u][i];
         const int b = b_at + 2 * t + u;
         if (b * B + B - 1 > p_lo || b * B < w_lo) hide(v + u * 16, b, half, last, lowest);
-        if (__any(x.w == 0.0f)) {
+        if (__any(x.x == 0.0f)) {
+          cs[u] = 1.0f;
 #pragma unroll
           for (int i = 0; i < 16; ++i) v[u * 16 + i] = neg_inf();
         }
       }
-      running_softmax(
+      running_softmax_half(
           m, l,
           [&](float mu) {
-            float all = 0.0f;
+            float2 all = {0.0f, 0.0f};
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
               const float off = lv[u] - mu;
               float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
               for (int w = 0; w < 2; ++w) {
-                bf16x8 x;
+                f16x8 x;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                   const float p = exp2_fast(fmaf(v[u * 16 + 4 * w + (e & 3) + 8 * (e >> 2)], cs[u], off));
                   sum[e & 3] += p;
-                  x[e] = (__bf16)p;
+                  x[e] = (_Float16)p;
                 }
                 pb[u * 2 + w] = __builtin_bit_cast(u32x4, x);
               }
-              all = fmaf((sum[0] + sum[1]) + (sum[2] + sum[3]), rs[u], all);
+              const float one = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+              all.x += one;
+              all.y = fmaf(one, rs[u], all.y);
             }
             return all;
           },
@@ -1066,7 +1155,7 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
               top[0] = fmaxf(top[0], v[i]);
               top[1] = fmaxf(top[1], v[16 + i]);
             }
-            const float x = fmaxf(top[0] * cs[0], top[1] * cs[1]);
+            const float x = fmaxf(fmaf(top[0], cs[0], lv[0]), fmaf(top[1], cs[1], lv[1]));
             return fmaxf(x, other_half(x));
           },
           [&](float al) {
@@ -1082,6 +1171,25 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
 
     meet();                           // the unit before is read
     look_up(0);
+    if (wave < 2 && b_at + 2 * cnt > full && open_rows > 0 && has_slot) {
+      u32x4 x[2 * NC];
+#pragma unroll
+      for (int i = 0; i < 2 * NC; ++i) x[i] = open_piece(i >> 1, i & 1);
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 2 * NC; ++i) top = max(top, largest(x[i]));
+#pragma unroll
+      for (int i = 32; i > 0; i >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, i));
+      if (lane == 0) open_power[wave] = exponent_of(top);
+    }
+    meet();
+    // the unit's value scale: that of its first block, as a power of two
+    unit_e = floorf(meta[0][0][0].y);
+    meet();
+    if (tid < 128) {
+      float& y = meta[0][tid >> 1][tid & 1].y;
+      if (meta[0][tid >> 1][tid & 1].x != 0.0f) y = against(y);
+    }
     meet();
     constexpr int AHEAD = TURNS ? 2 : 1;      // a tile is staged so many iterations before its softmax, fetched one more
     u32x4 raw[NCH];
@@ -1104,7 +1212,7 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
       scores(0, 0);
       if (second) meet();
       for (int t = 0; t < cnt; ++t) {
-        const float4 mt[2] = {meta[(t >> 6) & 1][t & 63][0], meta[(t >> 6) & 1][t & 63][1]};
+        const float4 mt = *reinterpret_cast<const float4*>(meta[(t >> 6) & 1][t & 63]);
         __builtin_amdgcn_sched_barrier(0);
         softmax(t, mt);
         read_values(t, 0, fr[0]);
@@ -1121,7 +1229,7 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
       if (!second) meet();
     } else {
       for (int t = 0; t < cnt; ++t) {
-        const float4 mt[2] = {meta[(t >> 6) & 1][t & 63][0], meta[(t >> 6) & 1][t & 63][1]};
+        const float4 mt = *reinterpret_cast<const float4*>(meta[(t >> 6) & 1][t & 63]);
         read_keys(t, 0, fr[0]);
         __builtin_amdgcn_sched_barrier(0);
         scores(t, 0);
@@ -1136,6 +1244,9 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
     }
     l += other_half(l);
     if (c >= un.M) return;
+    const float unit_scale = exp2_fast(unit_e);
+#pragma unroll
+    for (int i = 0; i < NC; ++i) O[i] *= unit_scale;
 #pragma unroll
     for (int i = 0; i < NC; ++i)
 #pragma unroll
