@@ -590,9 +590,9 @@ typedef struct {
 } ss_rows;
 
 /* Rotate n_tokens (1..65536) rows of n_heads (1..4096) heads.  positions: device int64
- * [n_tokens], below 2^31 in magnitude.  With `transposed` the transposed rotation (-sin), which is the
- * gradient of the other one, and undoes it when gain is 1.  `out` may be x, rows
- * and strides alike; else they may not overlap. */
+ * [n_tokens], below 2^31 in magnitude.  With `transposed` the transposed rotation (-sin),
+ * which is the gradient of the other one, and undoes it when gain is 1.  `out` may be x,
+ * rows and strides alike; else they may not overlap. */
 ss_status ss_rotate(const ss_rotary* rotary, int32_t n_heads, int32_t n_tokens, int32_t head_dim, const ss_rows* x,
                     const int64_t* positions, int32_t transposed, const ss_rows* out, void* stream);
 
@@ -675,10 +675,12 @@ ss_status ss_cache_append(ss_cache* cache, const ss_cache_streams* streams, int3
  *                 aligned), which the call leaves dirty: calls that may overlap need one each,
  *                 unless the size is 256, the least: those calls write nothing to it.
  * out and lse may overlap nothing that is read.  A query that sees nothing gives out = 0 and
- * lse = -inf.  Maxima, sums and outputs are fp32 until the one rounding at the end; p keeps
- * at least 11 bits when it meets the values.  Seen rows must be finite, a stream's largest values in any two pages
- * within 2^112 of each other; rows behind a
- * stream's end may hold anything.  A result is the same bit for bit each time. */
+ * lse = -inf.  Maxima, sums and outputs are fp32 until the one rounding at the end; p,
+ * times its block's value scale, keeps at least 11 bits or steps of 2^-33 of the largest
+ * such product when it meets the values.  Queries and the blocks that one sees must be
+ * finite, values at most 2^48 (values of a block in which all are below 2^-55 may count as
+ * zeros); blocks that none sees, and rows behind a stream's end, may hold anything.  A
+ * result is the same bit for bit each time. */
 size_t ss_cache_attend_workspace_bytes(const ss_cache* cache, const ss_cache_streams* streams, int32_t n_tokens,
                                        const int32_t* n_q, int32_t window);
 ss_status ss_cache_attend(const ss_cache* cache, const ss_cache_streams* streams, int32_t layer, int32_t n_tokens,

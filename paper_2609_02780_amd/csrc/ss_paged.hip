@@ -10,8 +10,9 @@
 //           32 c + l % 32, the 16 tokens whose scores its half of S^T holds,
 //           8 g + 4 (l / 32) + e, in the order of groups g = 0, 2, 1, 3.
 // Elements are e4m3 with a scale for each page, or bf16 in an open block.  e4m3 is
-// exact in bf16, so the products are bf16 MFMAs with fp32 sums; a key scale meets the
-// scores, a value scale joins the exponent of p.
+// exact in bf16 and in fp16, so the products are MFMAs of these with fp32 sums (bf16 where
+// reading the pages bounds, fp16 where the products do); a key scale meets the scores, a
+// value scale joins the exponent of p.
 #include "ss_paged.h"
 
 #include <algorithm>
@@ -574,7 +575,12 @@ __device__ __forceinline__ void finish(const PagedAttendArgs& a, int h, int at, 
 #pragma unroll
   for (int e = 0; e < 4; ++e) y[e] = (__bf16)(o[e] * scale);
   *reinterpret_cast<bf16x4*>(const_cast<uint16_t*>(a.out.p) + h * a.out.hs + at * a.out.ts + d) = y;
-  if (d == 0 && a.lse) a.lse[(int64_t)h * a.N + at] = l > 0.0f ? (m + log2_fast(l)) * kLn2 : neg_inf();
+  if (d == 0 && a.lse) {
+    // (the exponent of l apart: where values are tiny m and log2 l are far from 0 on either side, and steps there wide)
+    float z = neg_inf();
+    if (l > 0.0f) z = (m + (float)__builtin_amdgcn_frexp_expf(l) + log2_fast(__builtin_amdgcn_frexp_mantf(l))) * kLn2;
+    a.lse[(int64_t)h * a.N + at] = z;
+  }
 }
 
 // exp2 of scores against m, as the second product's operand takes them.  v: scores in units of log 2; lvs: log 2
@@ -602,7 +608,7 @@ template <class Form, class Top, class Scale>
 __device__ __forceinline__ void running_softmax_half(float& m, float& l, Form&& form, Top&& top, Scale&& rescale) {
   float2 sum = form(m == neg_inf() ? 0.0f : m);
   if (__any(!(sum.x <= 32768.0f) || m == neg_inf())) {
-    const float mn = fmaxf(m, top() - 6.0f);
+    const float mn = fmaxf(m, top() - 9.0f);
     const float al = m == neg_inf() ? 0.0f : exp2_fast(m - mn);
     m = mn;
     l *= al;
@@ -617,7 +623,10 @@ __device__ __forceinline__ void running_softmax_half(float& m, float& l, Form&& 
 struct ValueScale {
   float log2, inverse, codes;
 };
-__device__ __forceinline__ ValueScale cut_scale(float vs) {
+// (a scale below what the library writes, 0 among them, as that)
+__device__ __forceinline__ float at_least(float scale) { return fmaxf(scale, 0x1p-109f); }
+__device__ __forceinline__ ValueScale cut_scale(float scale) {
+  const float vs = at_least(scale);
   const int e = (int)(__float_as_uint(vs) >> 23) - 127;
   const int k = e < -60 ? e + 60 : e > 60 ? e - 60 : 0;
   const float in_p = vs * __uint_as_float((uint32_t)(127 - k) << 23);
@@ -641,14 +650,14 @@ __device__ __forceinline__ u32x4 open_masked(u32x4 v, int h, int y, int cnt) {
 __device__ __forceinline__ u32x4 open_value(const uint16_t* base, int c, int h, int m, int y, int cnt) {
   return open_masked(*reinterpret_cast<const u32x4*>(base + ((c * 2 + h) * 32 + m) * 16 + 8 * y), h, y, cnt);
 }
-// The largest magnitude of eight bf16, as bits, and the power of two that lifts it to 2^7.
+// The largest magnitude of eight bf16, as bits, and the power of two that lifts it to 2^7 (2^least and less: as that).
 __device__ __forceinline__ uint32_t largest(u32x4 v) {
   uint32_t top = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) top = max(top, max(v[i] & 0x7FFFu, (v[i] >> 16) & 0x7FFFu));
   return top;
 }
-__device__ __forceinline__ int exponent_of(uint32_t top) { return (int)max(top >> 7, 1u) - 127 - 7; }
+__device__ __forceinline__ int exponent_of(uint32_t top, int least) { return max((int)(top >> 7) - 127, least) - 7; }
 // Eight bf16 times 2^-e as fp16.
 __device__ __forceinline__ u32x4 halves(u32x4 v, int e) {
   f16x8 x;
@@ -819,7 +828,7 @@ __global__ __launch_bounds__(64 * W, W == 4 ? 2 : 1) void k_paged_few(PagedAtten
         load_values(at, bytes, vq[k]);
       }
       if (id >= 0) {
-        ksv = a.c.ks[(int64_t)id * a.c.Hk + hk] * a.c1;
+        ksv = at_least(a.c.ks[(int64_t)id * a.c.Hk + hk]) * a.c1;
         vsv = cut_scale(a.c.vs[(int64_t)id * a.c.Hk + hk]);
       }
       auto one = [&](int k, u32x4 (&kr)[NL], u32x4 (&vr)[NL]) {
@@ -941,8 +950,9 @@ __device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts
 // The products are of fp16: e4m3 is exact in it, and its 11 bits of p are off by an eighth of what bf16's 8 are,
 // at the same cost.  What is bf16, queries and open rows, is brought into its range by a power of two that
 // lifts the largest of a column (a block) to 2^7: exact, but for elements 2^21 times smaller.  p's range is kept by
-// what m is: the largest score with its value scale (against that of the first block, a power of two that the output
-// takes at the end), less 6, so that p reaches up to 2^6 (2^15 before m moves) and is lost only below 2^-31 of it.
+// what m is: the largest score with its value scale, less 9, so that p reaches up to 2^9 (2^15 before m moves) and its
+// steps are at most 2^-33 of the largest (less 12, m moves too often; less 6, 9 and 10 take the same time).  Value scales count as 2^-64 .. 2^40, so that fp32 holds the sums without them beside
+// each other; the values of a block with a smaller one (values below 2^-55) count as zeros.
 // WQ = 8: the two waves of a SIMD (w and w + 4) take turns: while one forms its softmax on the
 // vector unit, the other keeps the matrix unit busy, half an iteration behind.  WQ = 4 (33 to 128
 // columns): two blocks a CU, whose phases fall beside each other by themselves.
@@ -953,8 +963,8 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
   constexpr int KB = 2 * KST * 64, TB = 2 * KB;        // 16-byte pieces of a tile's keys, of a tile
   static_assert(NCH >= 1);
   __shared__ __align__(16) u32x4 ring[NS][TB];
-  __shared__ __align__(16) float2 meta[2][64][2];   // of a tile's blocks, 64 tiles at a time: key scale (0: not seen), log 2
-                                                    // of the value scale against the unit's
+  __shared__ __align__(16) float2 meta[2][64][2];   // of a tile's blocks, 64 tiles at a time: key scale (0: not seen;
+                                                    // negative: values count as zeros), log 2 of the value scale
   __shared__ int open_power[2];       // of the open block's keys, of its values
   __shared__ int pre[kPagedUnits + 1];
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, c32 = lane & 31, wave = uniform(tid >> 6);
@@ -967,6 +977,8 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
     // tokens that every column of the unit sees: w_lo .. p_lo
     const int p_lo = uniform(un.L - un.n + un.c0 / a.G);
     const int w_lo = uniform(a.window > 0 ? un.L - un.n + (min(un.M, un.c0 + BM) - 1) / a.G - a.window + 1 : 0);
+    // the first block that one of them sees: a tile's other block may lie before it, and hold anything
+    const int b_first = uniform(a.window > 0 ? max(0, p_lo - a.window + 1) / B : 0);
     const int sl = uniform(a.c.slots[un.s]);
     const bool has_slot = (unsigned)sl < (unsigned)a.c.n_slots;
     const int32_t* table = a.c.tables + (int64_t)un.s * a.c.width;
@@ -982,7 +994,7 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
 #pragma unroll
       for (int i = 0; i < KST; ++i) top = max(top, largest(qf[i]));
       top = max(top, __float_as_uint(other_half(__uint_as_float(top))));
-      const int e = exponent_of(top);
+      const int e = exponent_of(top, -100);
 #pragma unroll
       for (int i = 0; i < KST; ++i) qf[i] = halves(qf[i], e);
       qs = ldexpf(a.c1, e);
@@ -990,7 +1002,7 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
     f32x16 O[NC];
 #pragma unroll
     for (int i = 0; i < NC; ++i) O[i] = f32x16{};
-    float m = neg_inf(), l = 0.0f, unit_e = 0.0f;
+    float m = neg_inf(), l = 0.0f;
 
     // (kept in registers: read again from the arguments in every tile they cost a trip each)
     const uint8_t* pages = (values ? a.c.v8 : a.c.k8) + hk * (B * D);
@@ -1002,17 +1014,18 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
       return values ? open_value(a.c.ov + at, ch, half, c32, x, open_rows)
                     : open_key(a.c.ok + at, 2 * ch + half, c32, x, open_rows);
     };
-    // against the unit's value scale, as far as fp32 goes (blocks 2^112 apart)
-    auto against = [&](float e) { return fminf(fmaxf(e - unit_e, -112.0f), 112.0f); };
+    auto held = [&](float log2) { return fminf(fmaxf(log2, -64.0f), 40.0f); };
     // pages and scales of tiles t .. t + 63; they may be used behind the next barrier
     auto look_up = [&](int t) {
       const int b = b_at + 2 * (t + lane) + su;
-      ids = t + lane < cnt && b < full ? table[b] : -1;
+      ids = t + lane < cnt && b >= b_first && b < full ? table[b] : -1;
       if ((unsigned)ids >= (unsigned)a.c.n_pages) ids = -1;
       if (values || sub != 0) return;
       float2 x = {0.0f, 0.0f};                               // (an open block's: put_open)
-      if (ids >= 0)
-        x = make_float2(a.c.ks[(int64_t)ids * a.c.Hk + hk], against(log2_fast(a.c.vs[(int64_t)ids * a.c.Hk + hk])));
+      if (ids >= 0) {
+        const float ks = at_least(a.c.ks[(int64_t)ids * a.c.Hk + hk]), vs = at_least(a.c.vs[(int64_t)ids * a.c.Hk + hk]);
+        x = make_float2(vs < 0x1p-64f ? -ks : ks, held(log2_fast(vs)));
+      }
       meta[(t >> 6) & 1][lane][su] = x;
     };
     // this wave's pieces of tile t, to registers; of no page, or behind the last tile, none are read
@@ -1037,7 +1050,7 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
       for (int i = 0; i < 2 * NCH; ++i) to[64 * i] = halves(open_piece(sub * NCH + (i >> 1), i & 1), e);
       if (sub == 0 && lane == 0) {
         float2& x = meta[(t >> 6) & 1][t & 63][su];
-        if (values) x.y = against((float)e);
+        if (values) x.y = held((float)e);
         else x.x = ldexpf(1.0f, e);
       }
     };
@@ -1110,7 +1123,7 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const float2 x = u ? make_float2(mt.z, mt.w) : make_float2(mt.x, mt.y);
-        cs[u] = x.x * qs;
+        cs[u] = fmaxf(fabsf(x.x) * qs, 0x1p-126f);          // (above 0: -inf times it stays -inf)
         lv[u] = x.y;
         rs[u] = exp2_fast(-x.y);
 #pragma unroll
@@ -1118,7 +1131,6 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
         const int b = b_at + 2 * t + u;
         if (b * B + B - 1 > p_lo || b * B < w_lo) hide(v + u * 16, b, half, last, lowest);
         if (__any(x.x == 0.0f)) {
-          cs[u] = 1.0f;
 #pragma unroll
           for (int i = 0; i < 16; ++i) v[u * 16 + i] = neg_inf();
         }
@@ -1162,6 +1174,8 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
 #pragma unroll
             for (int i = 0; i < NC; ++i) O[i] *= al;
           });
+      if (__any(mt.x < 0.0f)) pb[0] = pb[1] = u32x4{0, 0, 0, 0};
+      if (__any(mt.z < 0.0f)) pb[2] = pb[3] = u32x4{0, 0, 0, 0};
       if constexpr (TURNS) {       // formed here, not behind the barrier
 #pragma unroll
         for (int w = 0; w < 4; ++w) asm volatile("" : "+v"(pb[w]));
@@ -1180,15 +1194,7 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
       for (int i = 0; i < 2 * NC; ++i) top = max(top, largest(x[i]));
 #pragma unroll
       for (int i = 32; i > 0; i >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, i));
-      if (lane == 0) open_power[wave] = exponent_of(top);
-    }
-    meet();
-    // the unit's value scale: that of its first block, as a power of two
-    unit_e = floorf(meta[0][0][0].y);
-    meet();
-    if (tid < 128) {
-      float& y = meta[0][tid >> 1][tid & 1].y;
-      if (meta[0][tid >> 1][tid & 1].x != 0.0f) y = against(y);
+      if (lane == 0) open_power[wave] = exponent_of(top, values ? -57 : -100);
     }
     meet();
     constexpr int AHEAD = TURNS ? 2 : 1;      // a tile is staged so many iterations before its softmax, fetched one more
@@ -1244,9 +1250,6 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
     }
     l += other_half(l);
     if (c >= un.M) return;
-    const float unit_scale = exp2_fast(unit_e);
-#pragma unroll
-    for (int i = 0; i < NC; ++i) O[i] *= unit_scale;
 #pragma unroll
     for (int i = 0; i < NC; ++i)
 #pragma unroll

@@ -59,10 +59,23 @@ class Stream:
             out.append(y)
         return out
 
+    def value_steps(self):
+        """What a value is counted in, [H][n]: the scale of a full block, the power of two that lifts the largest of
+        an open one to 2^7."""
+        out, n = [], self.v.shape[1]
+        for b in range(0, n, BLOCK):
+            x = self.v[:, b:b + BLOCK]
+            if x.shape[1] == BLOCK:
+                s = quantised(x)[1].double()
+            else:
+                s = 2.0 ** (torch.floor(torch.log2(x.abs().amax((1, 2)).clamp_min(2.0 ** -57))) - 7)
+            out.append(s.clamp_min(2.0 ** -64)[:, None].expand(-1, x.shape[1]))
+        return torch.cat(out, 1) if out else torch.zeros(self.v.shape[0], 0, dtype=torch.float64)
 
-def attend(q, k, v, length, window=0, seen=None, prior=None):
+
+def attend(q, k, v, length, window=0, seen=None, prior=None, steps=None):
     """q [Hq][n][d] float64, the last n of `length` tokens; k, v [Hk][length][d].  seen: truth of each
-    token.  Returns out, lse, and for bounds sum p |v| and the largest sum |q_i k_i| / sqrt(d)."""
+    token; steps: Stream.value_steps().  Returns out, lse, and for bounds sum p |v| and the largest sum |q_i k_i| / sqrt(d)."""
     Hq, n, d = q.shape
     G = Hq // k.shape[0]
     kk, vv = k.repeat_interleave(G, 0), v.repeat_interleave(G, 0)
@@ -79,6 +92,11 @@ def attend(q, k, v, length, window=0, seen=None, prior=None):
     lse = torch.logsumexp(z, -1) if length else torch.full((Hq, n), -math.inf, dtype=torch.float64)
     p = torch.exp(z - torch.where(torch.isinf(lse), 0.0, lse)[..., None])
     out, size = p @ vv, p @ vv.abs()
+    if steps is not None and length:
+        # p times its step is kept in 11 bits or steps of 2^-33 of the largest such product: off by 2^-34 of it
+        # for each seen value, in its step.  bounds() multiplies by 2^-8
+        w = steps.repeat_interleave(G, 0)
+        size = size + 2.0 ** -26 * (p * w[:, None]).amax(-1, keepdim=True) * ((p > 0).double() @ (vv.abs() / w[..., None]))
     top = mass.amax(-1) if length else torch.zeros(Hq, n, dtype=torch.float64)
     if prior is not None:
         po, pl = prior

@@ -177,7 +177,7 @@ def check_attend(rig, counts, window=0, prior=None, seen=None, q=None, uniform=F
             continue
         p64 = None if prior is None else (prior[0][:, sl].double(), prior[1][:, sl].double())
         want, wlse, size, top = R.attend(q[:, sl].double(), k, v, k.shape[1], window,
-                                         None if seen is None else seen[s], p64)
+                                         None if seen is None else seen[s], p64, rig.ref[s].value_steps())
         tol, ltol = R.bounds(want, wlse, size, top, rig.d)
         got, glse = out[:, sl].cpu().double(), lse[:, sl].cpu().double()
         assert torch.isfinite(got).all(), s

@@ -1,0 +1,411 @@
+"""The paged cache in use: captured and replayed, on other streams, joined with attention over
+an index, far places, many streams, and contents that could spoil what lies beside them."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paged_ref as R
+from test_gpu_paged_cache import DEV, Rig, check_attend, check_turn, normal
+
+pytestmark = pytest.mark.gpu
+
+
+# --------------------------------------------------------------------------
+# graphs and streams
+# --------------------------------------------------------------------------
+
+@pytest.mark.parametrize("heads,width,start", [((28, 4, 128), 6, [0, 30, 61, 95]), ((4, 2, 64), 90, [2501, 31, 0, 64])])
+def test_a_captured_loop_follows_its_tensors(heads, width, start):
+    """Steps of a decode, two layers each: replays and eager calls in turn give what eager calls alone do."""
+    import paper_2609_02780_amd as P
+    Hq, Hk, d = heads
+    S, rot = len(start), P.Rotary(d)
+
+    class Side:
+        def __init__(self):
+            self.rig = Rig(heads, S, width)
+            self.q, self.k, self.v = (torch.zeros(h, S, d, dtype=torch.bfloat16, device=DEV) for h in (Hq, Hk, Hk))
+            self.out = torch.zeros(2, Hq, S, d, dtype=torch.bfloat16, device=DEV)
+            if any(start):
+                n = sum(start)
+                self.rig.lengths += torch.tensor(start, dtype=torch.int32, device=DEV)
+                for layer in range(2):
+                    self.rig.batch.append(layer, normal(layer, Hk, n, d).to(DEV), normal(9 + layer, Hk, n, d).to(DEV),
+                                          n_new=start, rotary=rot)
+
+        def step(self):
+            b = self.rig.batch
+            b.lengths += 1
+            for layer in range(2):
+                q = b.append(layer, self.k, self.v, rotary=rot, queries=self.q)
+                self.out[layer].copy_(b.attend(layer, q)[0])
+
+    eager, mixed = Side(), Side()
+    with torch.cuda.stream(torch.cuda.Stream()):       # a first run outside the capture
+        mixed.step()
+    torch.cuda.synchronize()
+    mixed.rig.lengths -= 1
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        mixed.step()
+    for t in range(36):
+        for x in (eager, mixed):
+            for y, h, s in ((x.q, Hq, 1), (x.k, Hk, 2), (x.v, Hk, 3)):
+                y.copy_(normal(100 * t + s, h, S, d))
+        eager.step()
+        mixed.step() if t % 5 == 3 else graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(eager.out, mixed.out), t
+        assert torch.equal(eager.rig.lengths, mixed.rig.lengths)
+    assert torch.equal(eager.rig.cache.arena, mixed.rig.cache.arena)
+
+
+@pytest.mark.parametrize("counts", [[1, 1, 1], [2, 1, 0], [200, 3, 40]], ids=str)
+def test_calls_and_graphs_at_once(counts):
+    """Calls whose parts are joined from workspaces, on two streams and in two graphs together."""
+    rig = Rig((16, 2, 128), 3, 90, seed=21)
+    rig.add([2700, 40, 1500])
+    qs = [normal(s, 16, sum(counts), 128, scale=1.5).to(DEV) for s in (1, 2)]
+    want = [rig.batch.attend(1, q, n_q=counts) for q in qs]
+    sides = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for rep in range(3):
+        got = []
+        for _ in range(4):
+            for q, side in zip(qs, sides):
+                got.append(rig.batch.attend(1, q, n_q=counts, stream=side))
+        torch.cuda.synchronize()
+        for i, (o, l) in enumerate(got):
+            assert torch.equal(o, want[i % 2][0]) and torch.equal(l, want[i % 2][1]), (rep, i)
+    graphs, got = [], []
+    for q in qs:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            for _ in range(3):
+                r = rig.batch.attend(1, q, n_q=counts)
+        graphs.append(g)
+        got.append(r)
+    for rep in range(4):
+        for o, l in got:
+            o.fill_(3.0)
+            l.fill_(3.0)
+        torch.cuda.synchronize()
+        for side, g in zip(sides, graphs):
+            with torch.cuda.stream(side):
+                g.replay()
+        torch.cuda.synchronize()
+        for (o, l), (wo, wl) in zip(got, want):
+            assert torch.equal(o, wo) and torch.equal(l, wl), rep
+
+
+def test_a_callers_stream(monkeypatch):
+    """What a call on a given stream fills is that stream's memory, and all it uses is recorded."""
+    import paper_2609_02780_amd as P
+    rig = Rig((8, 2, 64), 2, 90)
+    rig.add([2600, 40])
+    rot = P.Rotary(64)
+    k, v, q = (normal(s, h, 2, 64).to(DEV) for s, h in ((1, 2), (2, 2), (3, 8)))
+    pos = torch.tensor([2601, 41], device=DEV)
+    prior = rig.batch.attend(1, q)
+    rig.lengths += 1
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    here = torch.cuda.current_stream()
+    empty, like, record = torch.empty, torch.empty_like, torch.Tensor.record_stream
+    made, used, read = [], set(), set()
+
+    def note(f):
+        def g(*a, **kw):
+            made.append(torch.cuda.current_stream() == side)
+            return f(*a, **kw)
+        return g
+
+    def note_read(t, stream):
+        (read if stream == here else used).add(t.data_ptr())
+        return record(t, stream)
+
+    monkeypatch.setattr(torch, "empty", note(empty))
+    monkeypatch.setattr(torch, "empty_like", note(like))
+    monkeypatch.setattr(torch.Tensor, "record_stream", note_read)
+    b = {rig.cache.arena, rig.tables, rig.lengths, rig.slots}
+    cases = {
+        "rotate": (lambda: [rot(q, pos, stream=side)], {q, pos, rot.freqs}),
+        "append": (lambda: [rig.batch.append(1, k, v, rotary=rot, positions=pos, queries=q, stream=side)],
+                   b | {k, v, q, pos, rot.freqs}),
+        "attend": (lambda: list(rig.batch.attend(1, q, prior=prior, stream=side)), b | {q, *prior}),
+    }
+    for name, (call, inputs) in cases.items():
+        made.clear(), used.clear(), read.clear()
+        out = call()
+        assert made and all(made), name
+        assert {t.data_ptr() for t in inputs} <= used, name
+        assert {t.data_ptr() for t in out} <= read, name
+    torch.cuda.synchronize()
+
+
+def test_refused_through_the_binding(monkeypatch):
+    import paper_2609_02780_amd as P
+    rig = Rig((8, 2, 64), 2, 4)
+    rot, b = P.Rotary(64), rig.batch
+    k, q = normal(1, 2, 2, 64).to(DEV), normal(2, 8, 2, 64).to(DEV)
+    pos = torch.zeros(2, dtype=torch.int64, device=DEV)
+    before = rig.cache.arena.clone()
+
+    class Elsewhere(torch.Tensor):
+        device = torch.device("cuda", 1)
+
+    for call in (lambda: rot(q.as_subclass(Elsewhere), pos), lambda: rot(q, pos.as_subclass(Elsewhere)),
+                 lambda: b.append(0, k.as_subclass(Elsewhere), k), lambda: b.append(0, k, k.as_subclass(Elsewhere)),
+                 lambda: b.attend(0, q.as_subclass(Elsewhere)),
+                 lambda: P.PagedBatch(rig.cache, rig.tables.as_subclass(Elsewhere), rig.lengths, rig.slots)):
+        with pytest.raises(ValueError, match="lives on cuda:1"):
+            call()
+    for call, what in ((lambda: b.append(0, k, k, queries_out=q), "queries_out without queries"),
+                       (lambda: b.append(0, k, k, n_new=[2]), "each of 2 streams"),
+                       (lambda: b.append(0, k, k[:, :1]), "shape"), (lambda: b.append(0, k.float(), k), "bfloat16"),
+                       (lambda: b.append(0, k[0], k), "keys must be"), (lambda: b.attend(0, k), "shape"),
+                       (lambda: b.attend(0, q[0]), "queries must be"), (lambda: rot(q[0], pos), "x must be"),
+                       (lambda: rot(q, pos.int()), "positions must be"),
+                       (lambda: b.attend(0, q, prior=(q, pos)), "prior lse"),
+                       (lambda: P.PagedBatch(rig.cache, rig.tables[0], rig.lengths, rig.slots), "tables must be"),
+                       (lambda: P.PagedBatch(rig.cache, rig.tables, rig.lengths[:1], rig.slots), "lengths must be"),
+                       (lambda: P.PagedBatch(rig.cache, rig.tables[:, ::2], rig.lengths, rig.slots), "contiguous")):
+        with pytest.raises(ValueError, match=what):
+            call()
+    for call, what in ((lambda: b.append(2, k, k), "layer"), (lambda: b.append(0, k, k, n_new=[2, 1]), "n_new"),
+                       (lambda: b.attend(0, q, window=-1), "window"), (lambda: b.attend(0, q[:, :1]), "same number"),
+                       (lambda: P.Rotary(128)(q, pos), "dims"), (lambda: b.append(0, k, k, rotary=P.Rotary(128)), "dims"),
+                       (lambda: rot(q, pos, out=q.transpose(1, 2)[:, :2, :8].transpose(1, 2)), "x")):
+        with pytest.raises((P.SSError, ValueError), match=what):
+            call()
+    with pytest.raises(P.SSError):
+        P.PagedCache(1, 8, 3, 64, 10, 1)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    for call in (lambda: rot(q, pos), lambda: b.append(0, k, k), lambda: b.attend(0, q)):
+        with pytest.raises(ValueError, match="not the current device"):
+            call()
+    monkeypatch.undo()
+    assert torch.equal(before, rig.cache.arena)
+    rig.cache.close()
+    for call in (lambda: b.append(0, k, k), lambda: b.attend(0, q)):
+        with pytest.raises(RuntimeError, match="closed"):
+            call()
+
+
+# --------------------------------------------------------------------------
+# beside attention over an index
+# --------------------------------------------------------------------------
+
+@pytest.mark.parametrize("heads", [(28, 4, 128), (4, 2, 64)])
+def test_text_in_the_cache_and_frames_in_an_index(heads):
+    """A question and drafted tokens: rows of a video in an index with values, those of the text in pages; both
+    attentions joined are attention over all rows."""
+    import paper_2609_02780_amd as P
+    Hq, Hk, d = heads
+    frames, per = 30, 17
+    ix = P.ShallowIndex(1, *heads, frames, frames * per)
+    ix.attach_values()
+    ik, iv = normal(1, Hk, frames * per, d), normal(2, Hk, frames * per, d)
+    ix.append_kv([ik.to(DEV)], [iv.to(DEV)], frames, per)
+    rig, rot = Rig(heads, 1, 8, layers=1, layer=0), P.Rotary(d)
+    f, gain = R.frequencies(d)
+    hist = P.HistoryAttention([ix])
+    k64 = torch.zeros(Hk, 0, d, dtype=torch.float64)
+    at = 0
+    for n in (45, 1, 7, 1):
+        q = normal(10 + at, Hq, n, d, scale=1.5)
+        k, v = rig.rows(n)
+        rig.lengths += n
+        turned = rig.batch.append(0, k.to(DEV), v.to(DEV), rotary=rot, queries=q.to(DEV))
+        check_turn(turned, q.double(), R.rotate(q.double(), range(at, at + n), f))
+        alone = rot(q.to(DEV), torch.arange(at, at + n, device=DEV))
+        assert torch.equal(alone, turned)               # one rotation, two entry points
+        out, lse = hist(0, [turned.contiguous()])
+        got, z = rig.batch.attend(0, turned, prior=(out[0], lse[0]))
+        # the cache's rows as it stands for them: keys after the device's own rotation
+        rig.ref[0].add(rot(k.to(DEV), torch.arange(at, at + n, device=DEV)).double().cpu(), v.double())
+        at += n
+        ck, cv = rig.ref[0].held()
+        t64 = turned.cpu().double()
+        po, pl, psize, ptop = R.attend(t64, torch.cat([ik.double(), torch.zeros(Hk, n, d, dtype=torch.float64)], 1),
+                                       torch.cat([iv.double(), torch.zeros(Hk, n, d, dtype=torch.float64)], 1),
+                                       frames * per + n, seen=torch.arange(frames * per + n) < frames * per)
+        want, wl, size, top = R.attend(t64, ck, cv, at, prior=(po, pl))
+        m = torch.exp(pl - wl)[..., None]
+        size = size + m * psize                          # the prior's own error, a bf16 rounding of it among them
+        tol, ltol = R.bounds(want, wl, size, torch.maximum(top, ptop), d)
+        assert ((got.cpu().double() - want).abs() <= 2 * tol).all()
+        assert ((z.cpu().double() - wl).abs() <= 2 * ltol).all()
+
+
+# --------------------------------------------------------------------------
+# places and sizes
+# --------------------------------------------------------------------------
+
+def test_places_beyond_32_bits():
+    """Pages and slots that lie more than 4 GiB into their parts of the arena."""
+    import paper_2609_02780_amd as P
+    heads, n_pages, n_slots, width = (16, 8, 128), 140_000, 66_000, 40
+    rig = Rig(heads, 2, width, layers=1, layer=0)
+    rig.cache = c = P.PagedCache(1, *heads, n_pages, n_slots)
+    assert 8 * 32 * 128 * (n_pages - 100) > 2 ** 32 and 2 * 8 * 32 * 128 * (n_slots - 10) > 2 ** 32
+    rig.pages = (n_pages - 1 - np.random.default_rng(3).permutation(100)[:2 * width].reshape(2, width)).astype(np.int32)
+    rig.slot = np.array([n_slots - 1, n_slots - 7], dtype=np.int32)
+    for t in (c.key_scales[0], c.value_scales[0]):
+        t.fill_(math.nan)
+    rig.tables.copy_(torch.from_numpy(rig.pages))
+    rig.slots.copy_(torch.from_numpy(rig.slot))
+    rig.batch = P.PagedBatch(c, rig.tables, rig.lengths, rig.slots)
+    rig.add([1201, 70])
+    rig.add([1, 60])
+    check_attend(rig, [1, 1], uniform=True)
+    check_attend(rig, [90, 3])
+    lo = slice(0, n_pages - 100)
+    assert torch.isnan(c.key_scales[0][lo]).all() and torch.isnan(c.value_scales[0][lo]).all()
+    back = c.keys[0][torch.from_numpy(rig.pages[0, :2].astype(np.int64)).to(DEV)].cpu().float().reshape(2, 8, 32, 128)
+    scale = c.key_scales[0][torch.from_numpy(rig.pages[0, :2].astype(np.int64)).to(DEV)].cpu()
+    want = rig.ref[0].held()[0][:, :64].reshape(8, 2, 32, 128).transpose(0, 1)
+    assert torch.equal(back * scale[..., None, None], want.float())
+
+
+@pytest.mark.parametrize("per", [128, None])
+def test_as_many_streams_and_tokens_as_a_call_takes(per):
+    """512 streams, 65,536 tokens, more units of work than are planned: a block of threads each."""
+    heads = (3, 1, 64)
+    rig = Rig(heads, 512, 6, layers=1, layer=0)
+    rng = np.random.default_rng(5)
+    counts = [per] * 512 if per else np.diff(np.concatenate([[0], np.sort(rng.integers(0, 65537, 511)), [65536]])).tolist()
+    counts = [min(c, 6 * 32 + 31) for c in counts]
+    rig.add(counts)
+    check_attend(rig, counts, uniform=per is not None)
+    check_attend(rig, [1] * 512, uniform=True)
+    check_attend(rig, counts, window=40)
+    some = [s for s in range(512) if s % 37 == 0]
+    got = rig.stored()
+    for s in some:
+        for x, y in zip(got[s], rig.ref[s].held()):
+            assert torch.equal(x.float(), y.float()), s
+
+
+def test_streams_may_share_full_pages():
+    """A common beginning in one set of pages, read by streams that go on in their own."""
+    rig = Rig((4, 2, 64), 3, 6, seed=31)
+    k, v = rig.rows(64)
+    rig.tables[1:, :2] = rig.tables[:1, :2]
+    rig.pages[1:, :2] = rig.pages[:1, :2]
+    rig.lengths.copy_(torch.tensor([64, 0, 0], dtype=torch.int32))
+    rig.batch.append(1, k.to(DEV), v.to(DEV), n_new=[64, 0, 0])
+    rig.lengths.fill_(64)
+    for r in rig.ref:
+        r.add(k.double(), v.double())
+    rig.add([3, 40, 80])
+    rig.check_stored()
+    check_attend(rig, [3, 40, 80])
+    check_attend(rig, [1, 1, 1], window=70)
+
+
+def test_queries_rotated_where_they_lie():
+    """queries_out = queries, also with pairs that lie across 16 bytes; keys read from a wider projection."""
+    import paper_2609_02780_amd as P
+    Hq, Hk, d = 28, 4, 128
+    for dims in (128, 20, 126):
+        rot = P.Rotary(dims)
+        rig, two = (Rig((Hq, Hk, d), 2, 4) for _ in range(2))
+        for counts in ([40, 1], [1, 90]):
+            n = sum(counts)
+            wide = normal(n + dims, n, Hq + 2 * Hk, d).to(DEV)
+            q, k, v = (x.transpose(0, 1) for x in wide.split([Hq, Hk, Hk], 1))
+            want = two.add(counts, rotary=rot, queries=q)
+            kept = wide.clone()
+            rig.lengths += torch.tensor(counts, dtype=torch.int32, device=DEV)
+            assert rig.batch.append(1, k, v, n_new=counts, rotary=rot, queries=q, queries_out=q) is q
+            assert torch.equal(q, want)
+            assert torch.equal(wide[:, Hq:], kept[:, Hq:])
+            for s, c in enumerate(counts):
+                a = sum(counts[:s])
+                rig.ref[s].add(*(x[:, a:a + c].cpu().double() for x in (rot(k, _places(rig, counts)), v)))
+        rig.check_stored()
+
+
+def _places(rig, counts):
+    ends = rig.lengths.cpu().tolist()
+    return torch.cat([torch.arange(e - c, e) for e, c in zip(ends, counts)]).to(DEV)
+
+
+# --------------------------------------------------------------------------
+# contents
+# --------------------------------------------------------------------------
+
+@pytest.mark.parametrize("heads", [(28, 4, 128), (4, 2, 64)])
+def test_blocks_before_the_window_may_hold_anything(heads):
+    rig = Rig(heads, 2, 80, layers=1, layer=0, seed=41)
+    rig.add([2400, 700])
+    c = rig.cache
+    for window, counts in ((65, [1, 1]), (100, [150, 40]), (1, [1, 3]), (33, [300, 5]), (1000, [2, 1])):
+        for s, L in enumerate((2400, 700)):
+            first = max(0, L - counts[s] - window + 1) // 32
+            bad = torch.from_numpy(rig.pages[s, :first].astype(np.int64)).to(DEV)
+            held = [(t, t[bad].clone()) for t in (c.keys[0].view(torch.uint8), c.values[0].view(torch.uint8),
+                                                  c.key_scales[0].view(torch.uint8), c.value_scales[0].view(torch.uint8))]
+            for t, _ in held:
+                t[bad] = 0xFF
+            rig.held = getattr(rig, "held", []) + [(t, bad, x) for t, x in held]
+        check_attend(rig, counts, window=window)
+        for t, bad, x in rig.held:
+            t[bad] = x
+        rig.held = []
+
+
+def _blocks(rig, counts, key_scale, value_scale):
+    """Rows whose blocks of 32 have their own magnitudes (0 among them), appended to a rig of one stream."""
+    n = sum(counts)
+    k, v = normal(1, rig.Hk, n, rig.d), normal(2, rig.Hk, n, rig.d)
+    for b in range((n + 31) // 32):
+        k[:, 32 * b:32 * b + 32] *= key_scale[b % len(key_scale)]
+        v[:, 32 * b:32 * b + 32] *= value_scale[b % len(value_scale)]
+    at = 0
+    for c in counts:
+        rig.lengths += c
+        rig.batch.append(rig.layer, k[:, at:at + c].contiguous().to(DEV), v[:, at:at + c].contiguous().to(DEV))
+        rig.ref[0].add(k[:, at:at + c].double(), v[:, at:at + c].double())
+        at += c
+
+
+@pytest.mark.parametrize("heads", [(28, 4, 128), (4, 2, 64)])
+@pytest.mark.parametrize("key_scale,value_scale", [
+    ((1.0,), (0.0, 2.0 ** 20, 1.0)), ((1.0,), (1.0, 0.0, 0.0)), ((1.0,), (0.0,)), ((0.0,), (1.0,)),
+    ((1.0, 0.0, 2.0 ** -90), (2.0 ** -48, 2.0 ** 30, 2.0 ** -20)), ((2.0 ** 3, 1.0), (2.0 ** 44, 2.0 ** -40, 0.0)),
+    ((2.0 ** -120,), (1.0, 2.0 ** -80, 2.0 ** -120)), ((1.0,), (2.0 ** -48,))], ids=str)
+def test_blocks_of_any_magnitude(heads, key_scale, value_scale):
+    """From zeros to 2^44; a row of queries of zeros, one far larger and one far smaller than its neighbours."""
+    rig = Rig(heads, 1, 80, layers=1, layer=0, seed=51)
+    _blocks(rig, [300, 1], key_scale, value_scale)
+    for n in (1, 40, 130):
+        q = normal(n, rig.Hq, n, rig.d, scale=1.5)
+        q[0] = 0.0
+        q[1, -1] *= 2.0 ** -100
+        q[-1, 0] *= 2.0 ** 6
+        check_attend(rig, [n], q=q)
+    _blocks(rig, [32 * 60], key_scale, value_scale)
+    check_attend(rig, [1], q=normal(3, rig.Hq, 1, rig.d))
+    check_attend(rig, [70], q=normal(4, rig.Hq, 70, rig.d))
+
+
+def test_rows_of_the_call_alone_are_written():
+    """Outputs with room around them, and what lies behind the last stream's tokens."""
+    import paper_2609_02780_amd as P
+    rig, rot = Rig((6, 2, 64), 2, 4), P.Rotary(64)
+    q = torch.full((60, 8, 64), 7.0, dtype=torch.bfloat16, device=DEV)
+    inner = q[5:50, 1:7].transpose(0, 1)
+    k, v = rig.rows(45)
+    rig.lengths.copy_(torch.tensor([40, 3], dtype=torch.int32))       # two tokens of the second stream are passed over
+    got = torch.full_like(q, 9.0)
+    out = got[5:50, 1:7].transpose(0, 1)
+    rig.batch.append(1, k.to(DEV), v.to(DEV), n_new=[40, 5], rotary=rot, queries=inner, queries_out=out)
+    assert (q == 7.0).all()
+    mask = torch.ones_like(got, dtype=torch.bool)
+    mask[5:50, 1:7] = False
+    mask[45:47, 1:7] = True
+    assert (got[mask] == 9.0).all() and not (out[:, :40] == 9.0).all(-1).any() and not (out[:, 42:] == 9.0).all(-1).any()
