@@ -25,16 +25,19 @@ def _rows(t, shape: tuple, device, what: str) -> L.Rows:
         raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {shape}")
     if t.device != device:
         raise ValueError(f"{what} lives on {t.device}, expected {device}")
-    return _strides(t, what)
-
-
-def _strides(t, what: str) -> L.Rows:
-    heads, tokens, _ = t.shape
     hs, ts, one = t.stride()
     if one != 1:
         raise ValueError(f"the elements of a row of {what} must lie side by side")
     # a dimension of one row has any stride
-    return L.Rows(t.data_ptr(), hs if heads > 1 else 0, ts if tokens > 1 else 0)
+    return L.Rows(t.data_ptr(), hs if shape[0] > 1 else 0, ts if shape[1] > 1 else 0)
+
+
+def _like(stream, x, r: L.Rows):
+    """A new tensor laid out as ``x``, whose rows are ``r``, and its rows."""
+    out = torch.empty_like(x) if stream is None else _new(stream, torch.empty_like, x)
+    if out.stride() == x.stride():
+        return out, L.Rows(out.data_ptr(), r.head_stride, r.token_stride)
+    return out, _rows(out, out.shape, out.device, "out")
 
 
 def _new(stream, f, *args, **kw):
@@ -53,7 +56,7 @@ def _launch_stream(stream, device) -> int:
 
 
 def _ints(t, shape, dtype, device, what: str) -> int:
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous {dtype} tensor {list(shape)}")
     if t.device != device:
         raise ValueError(f"{what} lives on {t.device}, expected {device}")
@@ -90,16 +93,16 @@ class Rotary:
         if not isinstance(x, torch.Tensor) or x.dim() != 3:
             raise ValueError("x must be [heads][tokens][d]")
         _on_current(self._device, "the frequencies live")
-        H, N, d = x.shape
+        shape = x.shape
+        H, N, d = shape
         dev = self._device
-        src = _rows(x, (H, N, d), dev, "x")
+        src = _rows(x, shape, dev, "x")
         at = _ints(positions, (N,), torch.int64, dev, "positions")
         fresh = out is None
         if fresh:
-            out = _new(stream, torch.empty_like, x)
-            dst = _strides(out, "out")
+            out, dst = _like(stream, x, src)
         else:
-            dst = _rows(out, (H, N, d), dev, "out")
+            dst = _rows(out, shape, dev, "out")
         L.check(self._lib.ss_rotate(self._ref, H, N, d, C.byref(src), at, transposed, C.byref(dst),
                                     _launch_stream(stream, dev)))
         if stream is not None:
@@ -213,7 +216,7 @@ class PagedBatch:
         self._ref = C.byref(self._c)
         self._counts_type = C.c_int32 * max(S, 1)
         self._least = torch.empty(256, dtype=torch.uint8, device=dev)
-        self._needs = {}
+        self._needs, self._fp32 = {}, torch.empty(1, dtype=torch.float32, device=dev)
 
     def _counts(self, n, what: str):
         if n is None:
@@ -247,12 +250,12 @@ class PagedBatch:
         out = queries_out
         if queries is not None:
             shape = (c.n_q_heads, N, d)
-            q = C.byref(_rows(queries, shape, dev, "queries"))
+            q = _rows(queries, shape, dev, "queries")
             if out is None:
-                out = _new(stream, torch.empty_like, queries)
-                qo = C.byref(_strides(out, "queries_out"))
+                out, qo = _like(stream, queries, q)
             else:
-                qo = C.byref(_rows(out, shape, dev, "queries_out"))
+                qo = _rows(out, shape, dev, "queries_out")
+            q, qo = C.byref(q), C.byref(qo)
         elif out is not None:
             raise ValueError("queries_out without queries")
         L.check(self._lib.ss_cache_append(c.handle, self._ref, layer, N, self._counts(n_new, "n_new"), C.byref(k),
@@ -278,26 +281,26 @@ class PagedBatch:
         q = _rows(queries, (Hq, N, d), dev, "queries")
         po = pl = None
         if prior is not None:
-            o, z = prior
-            po = C.byref(_rows(o, (Hq, N, d), dev, "prior out"))
-            pl = _ints(z, (Hq, N), torch.float32, dev, "prior lse")
+            po = C.byref(_rows(prior[0], (Hq, N, d), dev, "prior out"))
+            pl = _ints(prior[1], (Hq, N), torch.float32, dev, "prior lse")
         n = self._counts(n_q, "n_q")
-        # (of calls with the same number of queries for every stream the size, which is theirs alone, is asked for once)
-        need = self._needs.get((N, window)) if n is None else None
+        # (calls with the same number of queries for every stream, whose size is theirs alone, ask for it once)
+        need, like = self._needs.get((N, window), (None, None)) if n is None else (None, None)
         if need is None:
             need = lib.ss_cache_attend_workspace_bytes(c.handle, self._ref, N, n, window)
             if need == 0:
                 raise L.SSError(L.SS_ERR_INVALID_ARGUMENT, lib.ss_last_error().decode())
+            like = self._fp32.expand(Hq, N)                 # (an empty tensor like it takes less of the host than one by size)
             if n is None:
                 if len(self._needs) >= 256:
                     self._needs.clear()
-                self._needs[N, window] = need
+                self._needs[N, window] = need, like
         # a need of 256, the least, is of a call that writes no workspace: those share one
         ws = self._least if need == 256 else _new(stream, torch.empty, need, dtype=torch.uint8, device=dev)
-        out = _new(stream, torch.empty_like, queries)
-        lse = _new(stream, torch.empty, (Hq, N), dtype=torch.float32, device=dev)
+        out, o = _like(stream, queries, q)
+        lse = torch.empty_like(like) if stream is None else _new(stream, torch.empty_like, like)
         L.check(lib.ss_cache_attend(c.handle, self._ref, layer, N, n, C.byref(q), window, po, pl, ws.data_ptr(),
-                                    need, _launch_stream(stream, dev), C.byref(_strides(out, "out")), lse.data_ptr()))
+                                    need, _launch_stream(stream, dev), C.byref(o), lse.data_ptr()))
         if stream is not None:
             _used_on(stream, c.arena, self.tables, self.lengths, self.slots, queries, *(prior or ()))
             _returned_from(stream, out, lse)
