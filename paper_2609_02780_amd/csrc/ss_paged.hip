@@ -757,7 +757,7 @@ __global__ __launch_bounds__(64 * W, W == 4 ? 2 : 1) void k_paged_few(PagedAtten
           m, l,
           [&](float mu) {
             const float off = lvs - mu;
-            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            float sum[4];
 #pragma unroll
             for (int w = 0; w < NV / 8; ++w) {
               bf16x8 x, y;
@@ -765,7 +765,7 @@ __global__ __launch_bounds__(64 * W, W == 4 ? 2 : 1) void k_paged_few(PagedAtten
               for (int e = 0; e < 8; ++e) {
                 const int i = WIDE ? 4 * w + (e & 3) + 8 * (e >> 2) : e;
                 const float p = exp2_fast(fmaf(v[i], cs, off));
-                sum[e & 3] += p;
+                sum[e & 3] = w == 0 && e < 4 ? p : sum[e & 3] + p;
                 x[e] = (__bf16)p;
                 y[e] = (__bf16)(p - (float)x[e]);
               }
@@ -1149,14 +1149,14 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
               const float off = lv[u] - mu;
-              float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+              float sum[4];
 #pragma unroll
               for (int w = 0; w < 2; ++w) {
                 f16x8 x;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                   const float p = exp2_fast(fmaf(v[u * 16 + 4 * w + (e & 3) + 8 * (e >> 2)], cs[u], off));
-                  sum[e & 3] += p;
+                  sum[e & 3] = w == 0 && e < 4 ? p : sum[e & 3] + p;     // (0 + p costs a prompt 3%)
                   x[e] = (_Float16)p;
                 }
                 pb[u * 2 + w] = __builtin_bit_cast(u32x4, x);
