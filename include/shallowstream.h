@@ -631,7 +631,7 @@ ss_status ss_cache_destroy(ss_cache* cache);
  *            most 32 width + 31 count (the last 31 need no page); below 0 counts as 0;
  *   slots    int32 [n_streams]: where the stream's open block lies, different ones for the
  *            streams of an append;
- *   n_streams 1..512, width 1..2^26-1.
+ *   n_streams 1..512, width 1..2^26-2.
  * A page outside 0 .. n_pages-1 is not written, and its tokens are not seen; nor are
  * those of an open block in a slot outside 0 .. n_slots-1. */
 typedef struct {

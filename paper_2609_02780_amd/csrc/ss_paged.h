@@ -12,8 +12,8 @@ namespace ss {
 constexpr int kBlockTokens = 32;      // tokens of a page
 constexpr int kPagedStreams = 512;    // streams of a call
 constexpr int kPagedTokens = 1 << 16; // new tokens (queries) of a call
-constexpr int kPagedUnits = 1536;      // units of a KV head that are cut into shares (more are not)
-constexpr int kPagedWidth = (1 << 26) - 1;   // pages of a stream: its tokens are counted in 31 bits
+constexpr int kPagedUnits = 1536;     // units of a KV head that are cut into shares (more are not)
+constexpr int kPagedWidth = (1 << 26) - 2;   // pages of a stream: tokens, up to the end of its open block, in 31 bits
 
 // Which tokens of a call are a stream's.  Kernels of small calls take the one or the other: 2 KB more of
 // arguments cost a launch some 0.4 us.

@@ -208,7 +208,7 @@ class PagedBatch:
         if not isinstance(tables, torch.Tensor) or tables.dim() != 2:
             raise ValueError("tables must be [n_streams][width]")
         S, width = tables.shape
-        self.cache, self.tables, self.lengths, self.slots = cache, tables, lengths, slots
+        self.cache, self._tables, self._lengths, self._slots = cache, tables, lengths, slots
         self._device, self._lib, self._S = dev, L.lib(), S
         self._c = L.CacheStreams(_ints(tables, (S, width), torch.int32, dev, "tables"),
                                  _ints(lengths, (S,), torch.int32, dev, "lengths"),
@@ -217,6 +217,36 @@ class PagedBatch:
         self._counts_type = C.c_int32 * max(S, 1)
         self._least = torch.empty(256, dtype=torch.uint8, device=dev)
         self._needs, self._fp32 = {}, torch.empty(1, dtype=torch.float32, device=dev)
+
+    # (what writes in place, as `batch.lengths += 1`, assigns the tensor that is there)
+    @property
+    def tables(self) -> torch.Tensor:
+        return self._tables
+
+    @tables.setter
+    def tables(self, t) -> None:
+        self._same(t, self._tables, "tables")
+
+    @property
+    def lengths(self) -> torch.Tensor:
+        return self._lengths
+
+    @lengths.setter
+    def lengths(self, t) -> None:
+        self._same(t, self._lengths, "lengths")
+
+    @property
+    def slots(self) -> torch.Tensor:
+        return self._slots
+
+    @slots.setter
+    def slots(self, t) -> None:
+        self._same(t, self._slots, "slots")
+
+    @staticmethod
+    def _same(t, held, what: str) -> None:
+        if t is not held:
+            raise ValueError(f"{what} of a batch are written in place; make a new batch for another tensor")
 
     def _counts(self, n, what: str):
         if n is None:

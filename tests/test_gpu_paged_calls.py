@@ -182,6 +182,10 @@ def test_refused_through_the_binding(monkeypatch):
             call()
     with pytest.raises(P.SSError):
         P.PagedCache(1, 8, 3, 64, 10, 1)
+    b.lengths += 0
+    for name in ("tables", "lengths", "slots"):
+        with pytest.raises(ValueError, match="in place"):
+            setattr(b, name, getattr(b, name) + 1)
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
     for call in (lambda: rot(q, pos), lambda: b.append(0, k, k), lambda: b.attend(0, q)):
         with pytest.raises(ValueError, match="not the current device"):
@@ -409,3 +413,56 @@ def test_rows_of_the_call_alone_are_written():
     mask[5:50, 1:7] = False
     mask[45:47, 1:7] = True
     assert (got[mask] == 9.0).all() and not (out[:, :40] == 9.0).all(-1).any() and not (out[:, 42:] == 9.0).all(-1).any()
+
+
+def test_queries_without_a_rotation_are_copied():
+    rig = Rig((6, 2, 64), 2, 4)
+    rig.add([30, 5])
+    q = normal(5, 40, 6, 64).to(DEV).transpose(0, 1)
+    got = rig.add([7, 33], queries=q)
+    assert torch.equal(got, q) and got.data_ptr() != q.data_ptr()
+    rig.check_stored()
+
+
+@pytest.mark.parametrize("heads", [(28, 4, 128), (4, 2, 64)])
+def test_streams_of_padding(heads):
+    """Streams without tokens whose queries are anything: outputs of 0 and lse of -inf, and no one else's change."""
+    rig = Rig(heads, 3, 6)
+    rig.add([150, 0, 40])
+    for n in (1, 8, 40):
+        q = normal(n, heads[0], 3 * n, heads[2]).to(DEV)
+        want, wl = rig.batch.attend(1, q)
+        q[:, n:2 * n] = math.nan
+        q[0, n:2 * n] = math.inf
+        out, lse = rig.batch.attend(1, q)
+        assert (out[:, n:2 * n] == 0).all() and (lse[:, n:2 * n] == -math.inf).all()
+        assert torch.equal(out, want) and torch.equal(lse, wl)
+
+
+def test_without_lse_and_a_prior_of_other_strides():
+    """Through the C ABI without an lse, also beside a prior, laid out token by token."""
+    import ctypes as C
+
+    from paper_2609_02780_amd import _lib as L
+    rig = Rig((16, 2, 128), 2, 60)
+    rig.add([1800, 70])
+    lib = L.lib()
+    for counts in ([1, 1], [30, 40]):
+        n = sum(counts)
+        q, po = (normal(s, n, 16, 128).to(DEV).transpose(0, 1) for s in (1, 2))
+        pl = torch.randn(16, n, device=DEV) + 5
+        for prior in (None, (po, pl)):
+            want, _ = rig.batch.attend(1, q, n_q=counts, prior=prior)
+            if prior is not None:
+                same, _ = rig.batch.attend(1, q, n_q=counts, prior=(po.contiguous(), pl))
+                assert torch.equal(want, same)
+            out = torch.full((16, n, 128), 7.0, dtype=torch.bfloat16, device=DEV)
+            rows = [L.Rows(t.data_ptr(), t.stride(0), t.stride(1)) for t in (q, out, po)]
+            ns = (C.c_int32 * 2)(*counts)
+            need = lib.ss_cache_attend_workspace_bytes(rig.cache.handle, rig.batch._ref, n, ns, 0)
+            ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+            st = lib.ss_cache_attend(rig.cache.handle, rig.batch._ref, 1, n, ns, C.byref(rows[0]), 0,
+                                     C.byref(rows[2]) if prior else None, pl.data_ptr() if prior else None, ws.data_ptr(),
+                                     need, torch.cuda.current_stream().cuda_stream, C.byref(rows[1]), None)
+            assert st == 0, lib.ss_last_error()
+            assert torch.equal(out, want)

@@ -145,7 +145,7 @@ def test_append_and_attention_refused(L):
         assert call(n=ints(1, 2, 4)) == call(n=ints(-1, 3, 4)) == bad
         assert call(tokens=65539, n=ints(65539, 0, 0)) == L.SS_ERR_UNSUPPORTED
         assert call(s=streams(L, n=0)) == call(s=streams(L, n=513)) == L.SS_ERR_UNSUPPORTED
-        assert call(s=streams(L, width=0)) == call(s=streams(L, width=2 ** 26)) == L.SS_ERR_UNSUPPORTED
+        assert call(s=streams(L, width=0)) == call(s=streams(L, width=2 ** 26 - 1)) == L.SS_ERR_UNSUPPORTED
         for name in ("tables", "lengths", "slots"):
             assert call(s=streams(L, **{name: None})) == call(s=streams(L, **{name: FAKE + 2})) == bad
     assert append(k=None) == append(v=None) == append(k=rows(L, at=FAKE + 4)) == append(v=rows(L, hs=4)) == bad
@@ -158,7 +158,7 @@ def test_append_and_attention_refused(L):
     assert attend(ws=None) == attend(ws=FAKE + 64) == L.SS_ERR_WORKSPACE
     assert attend(s=streams(L, width=5000), nbytes=1024) == L.SS_ERR_WORKSPACE
     # units of work are counted in 31 bits
-    wide = dict(s=streams(L, n=512, width=2 ** 26 - 1), tokens=512, q=rows(L, 28, 512), out=rows(L, 28, 512, at=o.data))
+    wide = dict(s=streams(L, n=512, width=2 ** 26 - 2), tokens=512, q=rows(L, 28, 512), out=rows(L, 28, 512, at=o.data))
     assert attend(**wide) in (L.SS_ERR_UNSUPPORTED, L.SS_ERR_WORKSPACE)
     need = lib.ss_cache_attend_workspace_bytes
     s = streams(L)
