@@ -679,8 +679,8 @@ __device__ __forceinline__ float of_lane(float x, int lane) {
 // block take its 32-token blocks in turn, each straight from memory to registers, and join
 // at the end of a unit.  Bound by reading the pages, so p is kept in two bf16 parts (16 bits
 // of it): the second product twice costs nothing (the matrix unit is busy for 13% of the clocks).
-// A token over 705,634 (723 MB) 113 us, 6.4 TB/s; for each of 64 streams (560 MB) 95 us, 5.9 TB/s; three for each of
-// 16 streams 45.
+// A token over 705,634 (723 MB) 113 us, 6.4 TB/s; for each of 64 streams (560 MB) 94 us, 6.0 TB/s; three for each of
+// 16 streams 43.
 // C = 16: 16x16x32 products.  Lane l = 16 g + r of S^T holds tokens 16 t + 4 g + e of column r;
 // a load of 16 bytes a lane brings piece 4 j + g of token 16 t + r, or the values of dimension
 // 32 c + 16 (g / 2) + r for half g & 1, of which the lanes 32 apart swap a half.
@@ -711,6 +711,9 @@ __global__ __launch_bounds__(64 * W, W == 4 ? 2 : 1) void k_paged_few(PagedAtten
     const int n = (cnt - wave + W - 1) / W;                 // this wave's blocks: b_at + wave + W i
     // tokens that every column sees: w_lo .. p_lo
     const int p_lo = uniform(un.L - un.n), w_lo = uniform(a.window > 0 ? max(0, un.L - a.window) : 0);
+    const int open_rows = un.L - full * B;
+    const bool opens = open_rows > 0 && b_at + cnt - 1 == full && wave == ((cnt - 1) & (W - 1));   // the open block is this wave's
+    const int sl = opens ? a.c.slots[un.s] : -1;
     u32x4 qf[KST];
     {
       const uint16_t* q = a.q.p + head * a.q.hs + (int64_t)(un.start + tok) * a.q.ts;
@@ -796,6 +799,25 @@ __global__ __launch_bounds__(64 * W, W == 4 ? 2 : 1) void k_paged_few(PagedAtten
         }
     };
 
+    // The open block, its loads all at once.  It comes last, when the pages' registers are free (beside the first page's
+    // loads its own cost 64 streams 3%).
+    auto open_step = [&]() {
+      const int at_slot = uniform(sl);
+      if ((unsigned)at_slot >= (unsigned)a.c.n_slots) return;
+      const int64_t at = (((int64_t)at_slot * 2 + (full & 1)) * a.c.Hk + hk) * (B * D);
+      u32x4 kr[NK], vr[NVF];
+#pragma unroll
+      for (int i = 0; i < NK; ++i) {
+        const int t = WIDE ? 0 : i / KST, st = WIDE ? i : i % KST;
+        kr[i] = open_key(a.c.ok + at, (st >> 1) * (64 / C) + g, 16 * t + r, st & 1, open_rows);
+      }
+#pragma unroll
+      for (int i = 0; i < NVF; ++i)
+        vr[i] = WIDE ? open_value(a.c.ov + at, i >> 1, g, r, i & 1, open_rows)
+                     : open_value(a.c.ov + at, i >> 1, g & 1, 16 * (i & 1) + r, g >> 1, open_rows);
+      step([&](int i) { return kr[i]; }, [&](int i) { return vr[i]; }, []() {}, a.c1, 0.0f, 1.0f, full);
+    };
+
     for (int i0 = 0; i0 < n; i0 += 64) {
       // pages and scales of the next 64 blocks, one a lane
       int id = -1;
@@ -871,23 +893,7 @@ __global__ __launch_bounds__(64 * W, W == 4 ? 2 : 1) void k_paged_few(PagedAtten
         }
       }
     }
-    const int open_rows = un.L - full * B;
-    if (open_rows > 0 && b_at + cnt - 1 == full && wave == ((cnt - 1) & (W - 1))) {
-      const int sl = uniform(a.c.slots[un.s]);
-      if ((unsigned)sl < (unsigned)a.c.n_slots) {
-        const int64_t at = (((int64_t)sl * 2 + (full & 1)) * a.c.Hk + hk) * (B * D);
-        step(
-            [&](int i) {
-              const int t = WIDE ? 0 : i / KST, st = WIDE ? i : i % KST;
-              return open_key(a.c.ok + at, (st >> 1) * (64 / C) + g, 16 * t + r, st & 1, open_rows);
-            },
-            [&](int i) {
-              return WIDE ? open_value(a.c.ov + at, i >> 1, g, r, i & 1, open_rows)
-                          : open_value(a.c.ov + at, i >> 1, g & 1, 16 * (i & 1) + r, g >> 1, open_rows);
-            },
-            []() {}, a.c1, 0.0f, 1.0f, full);
-      }
-    }
+    open_step();
     if constexpr (!WIDE) l += __shfl_xor(l, 16);
     l += other_half(l);
 
@@ -1022,11 +1028,13 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
                     : open_key(a.c.ok + at, 2 * ch + half, c32, x, open_rows);
     };
     auto held = [&](float log2) { return fminf(fmaxf(log2, -64.0f), 40.0f); };
-    // pages and scales of tiles t .. t + 63; they may be used behind the next barrier
+    // pages and scales of tiles t .. t + 63; the scales may be used behind the next barrier
     auto look_up = [&](int t) {
       const int b = b_at + 2 * (t + lane) + su;
       ids = t + lane < cnt && b >= b_first && b < full ? table[b] : -1;
       if ((unsigned)ids >= (unsigned)a.c.n_pages) ids = -1;
+    };
+    auto look_up_scales = [&](int t) {
       if (values || sub != 0) return;
       float2 x = {0.0f, 0.0f};                               // (an open block's: put_open)
       if (ids >= 0) {
@@ -1037,7 +1045,10 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
     };
     // this wave's pieces of tile t, to registers; of no page, or behind the last tile, none are read
     auto fetch = [&](int t, u32x4 (&raw)[NCH]) {
-      if ((t & 63) == 0 && t > 0) look_up(t);
+      if ((t & 63) == 0 && t > 0) {
+        look_up(t);
+        look_up_scales(t);
+      }
       const int id = __builtin_amdgcn_readlane(ids, t & 63);
       const auto p = page_bytes(pages + (int64_t)max(0, id) * page_stride, id < 0 ? 0 : B * D);
 #pragma unroll
@@ -1190,8 +1201,16 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
       }
     };
 
-    meet();                           // the unit before is read
+    // the first tiles' loads, under way while the unit before is read to its end and the scales are looked up (ragged
+    // prompts 55.4 -> 53.5 us)
+    constexpr int AHEAD = TURNS ? 2 : 1;      // a tile is staged so many iterations before its softmax, fetched one more
+    u32x4 first_raw[AHEAD][NCH], raw[NCH];
     look_up(0);
+#pragma unroll
+    for (int t = 0; t < AHEAD; ++t) fetch(t, first_raw[t]);
+    fetch(AHEAD, raw);
+    meet();                           // the unit before is read
+    look_up_scales(0);
     if (wave < 2 && b_at + 2 * cnt > full && open_rows > 0 && has_slot) {
       u32x4 x[2 * NC];
 #pragma unroll
@@ -1204,16 +1223,8 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
       if (lane == 0) open_power[wave] = exponent_of(top, values ? -57 : -100);
     }
     meet();
-    constexpr int AHEAD = TURNS ? 2 : 1;      // a tile is staged so many iterations before its softmax, fetched one more
-    u32x4 raw[NCH];
-    {
-      u32x4 first[AHEAD][NCH];
 #pragma unroll
-      for (int t = 0; t < AHEAD; ++t) fetch(t, first[t]);
-      fetch(AHEAD, raw);
-#pragma unroll
-      for (int t = 0; t < AHEAD; ++t) stage(t, first[t]);
-    }
+    for (int t = 0; t < AHEAD; ++t) stage(t, first_raw[t]);
     meet();
     if constexpr (TURNS) {
       // Halves of an iteration: half 2t is the first group's softmax of tile t beside the second group's
