@@ -108,36 +108,52 @@ __device__ __forceinline__ int stream_length(const PagedDev& c, int s) {
 // Rotation.  cos and sin of a block's tokens are formed once for all its heads: the angle
 // in turns, position * (f / 2 pi), in 64 bits (a far position times a frequency loses what
 // matters in 32), less the nearest quarter turn, still in 64, and of the rest the Taylor series of sine and
-// cosine in 32 bits, cut behind x^9 and x^10 (x up to pi / 4: off by less than 2^-28), so that a rotated
-// row is as near as fp32 products make it.  (The hardware's sine and cosine, off by 2^-22.9, take less of a
-// time that the rows' traffic covers.)
+// cosine (x up to pi / 4).  Queries, which are rounded to bf16 and multiplied, take it in 32 bits, cut behind x^9 and
+// x^10 (off by less than 2^-28); keys that are cached, which a rounding the other way would keep so, in 64 bits up to
+// that rounding, cut behind x^13 and x^12 (2^-41).  (64 bits for all: 1,777 tokens of 16 heads 7.6 -> 9.1 us, 8,192 of
+// 28 heads 21.3 -> 21.7.  The hardware's sine and cosine, off by 2^-22.9, take less of a time that the rows' traffic covers.)
 //
 // A thread takes 16 elements of a row as two groups of 8, so that what it loads is what it
 // writes: both elements of eight pairs (i, i + dims / 2) where the groups lie on 16 bytes; else
 // 16 side by side, where pairs of neighbours are.  (Other odd sizes read the other elements one by one.)
 // ---------------------------------------------------------------------------
 constexpr int kMaxPairs = 64;
-template <int ROWS>
+template <class T> struct PairOf;
+template <> struct PairOf<float> { using type = float2; };
+template <> struct PairOf<double> { using type = double2; };
+template <int ROWS, class T>
 struct Angles {
-  float2 cs[ROWS][kMaxPairs * 32 / ROWS + 1];       // gain cos, gain sin; 64 rows of d = 64, 32 of d = 128
+  typename PairOf<T>::type cs[ROWS][kMaxPairs * 32 / ROWS + 1];      // gain cos, gain sin; 64 rows of d = 64, 32 of d = 128
 };
 
+// cos and sin of x quarters of a turn, |x| <= 1 / 2.
+__device__ __forceinline__ void cos_sin(double quarters, float& c, float& s) {
+  const float x = (float)quarters * 1.57079632679489662f, z = x * x;
+  c = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -1.0f / 3628800, 1.0f / 40320), -1.0f / 720), 1.0f / 24), -0.5f), 1.0f);
+  s = x * fmaf(z, fmaf(z, fmaf(z, fmaf(z, 1.0f / 362880, -1.0f / 5040), 1.0f / 120), -1.0f / 6), 1.0f);
+}
+__device__ __forceinline__ void cos_sin(double quarters, double& c, double& s) {
+  const double x = quarters * 1.57079632679489662, z = x * x;
+  c = fma(z, fma(z, fma(z, fma(z, fma(z, fma(z, 1.0 / 479001600, -1.0 / 3628800), 1.0 / 40320), -1.0 / 720), 1.0 / 24),
+                 -0.5), 1.0);
+  s = fma(x * z, fma(z, fma(z, fma(z, fma(z, fma(z, 1.0 / 6227020800, -1.0 / 39916800), 1.0 / 362880), -1.0 / 5040),
+                            1.0 / 120), -1.0 / 6), x);
+}
 // Rows [r0, r1) of the table; token r's position is positions[first + r] or pos0 + r.
-template <int ROWS>
-__device__ __forceinline__ void fill_angles(Angles<ROWS>& g, const Turn& t, int r0, int r1, int first, int64_t pos0) {
-  constexpr int PAIRS = kMaxPairs * 32 / ROWS;
-  const int half = t.dims >> 1, j = threadIdx.x % PAIRS;
+template <int ROWS, class T>
+__device__ __forceinline__ void fill_angles(Angles<ROWS, T>& g, const Turn& t, int r0, int r1, int first, int64_t pos0) {
+  const int half = t.dims >> 1, lg = 32 - __clz(half - 1);      // 2^lg threads a token
+  const int j = threadIdx.x & ((1 << lg) - 1);
   if (j >= half) return;
   const double f = t.freqs[j];
-  for (int r = r0 + threadIdx.x / PAIRS; r < r1; r += blockDim.x / PAIRS) {
+  for (int r = r0 + (threadIdx.x >> lg); r < r1; r += blockDim.x >> lg) {
     const int64_t pos = t.positions ? t.positions[first + r] : pos0 + r;
     const double quarters = (double)pos * f * 4.0, q = rint(quarters);
-    const float x = (float)(quarters - q) * 1.57079632679489662f, z = x * x;
-    float c = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -1.0f / 3628800.0f, 1.0f / 40320.0f), -1.0f / 720.0f), 1.0f / 24.0f), -0.5f), 1.0f);
-    float s = x * fmaf(z, fmaf(z, fmaf(z, fmaf(z, 1.0f / 362880.0f, -1.0f / 5040.0f), 1.0f / 120.0f), -1.0f / 6.0f), 1.0f);
+    T c, s;
+    cos_sin(quarters - q, c, s);
     const int k = (int)(q - 4.0 * floor(q * 0.25));               // quarter turns, 0 .. 3
     if (k & 1) {
-      const float y = c;
+      const T y = c;
       c = -s;
       s = y;
     }
@@ -145,7 +161,7 @@ __device__ __forceinline__ void fill_angles(Angles<ROWS>& g, const Turn& t, int 
       c = -c;
       s = -s;
     }
-    g.cs[r][j] = make_float2(t.gain * c, t.gain * t.sign * s);
+    g.cs[r][j] = {t.gain * c, t.gain * t.sign * s};
   }
 }
 
@@ -174,8 +190,10 @@ __device__ __forceinline__ void as_floats(const Raw& v, float (&y)[16]) {
   }
 }
 // x: the row (read again only where its pairs lie across 16 bytes).
-__device__ __forceinline__ void turn_groups(const uint16_t* x, const Raw& v, Groups g, const float2* cs, const Turn& t,
+template <class T2>
+__device__ __forceinline__ void turn_groups(const uint16_t* x, const Raw& v, Groups g, const T2* cs, const Turn& t,
                                             float (&y)[16]) {
+  using T = decltype(cs->x);
   as_floats(v, y);
   const int half = t.dims >> 1;
   if (g.e0 >= t.dims) return;
@@ -183,19 +201,19 @@ __device__ __forceinline__ void turn_groups(const uint16_t* x, const Raw& v, Gro
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       if (g.e0 + 2 * i < t.dims) {
-        const float2 w = cs[g.e0 / 2 + i];
-        const float e = y[2 * i], o = y[2 * i + 1];
-        y[2 * i] = e * w.x - o * w.y;
-        y[2 * i + 1] = o * w.x + e * w.y;
+        const T2 w = cs[g.e0 / 2 + i];
+        const T e = y[2 * i], o = y[2 * i + 1];
+        y[2 * i] = (float)(e * w.x - o * w.y);
+        y[2 * i + 1] = (float)(o * w.x + e * w.y);
       }
     }
   } else if ((half & 7) == 0) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float2 w = cs[g.e0 + i];
-      const float e = y[i], o = y[8 + i];
-      y[i] = e * w.x - o * w.y;
-      y[8 + i] = o * w.x + e * w.y;
+      const T2 w = cs[g.e0 + i];
+      const T e = y[i], o = y[8 + i];
+      y[i] = (float)(e * w.x - o * w.y);
+      y[8 + i] = (float)(o * w.x + e * w.y);
     }
   } else {
 #pragma unroll
@@ -203,8 +221,9 @@ __device__ __forceinline__ void turn_groups(const uint16_t* x, const Raw& v, Gro
       const int at = g.e0 + i;
       if (at < t.dims) {
         const bool low = at < half;
-        const float2 w = cs[low ? at : at - half];
-        y[i] = y[i] * w.x + bf16_at(x[low ? at + half : at - half]) * (low ? -w.y : w.y);
+        const T2 w = cs[low ? at : at - half];
+        const T e = y[i], o = bf16_at(x[low ? at + half : at - half]);
+        y[i] = (float)(e * w.x + o * (low ? -w.y : w.y));
       }
     }
   }
@@ -248,7 +267,7 @@ __device__ __forceinline__ bool pairs_across(const Turn& t) { return t.dims > 0 
 template <int D, int H>
 __global__ __launch_bounds__(256) void k_rotate(RotateArgs a) {
   constexpr int P = D / 16, ROWS = 256 / P;
-  __shared__ Angles<ROWS> g;
+  __shared__ Angles<ROWS, float> g;
   const int t0 = blockIdx.x * ROWS, n = min(ROWS, a.N - t0), r = threadIdx.x / P;
   fill_angles(g, a.turn, 0, n, t0, t0);
   turn_heads<H>(a.x, a.out, t0 + r, blockIdx.y * H, min(a.heads, (int)(blockIdx.y + 1) * H), threadIdx.x % P, r < n,
@@ -280,7 +299,7 @@ __device__ __forceinline__ int value_place(int r, int e) {
 template <int D, int H, class SP>
 __global__ __launch_bounds__(2 * D) void k_paged_append(PagedAppendArgs a, SP spans) {
   constexpr int P = D / 16;
-  __shared__ Angles<32> g;
+  __shared__ Angles<32, double> g;
   __shared__ __align__(16) uint16_t vt[B][D + 8];
   __shared__ float part[8];
   const int tid = threadIdx.x, p = tid % P;
@@ -310,10 +329,11 @@ __global__ __launch_bounds__(2 * D) void k_paged_append(PagedAppendArgs a, SP sp
   const bool keys = (int)blockIdx.y < a.c.Hk;
   if (!keys) {
     const int t0 = max(max(old, 0), B * b), t1 = min(L, B * (b + 1)), i = tid / P;
-    if (a.turn.dims) fill_angles(g, a.turn, t0 - B * b, t1 - B * b, start + B * b - old, (int64_t)B * b);
+    auto& gq = reinterpret_cast<Angles<32, float>&>(g);
+    if (a.turn.dims) fill_angles(gq, a.turn, t0 - B * b, t1 - B * b, start + B * b - old, (int64_t)B * b);
     const int h0 = (blockIdx.y - a.c.Hk) * H;
     turn_heads<H>(a.q, a.q_out, start + (t0 - old) + i, h0, min(a.Hq, h0 + H), p, t0 + i < t1,
-                  g.cs[(t0 - B * b + i) & 31], a.turn, pairs_across(a.turn));
+                  gq.cs[(t0 - B * b + i) & 31], a.turn, pairs_across(a.turn));
     return;
   }
   // A token's open rows lie in buffer block & 1.  Where the last block's buffer is the one that

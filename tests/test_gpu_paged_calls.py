@@ -228,8 +228,7 @@ def test_text_in_the_cache_and_frames_in_an_index(heads):
         assert torch.equal(alone, turned)               # one rotation, two entry points
         out, lse = hist(0, [turned.contiguous()])
         got, z = rig.batch.attend(0, turned, prior=(out[0], lse[0]))
-        # the cache's rows as it stands for them: keys after the device's own rotation
-        rig.ref[0].add(rot(k.to(DEV), torch.arange(at, at + n, device=DEV)).double().cpu(), v.double())
+        rig.ref[0].add(R.rotate(k.double(), range(at, at + n), f).to(torch.bfloat16).double(), v.double())
         at += n
         ck, cv = rig.ref[0].held()
         t64 = turned.cpu().double()
@@ -311,7 +310,8 @@ def test_streams_may_share_full_pages():
 
 
 def test_queries_rotated_where_they_lie():
-    """queries_out = queries, also with pairs that lie across 16 bytes; keys read from a wider projection."""
+    """queries_out = queries, also with pairs that lie across 16 bytes; keys read from a wider projection, stored as the
+    exact rotation rounded."""
     import paper_2609_02780_amd as P
     Hq, Hk, d = 28, 4, 128
     for dims in (128, 20, 126):
@@ -329,13 +329,14 @@ def test_queries_rotated_where_they_lie():
             assert torch.equal(wide[:, Hq:], kept[:, Hq:])
             for s, c in enumerate(counts):
                 a = sum(counts[:s])
-                rig.ref[s].add(*(x[:, a:a + c].cpu().double() for x in (rot(k, _places(rig, counts)), v)))
+                kr = R.rotate(k.cpu().double(), _places(rig, counts), R.frequencies(dims)[0]).to(torch.bfloat16)
+                rig.ref[s].add(*(x[:, a:a + c].cpu().double() for x in (kr, v)))
         rig.check_stored()
 
 
 def _places(rig, counts):
     ends = rig.lengths.cpu().tolist()
-    return torch.cat([torch.arange(e - c, e) for e, c in zip(ends, counts)]).to(DEV)
+    return [t for e, c in zip(ends, counts) for t in range(e - c, e)]
 
 
 # --------------------------------------------------------------------------
