@@ -110,8 +110,9 @@ __device__ __forceinline__ int stream_length(const PagedDev& c, int s) {
 // matters in 32), less the nearest quarter turn, still in 64, and of the rest the Taylor series of sine and
 // cosine (x up to pi / 4).  Queries, which are rounded to bf16 and multiplied, take it in 32 bits, cut behind x^9 and
 // x^10 (off by less than 2^-28); keys that are cached, which a rounding the other way would keep so, in 64 bits up to
-// that rounding, cut behind x^13 and x^12 (2^-41).  (64 bits for all: 1,777 tokens of 16 heads 7.6 -> 9.1 us, 8,192 of
-// 28 heads 21.3 -> 21.7.  The hardware's sine and cosine, off by 2^-22.9, take less of a time that the rows' traffic covers.)
+// that rounding, cut behind x^13 and x^12 (2^-41; an append of 8,192 tokens 31.8 -> 32.9 us).  (64 bits for all: 1,777
+// tokens of 16 heads 7.6 -> 9.1 us.  The hardware's sine and cosine, off by 2^-22.9, save nothing that the rows' traffic
+// does not cover.)
 //
 // A thread takes 16 elements of a row as two groups of 8, so that what it loads is what it
 // writes: both elements of eight pairs (i, i + dims / 2) where the groups lie on 16 bytes; else
@@ -263,7 +264,7 @@ __device__ __forceinline__ void turn_heads(const RowsView& x, const RowsView& ou
 __device__ __forceinline__ bool pairs_across(const Turn& t) { return t.dims > 0 && !t.interleaved && ((t.dims >> 1) & 7) != 0; }
 
 // k_rotate: a block takes 32 tokens (64 at d = 64) and H heads.  Bound by reading and writing the
-// rows: 8,192 tokens of 28 heads of 128 (118 MB), 24 us, 5.0 TB/s, the rate of a large copy.
+// rows: 8,192 tokens of 28 heads of 128 (118 MB), 21 us, 5.6 TB/s, a little above the rate of a large copy.
 template <int D, int H>
 __global__ __launch_bounds__(256) void k_rotate(RotateArgs a) {
   constexpr int P = D / 16, ROWS = 256 / P;
@@ -278,8 +279,8 @@ __global__ __launch_bounds__(256) void k_rotate(RotateArgs a) {
 // k_paged_append: a block takes the tokens of one cache block of a stream and one KV
 // head (its keys and values) or some query heads.  Rows of a full block are rounded to
 // e4m3 with one scale; rows of the stream's open blocks stay bf16.  Bound by reading and writing
-// rows: 8,192 tokens of 4 KV heads with the rotation of 28 query heads (143 MB), 31.5 us, 4.5 TB/s; a token of
-// each of 64 streams 5.9 us, of one 3.2.
+// rows: 8,192 tokens of 4 KV heads with the rotation of 28 query heads (143 MB), 32.9 us, 4.3 TB/s; a token of
+// each of 64 streams 6.2 us, of one 3.3.
 // ---------------------------------------------------------------------------
 constexpr float kLeastMax = 0x1p-100f;    // 448 / it stays finite
 
@@ -1460,7 +1461,7 @@ hipError_t append_impl(const PagedAppendArgs& a, const SP& spans, int h, hipStre
 }  // namespace
 
 // Heads that a block rotates: four share its angles and have their loads under way together, where such
-// blocks fill the card; else one (1,777 tokens of 16 heads: 7.6 us with four, 6.7).
+// blocks fill the card; else one (1,777 tokens of 16 heads: 7.0 us with four, 6.4; 8,192 of 28: 21, 26.8).
 static int heads_a_block(int64_t token_blocks, int heads) { return token_blocks * ((heads + 3) / 4) >= 256 ? 4 : 1; }
 
 hipError_t launch_rotate(const RotateArgs& a, int D, hipStream_t st) {
