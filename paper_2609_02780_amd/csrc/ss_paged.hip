@@ -988,8 +988,8 @@ __device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts
 // WQ = 8: the two waves of a SIMD (w and w + 4) take turns: while one forms its softmax on the
 // vector unit, the other keeps the matrix unit busy, half an iteration behind.  WQ = 4 (33 to 128
 // columns): two blocks a CU, whose phases fall beside each other by themselves.
-// Bound by the matrix unit (busy for 58% of the clocks) and the clock that the card's power leaves it: 4,096 tokens,
-// the last of 16,384, 28 heads of 128: 751 us, 1.12 PFLOP/s.  At d = 64 by the vector unit's exponentials.
+// Bound by the matrix unit (busy for 62% of the clocks) and the clock that the card's power leaves it: 4,096 tokens,
+// the last of 16,384, 28 heads of 128: 743 us, 1.13 PFLOP/s.  At d = 64 by the vector unit's exponentials.
 template <int D, int WQ>
 __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_many(PagedAttendArgs a, Spans spans) {
   constexpr bool TURNS = WQ == 8;
