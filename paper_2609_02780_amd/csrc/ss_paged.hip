@@ -1310,7 +1310,7 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
 }
 
 // k_paged_join: the parts of a unit's columns, brought to one maximum and added in a fixed order.  Eight
-// groups of d / 4 lanes share a column's parts.  Bound by its trips to memory: 512 parts of a token 6 us, 64 parts of
+// groups of d / 4 lanes share a column's parts.  Bound by its trips to memory: 129 parts of a token 6 us, 33 parts of
 // each of 448 columns 10.
 template <int D, class SP>
 __global__ __launch_bounds__(2 * D) void k_paged_join(PagedAttendArgs a, SP spans, int bm, int round) {
