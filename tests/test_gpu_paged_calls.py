@@ -467,3 +467,35 @@ def test_without_lse_and_a_prior_of_other_strides():
                                      need, torch.cuda.current_stream().cuda_stream, C.byref(rows[1]), None)
             assert st == 0, lib.ss_last_error()
             assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("d,dims", [(64, 64), (128, 64), (128, 20)])
+def test_the_transposed_rotation_is_the_gradient(interleaved, d, dims):
+    """Of loss = sum(w * rotation(x)): against the formula's gradient, through 64-bit autograd of the definition, and
+    against differences of the device's own rotation, which is linear: (loss(x + e) - loss(x)) for single elements."""
+    import paper_2609_02780_amd as P
+    rot = P.Rotary(dims, interleaved=interleaved, factor=4.0, original=256)
+    f, gain = R.frequencies(dims, factor=4.0, original=256)
+    H, n = 3, 5
+    pos = [7, 0, 300_000, 12, 99]
+    x, w = normal(1, H, n, d), normal(2, H, n, d)
+    leaf = x.double().requires_grad_()
+    half = torch.arange(dims // 2)
+    ia, ib = (2 * half, 2 * half + 1) if interleaved else (half, half + dims // 2)
+    t = torch.tensor(pos, dtype=torch.float64)[:, None] * torch.from_numpy(f)
+    c, s = torch.cos(t) * gain, torch.sin(t) * gain
+    a, b = leaf[..., ia], leaf[..., ib]
+    loss = (w.double()[..., ia] * (a * c - b * s) + w.double()[..., ib] * (b * c + a * s)).sum()
+    loss = loss + (w.double()[..., dims:] * leaf[..., dims:]).sum()
+    loss.backward()
+    p = torch.tensor(pos, device=DEV)
+    got = rot(w.to(DEV), p, transposed=True)
+    check_turn(got, w.double() * gain, leaf.grad)
+    # the unit vectors' rotations: each is rounded to bf16 once, 2^-8 of its two elements, each off by the rotation's 2^-20
+    for h, i, e in ((0, 0, 0), (2, 2, dims - 1), (1, 4, dims // 2), (1, 3, d - 1)):
+        one = torch.zeros(H, n, d, dtype=torch.bfloat16)
+        one[h, i, e] = 1.0
+        y = rot(one.to(DEV), p).cpu().double()
+        tol = (2.0 ** -8 * y.abs() * w.double().abs()).sum() + 2.0 ** -18 * gain * w.double().abs()[h, i].max() + 1e-12
+        assert abs((w.double() * y).sum() - leaf.grad[h, i, e]) <= tol, (h, i, e)
