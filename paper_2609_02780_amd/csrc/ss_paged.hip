@@ -454,18 +454,19 @@ struct Unit {
 struct Streams {
   int start[kPagedStreams + 1], length[kPagedStreams];
 };
-template <class SP>
+template <bool LENGTHS, class SP>
 __device__ __forceinline__ void load_streams(const PagedAttendArgs& a, const SP& spans, Streams& t) {
   for (int i = threadIdx.x; i <= a.S; i += blockDim.x) {
     t.start[i] = span_start(spans, i);
-    if (i < a.S) t.length[i] = stream_length(a.c, i);
+    if (LENGTHS && i < a.S) t.length[i] = stream_length(a.c, i);
   }
   __syncthreads();
 }
 __device__ __forceinline__ int unit_first(const PagedAttendArgs& a, const Streams& t, int s, int bm) {
   return a.per ? s * a.per : a.G * t.start[s] / bm + s;
 }
-__device__ __forceinline__ Unit unit_of(const PagedAttendArgs& a, const Streams& t, int u, int bm, int round) {
+// A unit's columns, which take no lengths.
+__device__ __forceinline__ Unit columns_of(const PagedAttendArgs& a, const Streams& t, int u, int bm) {
   Unit x;
   if (a.per) {
     x.s = u / a.per;
@@ -484,6 +485,10 @@ __device__ __forceinline__ Unit unit_of(const PagedAttendArgs& a, const Streams&
   x.c0 = (u - unit_first(a, t, x.s, bm)) * bm;
   x.L = 0;
   x.b_lo = x.count = 0;
+  return x;
+}
+__device__ __forceinline__ Unit unit_of(const PagedAttendArgs& a, const Streams& t, int u, int bm, int round) {
+  Unit x = columns_of(a, t, u, bm);
   if (x.c0 >= x.M) return x;
   x.L = t.length[x.s];
   const int p_lo = x.L - x.n + x.c0 / a.G;                                   // the first and the last column's tokens
@@ -534,7 +539,7 @@ __device__ __forceinline__ void for_share(const PagedAttendArgs& a, const SP& sp
   if (a.n_wg != 0 && wg < a.n_wg / 8 * 8) wg = (wg & 7) * (a.n_wg / 8) + (wg >> 3);
   int64_t one = 1, x = 0, end = 1;
   __shared__ Streams streams;
-  load_streams(a, spans, streams);
+  load_streams<true>(a, spans, streams);
   if (a.n_wg != 0) {
     plan_units<T>(a, streams, bm, round, pre);
     one = pre[a.units];
@@ -1313,7 +1318,7 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
 // groups of d / 4 lanes share a column's parts.  Bound by its trips to memory: 129 parts of a token 6 us, 33 parts of
 // each of 448 columns 10.
 template <int D, class SP>
-__global__ __launch_bounds__(2 * D) void k_paged_join(PagedAttendArgs a, SP spans, int bm, int round) {
+__global__ __launch_bounds__(2 * D) void k_paged_join(PagedAttendArgs a, SP spans, int bm) {
   constexpr int L4 = D / 4, NG = 8;
   const int hk = blockIdx.x / a.units, u = blockIdx.x % a.units, c = blockIdx.y;
   const int64_t share = a.plan[0], one = a.plan[1 + a.units];
@@ -1322,8 +1327,8 @@ __global__ __launch_bounds__(2 * D) void k_paged_join(PagedAttendArgs a, SP span
   const int g0 = (int)(x0 / share), g1 = (int)((x1 - 1) / share);
   if (g0 == g1) return;
   __shared__ Streams streams;
-  load_streams(a, spans, streams);
-  const Unit un = unit_of(a, streams, u, bm, round);
+  load_streams<false>(a, spans, streams);
+  const Unit un = columns_of(a, streams, u, bm);
   if (c >= min(bm, un.M - un.c0)) return;
   __shared__ __align__(16) f32x4 so[NG][L4];
   __shared__ float sm[NG], sl[NG];
@@ -1386,7 +1391,7 @@ __global__ __launch_bounds__(2 * D) void k_paged_join(PagedAttendArgs a, SP span
 // The same where units have many columns and few parts: a group of d / 4 lanes a column (a prompt's 4,096 tokens of 28
 // heads: 22 us).
 template <int D>
-__global__ __launch_bounds__(256) void k_paged_join_many(PagedAttendArgs a, Spans spans, int bm, int round) {
+__global__ __launch_bounds__(256) void k_paged_join_many(PagedAttendArgs a, Spans spans, int bm) {
   constexpr int L4 = D / 4, ROWS = 256 / L4;
   const int hk = blockIdx.x / a.units, u = blockIdx.x % a.units;
   const int64_t share = a.plan[0], one = a.plan[1 + a.units];
@@ -1395,8 +1400,8 @@ __global__ __launch_bounds__(256) void k_paged_join_many(PagedAttendArgs a, Span
   const int g0 = (int)(x0 / share), g1 = (int)((x1 - 1) / share);
   if (g0 == g1) return;
   __shared__ Streams streams;
-  load_streams(a, spans, streams);
-  const Unit un = unit_of(a, streams, u, bm, round);
+  load_streams<false>(a, spans, streams);
+  const Unit un = columns_of(a, streams, u, bm);
   const int c = blockIdx.y * ROWS + threadIdx.x / L4, d = threadIdx.x % L4 * 4;
   if (c >= min(bm, un.M - un.c0)) return;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
@@ -1428,7 +1433,7 @@ hipError_t few_impl(const PagedAttendArgs& a, const SP& spans, const PagedAttend
   else hipLaunchKernelGGL((k_paged_few<D, 32, 4, SP>), grid, dim3(256), 0, st, a, spans);
   if (a.n_wg)
     hipLaunchKernelGGL((k_paged_join<D, SP>), dim3((unsigned)(a.units * a.c.Hk), (unsigned)a.cols), dim3(2 * D), 0, st, a,
-                       spans, p.bm, p.round);
+                       spans, p.bm);
   return hipGetLastError();
 }
 
@@ -1441,11 +1446,11 @@ hipError_t attend_impl(const PagedAttendArgs& a, const Spans& spans, const Paged
   if (p.bm == 128) hipLaunchKernelGGL((k_paged_many<D, 4>), grid, dim3(256), 0, st, a, spans);
   else hipLaunchKernelGGL((k_paged_many<D, 8>), grid, dim3(512), 0, st, a, spans);
   if (a.n_wg > 4 * (int64_t)rows) {                 // many parts a unit
-    hipLaunchKernelGGL((k_paged_join<D, Spans>), dim3(rows, (unsigned)a.cols), dim3(2 * D), 0, st, a, spans, p.bm, p.round);
+    hipLaunchKernelGGL((k_paged_join<D, Spans>), dim3(rows, (unsigned)a.cols), dim3(2 * D), 0, st, a, spans, p.bm);
   } else if (a.n_wg) {
     const int per = 256 / (D / 4);
     hipLaunchKernelGGL((k_paged_join_many<D>), dim3(rows, (unsigned)((a.cols + per - 1) / per)), dim3(256), 0, st, a,
-                       spans, p.bm, p.round);
+                       spans, p.bm);
   }
   return hipGetLastError();
 }
