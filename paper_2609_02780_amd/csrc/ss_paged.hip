@@ -1053,7 +1053,8 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
       return values ? open_value(a.c.ov + at, ch, half, c32, x, open_rows)
                     : open_key(a.c.ok + at, 2 * ch + half, c32, x, open_rows);
     };
-    auto held = [&](float log2) { return fminf(fmaxf(log2, -64.0f), 40.0f); };
+    constexpr int kMostScale = 40;
+    auto held = [&](float log2) { return fminf(fmaxf(log2, -64.0f), (float)kMostScale); };
     // pages and scales of tiles t .. t + 63; the scales may be used behind the next barrier
     auto look_up = [&](int t) {
       const int b = b_at + 2 * (t + lane) + su;
@@ -1246,7 +1247,8 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
       for (int i = 0; i < 2 * NC; ++i) top = max(top, largest(x[i]));
 #pragma unroll
       for (int i = 32; i > 0; i >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, i));
-      if (lane == 0) open_power[wave] = exponent_of(top, values ? -57 : -100);
+      // (the values' power within what their scale is held to: 2^48 is lifted to 2^8)
+      if (lane == 0) open_power[wave] = values ? min(exponent_of(top, -57), kMostScale) : exponent_of(top, -100);
     }
     meet();
 #pragma unroll
