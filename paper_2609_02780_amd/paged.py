@@ -72,6 +72,9 @@ class Rotary:
     ``fast`` turns and more over that length stay, those with ``slow`` and fewer are divided
     and the ones between are mixed; the result is then scaled by ``1 + 0.1 ln(factor)``
     (``gain``: by that instead).
+
+    Frequencies of any other rule are written in place, ``rotary.freqs.copy_(...)``: fp64
+    ``[dims / 2]`` on the device, in turns a position.  Calls that are captured read them there too.
     """
 
     def __init__(self, dims: int, base: float = 10000.0, interleaved: bool = False, factor: float = 1.0,
@@ -79,12 +82,33 @@ class Rotary:
         freqs, g = torch.empty(max(dims, 2) // 2, dtype=torch.float64), C.c_float()
         L.check(L.lib().ss_rotary_freqs(dims, base, factor, original, fast, slow, freqs.data_ptr(), C.byref(g)))
         dev = torch.device(device) if device is not None else torch.device("cuda", torch.cuda.current_device())
-        self.dims, self.interleaved = dims, bool(interleaved)
-        self.gain = float(g.value if gain is None else gain)
-        self.freqs = freqs.to(dev)          # turns a position
-        self._device, self._lib = self.freqs.device, L.lib()
-        self._c = L.Rotary(self.freqs.data_ptr(), dims, int(self.interleaved), self.gain)
+        self._freqs = freqs.to(dev)
+        self._device, self._lib = self._freqs.device, L.lib()
+        self._c = L.Rotary(self._freqs.data_ptr(), dims, int(bool(interleaved)), float(g.value if gain is None else gain))
         self._ref = C.byref(self._c)
+
+    # What a call uses is `_c`, so nothing here is exchanged.  (What writes in place, as `rotary.freqs /= 2`, assigns
+    # the tensor that is there.)
+    @property
+    def freqs(self) -> torch.Tensor:
+        return self._freqs
+
+    @freqs.setter
+    def freqs(self, t) -> None:
+        if t is not self._freqs:
+            raise ValueError("freqs of a rotation are written in place")
+
+    @property
+    def dims(self) -> int:
+        return self._c.dims
+
+    @property
+    def interleaved(self) -> bool:
+        return bool(self._c.interleaved)
+
+    @property
+    def gain(self) -> float:
+        return self._c.gain
 
     def __call__(self, x, positions, transposed: bool = False, out=None, stream=None):
         """``x``: ``[heads][tokens][d]`` bfloat16; ``positions``: int64 ``[tokens]``.  Returns ``out``
@@ -106,7 +130,7 @@ class Rotary:
         L.check(self._lib.ss_rotate(self._ref, H, N, d, C.byref(src), at, transposed, C.byref(dst),
                                     _launch_stream(stream, dev)))
         if stream is not None:
-            _used_on(stream, x, positions, self.freqs)
+            _used_on(stream, x, positions, self._freqs)
             if fresh:
                 _returned_from(stream, out)
             else:
