@@ -232,7 +232,7 @@ class PagedBatch:
         if not isinstance(tables, torch.Tensor) or tables.dim() != 2:
             raise ValueError("tables must be [n_streams][width]")
         S, width = tables.shape
-        self.cache, self._tables, self._lengths, self._slots = cache, tables, lengths, slots
+        self._cache, self._tables, self._lengths, self._slots = cache, tables, lengths, slots
         self._device, self._lib, self._S = dev, L.lib(), S
         self._c = L.CacheStreams(_ints(tables, (S, width), torch.int32, dev, "tables"),
                                  _ints(lengths, (S,), torch.int32, dev, "lengths"),
@@ -241,6 +241,11 @@ class PagedBatch:
         self._counts_type = C.c_int32 * max(S, 1)
         self._least = torch.empty(256, dtype=torch.uint8, device=dev)
         self._needs, self._fp32 = {}, torch.empty(1, dtype=torch.float32, device=dev)
+
+    # (workspaces and outputs are formed by its heads)
+    @property
+    def cache(self) -> PagedCache:
+        return self._cache
 
     # (what writes in place, as `batch.lengths += 1`, assigns the tensor that is there)
     @property
@@ -285,7 +290,7 @@ class PagedBatch:
         same number).  Keys are rotated by ``rotary`` at ``positions`` (int64 ``[tokens]``; default: a token's
         place in its stream).  ``queries`` ``[H_q][tokens][d]`` are rotated alike and returned
         (in ``queries_out``, which may be ``queries``; by default a new tensor laid out as they are)."""
-        c, dev = self.cache, self._device
+        c, dev = self._cache, self._device
         _on_current(dev, "the cache lives")
         if not isinstance(keys, torch.Tensor) or keys.dim() != 3:
             raise ValueError("keys must be [n_kv_heads][tokens][d]")
@@ -327,7 +332,7 @@ class PagedBatch:
         so many of those tokens.  ``prior``: ``(out, lse)`` of the same queries over other rows, which
         the result is joined with (as :class:`HistoryAttention` returns them; bfloat16 ``[H_q][tokens][d]``
         and fp32 ``[H_q][tokens]``).  Returns ``(out, lse)``, ``out`` laid out as ``queries``."""
-        c, dev, lib = self.cache, self._device, self._lib
+        c, dev, lib = self._cache, self._device, self._lib
         _on_current(dev, "the cache lives")
         if not isinstance(queries, torch.Tensor) or queries.dim() != 3:
             raise ValueError("queries must be [n_q_heads][tokens][d]")

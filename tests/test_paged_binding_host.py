@@ -32,3 +32,14 @@ def test_a_rotation_is_what_its_attributes_say(P):
     rot.freqs.copy_(torch.arange(32) / 64)
     assert rot._c.freqs == at == held.data_ptr()
     assert P.Rotary(64, gain=2.5, device="cpu").gain == 2.5
+
+
+def test_a_batch_stays_with_its_cache(P):
+    """Sizes of outputs and workspaces are kept by a batch and hold for its cache's heads alone."""
+    from types import SimpleNamespace
+    ints = torch.zeros(2, dtype=torch.int32)
+    cache, other = (SimpleNamespace(arena=torch.empty(1)) for _ in range(2))
+    batch = P.PagedBatch(cache, ints.reshape(2, 1), ints, ints)
+    with pytest.raises(AttributeError):
+        batch.cache = other
+    assert batch.cache is cache
