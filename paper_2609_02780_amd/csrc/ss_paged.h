@@ -74,10 +74,11 @@ struct PagedAttendArgs {
   float c1;                           // log2(e) / sqrt(d)
   int units, per, cols;               // units of a KV head; of a stream (0: ragged); columns kept of a unit
   int n_wg, min_share;                // blocks; 0: a block a unit, nothing to join
+  int start;                          // work that beginning a unit counts as
 };
 struct PagedAttendPlan {
   int bm, round;                      // columns of a unit, blocks that its work is counted in
-  int units, per, cols, n_wg, min_share;
+  int units, per, cols, n_wg, min_share, start;
   size_t o_bytes, ml_bytes, plan_bytes;
 };
 hipError_t launch_paged_attend(const PagedAttendArgs& a, const Spans& spans, const PagedAttendPlan& p, int D,

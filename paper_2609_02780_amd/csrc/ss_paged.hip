@@ -442,9 +442,12 @@ __global__ __launch_bounds__(2 * D) void k_paged_append(PagedAppendArgs a, SP sp
 
 // ---------------------------------------------------------------------------
 // Attention.  A unit is a stream's run of BM query columns (column c: token c / G, head c % G of
-// its KV head); its work are the blocks that some column sees.  All units' work, laid end to
-// end over the KV heads, is cut into equal shares, one a thread block, so streams of any
-// lengths fill the card alike.  A block's first and last unit may be parts, joined by k_paged_join.
+// its KV head); its work are the blocks that some column sees, behind `start` places that stand for
+// what beginning and ending a unit takes (without them a thread block that got the idle streams of a padded
+// batch was the last by far).  All units' work, laid end to end over the KV heads, is cut into equal shares,
+// one a thread block, so streams of any lengths fill the card alike; where no unit can be long, or units are
+// more than kPagedUnits, each is a thread block's.  A block's first and last unit may be parts, joined by
+// k_paged_join.
 // ---------------------------------------------------------------------------
 struct Unit {
   int s, n, start, L, c0, M;         // its columns c0 .. min(c0 + BM, M) - 1
@@ -499,13 +502,16 @@ __device__ __forceinline__ Unit unit_of(const PagedAttendArgs& a, const Streams&
   return x;
 }
 
+// A unit's work; that of no unit is none.
+__device__ __forceinline__ int work_of(const PagedAttendArgs& a, const Unit& x) { return x.count > 0 ? a.start + x.count : 0; }
+
 // pre[u]: the work before unit u (pre[units]: all of it).
 template <int T>
 __device__ __forceinline__ void plan_units(const PagedAttendArgs& a, const Streams& t, int bm, int round, int* pre) {
   __shared__ int part[T / 64];
   const int tid = threadIdx.x, run = (a.units + T - 1) / T, u0 = min(a.units, tid * run), u1 = min(a.units, u0 + run);
   int sum = 0;
-  for (int u = u0; u < u1; ++u) sum += unit_of(a, t, u, bm, round).count;
+  for (int u = u0; u < u1; ++u) sum += work_of(a, unit_of(a, t, u, bm, round));
   int upto = sum;
 #pragma unroll
   for (int x = 1; x < 64; x <<= 1) {
@@ -520,7 +526,7 @@ __device__ __forceinline__ void plan_units(const PagedAttendArgs& a, const Strea
     if (w < (tid >> 6)) at += part[w];
   for (int u = u0; u < u1; ++u) {
     pre[u] = at;
-    at += unit_of(a, t, u, bm, round).count;
+    at += work_of(a, unit_of(a, t, u, bm, round));
   }
   if (tid == T - 1) pre[a.units] = at;
   __syncthreads();
@@ -553,10 +559,10 @@ __device__ __forceinline__ void for_share(const PagedAttendArgs& a, const SP& sp
   }
   for (int side = 0; x < end; side = 1) {                // (one call of work: it is inlined)
     // (a block a unit: a head's on few XCDs, the last units, which may see the most, first)
-    int hk = wg % a.c.Hk, u = a.units - 1 - wg / a.c.Hk, first = 0;
+    int hk = wg % a.c.Hk, u = a.units - 1 - wg / a.c.Hk, first = 0, y = 0;
     if (a.n_wg != 0) {
       hk = (int)(x / one);
-      const int y = (int)(x % one);
+      y = (int)(x % one);
       int lo = 0, hi = a.units - 1;                      // the last unit whose work begins at y or before
       while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
@@ -564,20 +570,24 @@ __device__ __forceinline__ void for_share(const PagedAttendArgs& a, const SP& sp
         else hi = mid - 1;
       }
       u = lo;
-      first = y - pre[u];
+      y -= pre[u];
     }
     u = uniform(u);
-    first = uniform(first);
     const Unit un = unit_of(a, streams, u, bm, round);
     int cnt = un.count, slot = -1;
-    if (a.n_wg != 0) {
-      cnt = (int)min((int64_t)(un.count - first), end - x);
+    if (a.n_wg == 0) {
+      if (cnt == 0) return;
+      x = end;
+    } else {
+      // places y .. to - 1 of the unit; a share that ends among the first `start` leaves all blocks to the next
+      const int to = (int)min((int64_t)(a.start + un.count), y + (end - x));
+      x += to - y;
+      first = max(0, y - a.start);
+      cnt = max(0, to - a.start) - first;
+      if (cnt == 0) return;
       if (cnt != un.count) slot = 2 * wg + side;
     }
-    cnt = uniform(cnt);
-    if (cnt == 0) return;
-    work(uniform(hk), un, first, cnt, uniform(slot));
-    x += cnt;
+    work(uniform(hk), un, uniform(first), uniform(cnt), uniform(slot));
   }
 }
 
@@ -1326,7 +1336,7 @@ __global__ __launch_bounds__(2 * D) void k_paged_join(PagedAttendArgs a, SP span
   const int64_t share = a.plan[0], one = a.plan[1 + a.units];
   const int64_t x0 = hk * one + a.plan[1 + u], x1 = hk * one + a.plan[2 + u];
   if (x0 == x1) return;
-  const int g0 = (int)(x0 / share), g1 = (int)((x1 - 1) / share);
+  const int g0 = (int)((x0 + a.start) / share), g1 = (int)((x1 - 1) / share);
   if (g0 == g1) return;
   __shared__ Streams streams;
   load_streams<false>(a, spans, streams);
@@ -1399,7 +1409,7 @@ __global__ __launch_bounds__(256) void k_paged_join_many(PagedAttendArgs a, Span
   const int64_t share = a.plan[0], one = a.plan[1 + a.units];
   const int64_t x0 = hk * one + a.plan[1 + u], x1 = hk * one + a.plan[2 + u];
   if (x0 == x1) return;
-  const int g0 = (int)(x0 / share), g1 = (int)((x1 - 1) / share);
+  const int g0 = (int)((x0 + a.start) / share), g1 = (int)((x1 - 1) / share);
   if (g0 == g1) return;
   __shared__ Streams streams;
   load_streams<false>(a, spans, streams);

@@ -225,16 +225,28 @@ ss_status plan_attend(const ss_cache* c, const ss_cache_streams* s, int32_t n_to
   p.units = n_q ? (int)((int64_t)G * n_tokens / bm) + S : S * p.per;
   p.cols = std::min(bm, G * most);
   const int64_t work = cdiv(seen(bm), round);
-  if ((work + 1) * p.units > 0x7FFFFFFF)
+  // What beginning and ending a unit counts as, in blocks (pairs).  128 streams, 28/4 heads of 128, the last 64 of one token
+  // and the others of 16,000: 384 us with none, 191 with 8, 179 with 12; with 10 drafts, of 6,144: 711, 168, 151; 4,096
+  // tokens from the first: 260, 150, 149.  (More makes shares of equal units end apart: 64 tokens for each of 32
+  // streams of 6,144, 16/4 heads of 64: 83, 87, 90.)  Less where 31 bits would not hold the sum.
+  const int64_t most_work = 0x7FFFFFFF / p.units;
+  if (work + 1 > most_work)
     return fail(SS_ERR_UNSUPPORTED, "%d units of up to %lld blocks are more than 2^31", p.units, (long long)work);
-  const int64_t all = work * p.units * Hk;
+  p.start = (int)std::min<int64_t>(bm <= 32 ? 12 : 8, most_work - work - 1);
+  const int64_t all = (work + p.start) * p.units * Hk;
   p.min_share = 8;
   // A block a unit leaves part of the last round of blocks idle; shares fill all rounds, but their parts are
-  // joined by another kernel, which costs about as much as so many blocks (pairs) of work.
+  // joined by another kernel, which costs about as much as so many blocks (pairs) of work.  Where streams may differ, one
+  // that fills its table can be the only long one, and its units what everyone waits for: then a block a unit only
+  // as long as no unit can be long.  (28/4 heads of 128, a block a unit and shares.  A token for each of 128 streams: one of
+  // 705,000 tokens and the others of 100 5,298 us and 129, one of 16,000 124, 22, lengths spread up to that 204, 187,
+  // up to 8,192 108, 108, all of 8,192 167, 170, all of 100 9, 14.  64 tokens for each of 32 streams: one of 6,144
+  // 140, 57, spread up to that 150, 127, all of 6,144 186, 187, all of 100 25, 30.)
   const int64_t join_work = bm <= 32 ? 64 : 32;
   const int64_t room = bm == 256 ? 256 : bm == 128 && D == 64 ? 768 : 512, blocks = (int64_t)p.units * Hk;
   const int64_t idle = (cdiv(blocks, room) * room - blocks) * work / room;
-  if (idle <= join_work || p.units > ss::kPagedUnits) {
+  const int64_t short_work = bm <= 32 ? 256 : 64;
+  if ((idle <= join_work && (S == 1 || work <= short_work)) || p.units > ss::kPagedUnits) {
     p.n_wg = 0;
     p.o_bytes = p.ml_bytes = p.plan_bytes = 0;
     return SS_OK;
@@ -432,6 +444,7 @@ ss_status ss_cache_attend(const ss_cache* cache, const ss_cache_streams* streams
     a.cols = p.cols;
     a.n_wg = p.n_wg;
     a.min_share = p.min_share;
+    a.start = p.start;
     ss::Spans spans;
     fill_spans(spans, n_tokens, a.S, n_q);
     const hipError_t e = ss::launch_paged_attend(a, spans, p, d.head_dim, static_cast<hipStream_t>(stream));

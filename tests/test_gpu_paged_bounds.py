@@ -1,5 +1,6 @@
 """Rotation and the paged cache at the ends of what their documentation allows, against the 64-bit
 forms of ``paged_ref``."""
+import numpy as np
 import pytest
 import torch
 
@@ -37,8 +38,6 @@ def test_values_up_to_the_largest(heads, top):
 
 def test_frequencies_written_in_place():
     """Of a ramp over the pairs' indices, in eager calls, appends and replays."""
-    import numpy as np
-
     import paper_2609_02780_amd as P
     d, n, gain = 64, 5, 1.25
     rot = P.Rotary(d, gain=gain)
@@ -63,3 +62,46 @@ def test_frequencies_written_in_place():
         k, v = rig.rows(n)
         rig.lengths += n
         assert torch.equal(rig.batch.append(0, k.to(DEV), v.to(DEV), rotary=rot, positions=at, queries=dev), got)
+
+
+# --------------------------------------------------------------------------
+# streams of any lengths
+# --------------------------------------------------------------------------
+
+@pytest.mark.parametrize("heads,streams,per", [((8, 8, 128), 64, 1), ((28, 4, 128), 128, 1), ((28, 4, 128), 32, 3),
+                                               ((8, 8, 128), 16, 40), ((16, 4, 64), 24, 40), ((28, 4, 128), 5, 90)])
+def test_one_long_stream_among_short_and_idle_ones(heads, streams, per):
+    """Wide tables, the idle streams side by side, as a padded batch has them, in two orders."""
+    width = 300
+    rig = Rig(heads, streams, width, layers=1, layer=0, seed=71)
+    rng = np.random.default_rng(streams + per)
+    long = {0: 33 * 32 + 5, streams // 2: width * 32 + 31}
+    rig.add([long.get(s, int(rng.integers(1, 90)) if s < streams * 2 // 3 else 0) for s in range(streams)])
+    for window in (0, 9000):
+        check_attend(rig, [per] * streams, window=window, uniform=True)
+    counts = [int(c) for c in rng.integers(0, per + 1, streams)]
+    counts[streams // 2] = per
+    check_attend(rig, counts)
+    # the same rows in another order of streams
+    order = np.roll(np.arange(streams), streams // 2 - 1)
+    rig.tables.copy_(rig.tables[torch.from_numpy(order).to(DEV)].clone())
+    rig.slots.copy_(rig.slots[torch.from_numpy(order).to(DEV)].clone())
+    rig.lengths.copy_(rig.lengths[torch.from_numpy(order).to(DEV)].clone())
+    rig.ref = [rig.ref[s] for s in order]
+    check_attend(rig, [per] * streams, uniform=True)
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_shares_of_random_lengths(seed):
+    """Lengths and counts of any kind, so that shares end anywhere in a unit and before its first block."""
+    rng = np.random.default_rng(seed)
+    heads = [(4, 2, 64), (28, 4, 128), (3, 1, 64), (16, 2, 128)][seed]
+    streams = [40, 9, 61, 23][seed]
+    rig = Rig(heads, streams, 270, layers=1, layer=0, seed=80 + seed)
+    kinds = [0, 1, 32, 33, 90, 700, 2500]
+    rig.add([int(rng.choice(kinds)) for _ in range(streams)])
+    for most in (1, 2, 6, 40):
+        counts = [int(c) for c in rng.integers(0, most + 1, streams)]
+        counts[0] = most
+        check_attend(rig, counts, window=int(rng.choice([0, 2000])))
+        check_attend(rig, [most] * streams, uniform=True)

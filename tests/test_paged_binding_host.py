@@ -43,3 +43,23 @@ def test_a_batch_stays_with_its_cache(P):
     with pytest.raises(AttributeError):
         batch.cache = other
     assert batch.cache is cache
+
+
+@pytest.mark.parametrize("heads,streams,tokens", [((28, 4, 128), 128, 1), ((28, 4, 128), 256, 1), ((28, 4, 128), 512, 1), ((8, 8, 128), 64, 1),
+                                                  ((28, 4, 128), 128, 10), ((28, 4, 128), 32, 64), ((16, 2, 128), 4, 1024)])
+def test_streams_that_may_differ_are_shared(P, heads, streams, tokens):
+    """The tables' width stands for every stream's length, but streams of any lengths may be long alone: then no
+    unit is one thread block's, however well as many equal ones would fill the card.  Shares take a workspace."""
+    import ctypes as C
+
+    from paper_2609_02780_amd import _lib as L
+    fake, h = 0x7F0000000000, C.c_void_p()
+    d = L.CacheDesc(1, *heads, 10, 600)
+    assert L.lib().ss_cache_create(C.byref(d), fake, 1 << 60, C.byref(h)) == 0
+    need = lambda width, window=0: L.lib().ss_cache_attend_workspace_bytes(        # noqa: E731
+        h, C.byref(L.CacheStreams(fake, fake, fake, streams, width)), streams * tokens, None, window)
+    for width in (300, 500, 2000, 20000):
+        assert need(width) > 256, width
+    # short ones are not worth joining
+    assert need(20) == need(20000, 100) == 256
+    assert L.lib().ss_cache_destroy(h) == 0
