@@ -105,3 +105,49 @@ def test_shares_of_random_lengths(seed):
         counts[0] = most
         check_attend(rig, counts, window=int(rng.choice([0, 2000])))
         check_attend(rig, [most] * streams, uniform=True)
+
+
+# --------------------------------------------------------------------------
+# what p keeps
+# --------------------------------------------------------------------------
+
+def _pair_bounds(want, size, top, length, d):
+    """How far sums of few terms may be off where each p is kept in at least 11 bits: half a step, 2^-11, of each
+    |p v|, the scores' error as in paged_ref.bounds, at most a step of 2^-24 for each token that is added, and the
+    output's own rounding to bf16, 2^-8."""
+    score = (d + 16) * 2.0 ** -24 * top + 2.0 ** -18
+    return size * (2.0 ** -11 + 2 * score[..., None] + length * 2.0 ** -24) + 2.0 ** -8 * want.abs() + 1e-37
+
+
+@pytest.mark.parametrize("heads", [(28, 4, 128), (16, 4, 64), (3, 1, 64), (8, 8, 128)])
+@pytest.mark.parametrize("length", [7, 70, 2490])
+def test_p_keeps_eleven_bits(heads, length):
+    """Values of 0 but for two tokens of nearly the same weight and opposite values: what is left is small beside either,
+    and shows how p was rounded; a wrong or missing row shows as such."""
+    Hq, Hk, d = heads
+    rig = Rig(heads, 1, 80, layers=1, layer=0, seed=91)
+    k, v = normal(length, Hk, length, d), torch.zeros(Hk, length, d, dtype=torch.bfloat16)
+    a, b = length // 3, length - 2
+    k[:, b] = k[:, a]
+    k[:, b, ::16] += 0.0625
+    v[:, a], v[:, b] = 448.0, -448.0
+    rig.lengths += length
+    rig.batch.append(0, k.to(DEV), v.to(DEV))
+    rig.ref[0].add(k.double(), v.double())
+    hk, hv = rig.ref[0].held()
+    coarse = 0
+    for n in (1, 4, 8, 36, 70):
+        q = normal(n, Hq, n, d)
+        out, _ = rig.batch.attend(0, q.to(DEV))
+        want, lse, size, top = R.attend(q.double(), hk, hv, length)
+        # (a query before the second token sees the first alone, one before both sees neither)
+        tol = _pair_bounds(want, size, top, length, d)
+        off = (out.cpu().double() - want).abs()
+        assert (off <= tol).all(), (n, float((off / tol).max()))
+        # p of 8 bits would not do: half a step, 2^-9, of each weight
+        z = q.double() @ hk.repeat_interleave(Hq // Hk, 0).transpose(1, 2) / d ** 0.5
+        z = z.masked_fill(torch.arange(length) > torch.arange(length - n, length)[:, None], -torch.inf)
+        p = torch.exp(z - z.amax(-1, keepdim=True))
+        worse = (p.to(torch.bfloat16).double() @ hv.repeat_interleave(Hq // Hk, 0)) / p.sum(-1, keepdim=True)
+        coarse += int(((worse.nan_to_num() - want).abs() > tol).sum())
+    assert coarse > 0

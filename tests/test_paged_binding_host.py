@@ -63,3 +63,29 @@ def test_streams_that_may_differ_are_shared(P, heads, streams, tokens):
     # short ones are not worth joining
     assert need(20) == need(20000, 100) == 256
     assert L.lib().ss_cache_destroy(h) == 0
+
+
+def test_the_most_work_of_a_call(P):
+    """Units of work are counted in 31 bits: 31 streams of the widest tables fit, 32 do not."""
+    import ctypes as C
+
+    from paper_2609_02780_amd import _lib as L
+    fake, h = 0x7F0000000000, C.c_void_p()
+    d = L.CacheDesc(1, 28, 4, 128, 10, 600)
+    assert L.lib().ss_cache_create(C.byref(d), fake, 1 << 60, C.byref(h)) == 0
+    rows = L.Rows(fake, 128 * 512, 128)
+    out = L.Rows(fake + (1 << 30), 128 * 512, 128)
+
+    def attend(streams, width, ws=fake + (1 << 31)):
+        s = L.CacheStreams(fake, fake, fake, streams, width)
+        return L.lib().ss_cache_attend(h, C.byref(s), 0, streams, None, C.byref(rows), 0, None, None, ws, 0, None,
+                                       C.byref(out), None)
+
+    # (a workspace of 0 bytes: a call that could be planned is refused for that, and nothing runs)
+    assert attend(31, 2 ** 26 - 2) == L.SS_ERR_WORKSPACE
+    assert attend(32, 2 ** 26 - 2) == attend(512, 2 ** 26 - 2) == L.SS_ERR_UNSUPPORTED
+    for streams in (33, 100, 512):
+        widest = (2 ** 31 - 1) // streams - 2
+        assert attend(streams, widest) == L.SS_ERR_WORKSPACE
+        assert attend(streams, widest + 1) == L.SS_ERR_UNSUPPORTED
+    assert L.lib().ss_cache_destroy(h) == 0
