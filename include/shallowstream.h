@@ -651,8 +651,9 @@ typedef struct {
  *   positions     device int64 [n_tokens], or NULL: a token's place in its stream;
  *   queries       NULL, or n_q_heads heads, which are rotated alike into queries_out (may
  *                 be queries, rows and strides alike); rows that are passed over are not written.
- * A key is rotated in 64 bits and rounded to bf16 once; a block that becomes full is formed
- * from the bf16 rows, so the cache does not depend on how its tokens were cut into calls.
+ * A key is rotated in 64 bits (by the fp32 gain), then rounded to fp32 and from there to bf16, so that about
+ * one element in 2^17, all but half way between two bf16, becomes the farther one.  A block that becomes full
+ * is formed from the bf16 rows, so the cache does not depend on how its tokens were cut into calls.
  * Open rows of block b lie in half b & 1 of the slot.  The rows of the block that a call
  * begins in stay there too, unless the call ends an even number of blocks (2, 4, ...)
  * later: a call of at most 32 tokens a stream can be taken back, wholly or in

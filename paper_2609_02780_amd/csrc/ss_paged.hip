@@ -109,8 +109,9 @@ __device__ __forceinline__ int stream_length(const PagedDev& c, int s) {
 // in turns, position * (f / 2 pi), in 64 bits (a far position times a frequency loses what
 // matters in 32), less the nearest quarter turn, still in 64, and of the rest the Taylor series of sine and
 // cosine (x up to pi / 4).  Queries, which are rounded to bf16 and multiplied, take it in 32 bits, cut behind x^9 and
-// x^10 (off by less than 2^-28); keys that are cached, which a rounding the other way would keep so, in 64 bits up to
-// that rounding, cut behind x^13 and x^12 (2^-41; an append of 8,192 tokens 31.8 -> 32.9 us).  (64 bits for all: 1,777
+// x^10 (off by less than 2^-28); keys that are cached, which a rounding the other way would keep so, in 64 bits, cut
+// behind x^13 and x^12 (2^-41; an append of 8,192 tokens 31.8 -> 32.9 us), then rounded to fp32 and from there to bf16
+// (two roundings: one element in some 2^17, all but half way between two bf16, goes the other way).  (64 bits for all: 1,777
 // tokens of 16 heads 7.6 -> 9.1 us.  The hardware's sine and cosine, off by 2^-22.9, save nothing that the rows' traffic
 // does not cover.)
 //
@@ -714,9 +715,9 @@ __device__ __forceinline__ float of_lane(float x, int lane) {
 // k_paged_few: units of up to C columns (decoded tokens, a few drafts).  The W waves of a
 // block take its 32-token blocks in turn, each straight from memory to registers, and join
 // at the end of a unit.  Bound by reading the pages, so p is kept in two bf16 parts (16 bits
-// of it): the second product twice costs nothing (the matrix unit is busy for 13% of the clocks).
-// A token over 705,634 (723 MB) 113 us, 6.4 TB/s; for each of 64 streams (560 MB) 94 us, 6.0 TB/s; three for each of
-// 16 streams 43.
+// of it): the second product twice costs nothing (the matrix unit is busy for 12% of the clocks).
+// A token over 705,634 (723 MB) 113 us, 6.4 TB/s; for each of 64 streams (560 MB) 89 us, 6.3 TB/s; three for each of
+// 16 streams 36.
 // C = 16: 16x16x32 products.  Lane l = 16 g + r of S^T holds tokens 16 t + 4 g + e of column r;
 // a load of 16 bytes a lane brings piece 4 j + g of token 16 t + r, or the values of dimension
 // 32 c + 16 (g / 2) + r for half g & 1, of which the lanes 32 apart swap a half.
@@ -1004,7 +1005,7 @@ __device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts
 // vector unit, the other keeps the matrix unit busy, half an iteration behind.  WQ = 4 (33 to 128
 // columns): two blocks a CU, whose phases fall beside each other by themselves.
 // Bound by the matrix unit (busy for 62% of the clocks) and the clock that the card's power leaves it: 4,096 tokens,
-// the last of 16,384, 28 heads of 128: 743 us, 1.13 PFLOP/s.  At d = 64 by the vector unit's exponentials.
+// the last of 16,384, 28 heads of 128: 739 us, 1.14 PFLOP/s.  At d = 64 by the vector unit's exponentials.
 template <int D, int WQ>
 __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_many(PagedAttendArgs a, Spans spans) {
   constexpr bool TURNS = WQ == 8;
@@ -1327,8 +1328,8 @@ __global__ __launch_bounds__(64 * WQ, D == 64 && WQ == 4 ? 3 : 2) void k_paged_m
 }
 
 // k_paged_join: the parts of a unit's columns, brought to one maximum and added in a fixed order.  Eight
-// groups of d / 4 lanes share a column's parts.  Bound by its trips to memory: 129 parts of a token 5.5 us, 33 parts
-// of each of 448 columns 9.7.
+// groups of d / 4 lanes share a column's parts.  Bound by its trips to memory: 129 parts of a token 5.3 us, 33 parts
+// of each of 448 columns 9.6.
 template <int D, class SP>
 __global__ __launch_bounds__(2 * D) void k_paged_join(PagedAttendArgs a, SP spans, int bm) {
   constexpr int L4 = D / 4, NG = 8;
@@ -1401,7 +1402,7 @@ __global__ __launch_bounds__(2 * D) void k_paged_join(PagedAttendArgs a, SP span
 }
 
 // The same where units have many columns and few parts: a group of d / 4 lanes a column (a prompt's 4,096 tokens of 28
-// heads: 22 us).
+// heads: 20 us).
 template <int D>
 __global__ __launch_bounds__(256) void k_paged_join_many(PagedAttendArgs a, Spans spans, int bm) {
   constexpr int L4 = D / 4, ROWS = 256 / L4;
