@@ -1,4 +1,5 @@
-"""What the paged cache's binding holds for its calls cannot be exchanged beside them.  No GPU."""
+"""The paged cache on the host: what its binding holds for its calls cannot be exchanged beside them, and how
+attention is cut, by the workspaces that it asks for.  No GPU."""
 import os
 
 import pytest
